@@ -271,6 +271,86 @@ int moe_global_map(const moe_shape_t* shape, int32_t W, int32_t rank, const moe_
                    const int32_t* c_all, const moe_global_map_t* out, void* ws, size_t ws_bytes,
                    void* stream);
 
+/* ---- The shared projection with a low-rank adapter for each request ---------------
+ * Beside the routed experts a layer has dense projections (of a shared expert, of the router) that many
+ * requests share, each with a low-rank adapter of its own or none:
+ *   y[t] = x[t] W + s_a (x[t] A_a^T) B_a,   a = ids[t];   y[t] = x[t] W where ids[t] is outside [0, adapters)
+ * bf16 in, fp32 accumulate; h = s_a x A_a^T is kept to at least 16 bits of its fp32 value, and y is rounded once.  An
+ * adapter that holds infinities or NaN reaches the rows of its own tokens only.  Results are the same bits on every run.
+ * Limits (MOE_ERR_SHAPE otherwise): 0 <= T <= 2^26, K and N multiples of 8 from 8 to 2^17, T * max(K, N) <= 2^38, rank a
+ * multiple of 8 from 8 to 128, 1 <= adapters <= 1024. */
+typedef struct {
+    int32_t T;        /* tokens, packed: all requests' rows one behind the other, in any order */
+    int32_t K;        /* inner width: columns of x */
+    int32_t N;        /* outer width: columns of y */
+    int32_t rank;     /* of every adapter (zero rows fill up a smaller one) */
+    int32_t adapters;
+} moe_adapter_shape_t;
+
+/* Workspace of the forward and of the backward call, and bytes of the plan (host outputs; either may be NULL).  The plan of up to 256
+ * tokens has 0 bytes: moe_adapter_plan then enqueues nothing, and `plan` may be NULL everywhere. */
+int moe_adapter_workspace_bytes(const moe_adapter_shape_t* shape, size_t* ws_bytes, size_t* plan_bytes);
+
+/* Sorts the tokens by adapter (stable), for any number of forward and backward calls with the same ids, which have to
+ * stay as they are while the plan is in use.  ids: [T] int32. */
+int moe_adapter_plan(const moe_adapter_shape_t* shape, const int32_t* ids, void* plan, size_t plan_bytes, void* stream);
+
+/* Forward.
+ *   x      [T,K] bf16, rows ldx elements apart (a multiple of 8, at least K)
+ *   w      [K,N] bf16;   a [adapters,rank,K] bf16;   b [adapters,rank,N] bf16
+ *   scale  [adapters] fp32, or NULL (1)
+ *   ids    as given to the plan
+ *   y      [T,N] bf16, or fp32 with out_f32 = 1
+ *   h      NULL, or [T,rank] fp32: s x A^T of every token (0 without an adapter), which the backward call reads */
+int moe_adapter_forward(const moe_adapter_shape_t* shape, const void* x, int64_t ldx, const void* w, const void* a, const void* b,
+                        const float* scale, const int32_t* ids, const void* plan, void* y, int32_t out_f32, float* h, void* ws,
+                        size_t ws_bytes, void* stream);
+
+/* Backward given dy [T,N] bf16 (rows lddy apart): with g = s dy B^T,
+ *   dx [T,K] bf16 = dy W^T + g A;   da [adapters,rank,K] fp32 = sum over the adapter's tokens of g^T x;   db [adapters,rank,N] fp32 =
+ *   sum of h^T dy.  Adapters without tokens get zeros; W is frozen.
+ *   h      what the forward call wrote */
+int moe_adapter_backward(const moe_adapter_shape_t* shape, const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w,
+                         const void* a, const void* b, const float* scale, const int32_t* ids, const void* plan, const float* h,
+                         void* dx, float* da, float* db, void* ws, size_t ws_bytes, void* stream);
+
+/* ---- The router's balance loss and z loss -------------------------------------------
+ * Over the kept tokens of each packed sequence s, with p = softmax(logits) over all E experts:
+ *   P[s,e] = sum p[t,e];  c[s,e] = slots of these tokens with expert e;  f[s,e] = c[s,e] / (k tokens[s])
+ *   balance = E / n sum_s sum_e f[s,e] P[s,e];  z = 1 / n sum_t lse[t]^2;  loss = balance_coef balance + z_coef z
+ * n = all kept tokens (losses are 0 where none is).  Limits (MOE_ERR_SHAPE otherwise): 0 <= T, 1 <= E <= 1024, 1 <= k <= min(16, E), T * k < 2^30,
+ * 1 <= seqs <= 65536. */
+typedef struct {
+    int32_t T, E, k, seqs;
+    float balance_coef, z_coef;
+} moe_balance_shape_t;
+
+typedef struct {          /* device pointers: written by the forward call, counts, tokens and lse read by the backward one */
+    float* loss;          /* [3]  loss, balance, z */
+    int32_t* counts;      /* [seqs,E] */
+    int32_t* tokens;      /* [seqs + 1]  kept tokens of every sequence, then n */
+    float* prob_sums;     /* [seqs,E]  P */
+    float* lse;           /* [T]  log sum exp of the logits; -inf where the token is not kept */
+} moe_balance_stats_t;
+
+int moe_balance_workspace_bytes(const moe_balance_shape_t* shape, size_t* ws_bytes);
+
+/* Forward.
+ *   logits       [T,E] fp32
+ *   topk_idx     [T,k] int32, as moe_route writes it (values outside [0,E) are no slot)
+ *   seq_offsets  [seqs + 1] int32, ascending from 0 to T; NULL: one sequence (seqs must be 1)
+ *   mask         [T] bytes, 0 = not kept (padding: its logits are not looked at), or NULL (all kept) */
+int moe_balance_forward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
+                        const uint8_t* mask, const moe_balance_stats_t* out, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradient of the logits, every element written: with u = dloss[0] (fp32, device) the gradient of `loss`, counts being constants,
+ *   dlogits[t,e] = p (u balance_coef E / n (f[s,e] - sum_j f[s,j] p[t,j]) + u z_coef 2 / n lse[t])   for kept tokens, else 0,
+ * and, where topk_w and dtopk_w [T,k] fp32 are given (both or neither), for every token what moe_route_backward computes from them.
+ *   dlogits      [T,E] fp32, or bf16 with out_bf16 = 1 */
+int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
+                         const uint8_t* mask, const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w,
+                         const float* dloss, void* dlogits, int32_t out_bf16, void* stream);
+
 /* Synchronises `stream`, reads the status word a forward/backward call left in
  * its workspace and returns MOE_OK or MOE_ERR_DEVICE (test and debug aid; the
  * hot path never calls it). */

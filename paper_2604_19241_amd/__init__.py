@@ -11,4 +11,7 @@ from .binding import (  # noqa: F401
     saved_views, status_string,
     MoEPerfConfig, MoEPerfHw, MoEPerfProblem, make_perf_hw, make_perf_problem,
     moe_perf_model_eval, moe_perf_model_search,
+    AdapterPlan, BalanceStats, MoEAdapterShape, MoEBalanceShape, make_adapter_shape, make_balance_shape,
+    moe_adapter_backward, moe_adapter_forward, moe_adapter_plan, moe_adapter_workspace_bytes,
+    moe_balance_backward, moe_balance_forward, moe_balance_workspace_bytes,
 )

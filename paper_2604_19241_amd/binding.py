@@ -22,7 +22,8 @@ MOE_ERR_ARG, MOE_ERR_SHAPE, MOE_ERR_WORKSPACE, MOE_ERR_HIP, MOE_ERR_DEVICE = -1,
 EXPORTS = ("moe_workspace_bytes", "moe_backward_workspace_bytes", "moe_saved_layout", "moe_route", "moe_fused_forward",
            "moe_fused_backward", "moe_route_backward", "moe_global_map", "moe_device_status",
            "moe_status_string", "moe_calibration_copy", "moe_perf_model_eval",
-           "moe_perf_model_search", "moe_route_static", "moe_calibration_mfma")
+           "moe_perf_model_search", "moe_route_static", "moe_calibration_mfma", "moe_adapter_workspace_bytes", "moe_adapter_plan",
+           "moe_adapter_forward", "moe_adapter_backward", "moe_balance_workspace_bytes", "moe_balance_forward", "moe_balance_backward")
 
 ROUTE_STATIC_SCRATCH_BYTES = 4 << 20   # MOE_ROUTE_STATIC_SCRATCH_BYTES
 
@@ -52,7 +53,7 @@ class MoEError(RuntimeError):
 
 # Every function that takes a pointer from _ptr or _stream: with the types declared once, pointers and sizes go over as plain integers (an object made for each
 # argument of each call took as long as two launches).
-_P, _N, _I = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32
+_P, _N, _I, _L = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int32, ctypes.c_int64
 _ARGTYPES = {
     "moe_route": [_P, _P, _P, _P, _N, _P],
     "moe_route_static": [_P, _P, _P, _P],
@@ -63,6 +64,11 @@ _ARGTYPES = {
     "moe_device_status": [_P, _P],
     "moe_calibration_copy": [_P, _P, _N, _P],
     "moe_calibration_mfma": [_I, _I, _I, _P, _P, _P, _P],
+    "moe_adapter_plan": [_P, _P, _P, _N, _P],
+    "moe_adapter_forward": [_P, _P, _L, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P, _N, _P],
+    "moe_adapter_backward": [_P, _P, _L, _P, _L] + [_P] * 10 + [_P, _N, _P],
+    "moe_balance_forward": [_P] * 7 + [_N, _P],
+    "moe_balance_backward": [_P] * 10 + [_I, _P],
 }
 _lib = None
 
@@ -346,6 +352,178 @@ def saved_views(shape: MoEShape, saved: torch.Tensor) -> dict:
         return saved[off:off + A * cols * 2].view(torch.bfloat16).view(A, cols)
 
     return {"gu": view(L["gu"], 2 * shape.I), "h": view(L["h"], shape.I), "o": view(L["o"], shape.d)}
+
+
+# ---- the shared projection with a low-rank adapter for each request ----------
+
+class MoEAdapterShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "K", "N", "rank", "adapters")]
+
+
+def make_adapter_shape(T, K, N, rank, adapters) -> MoEAdapterShape:
+    return MoEAdapterShape(T, K, N, rank, adapters)
+
+
+def _adapter_bytes(shape: MoEAdapterShape) -> tuple:
+    ws, plan = ctypes.c_size_t(0), ctypes.c_size_t(0)
+    _check(load_library().moe_adapter_workspace_bytes(ctypes.byref(shape), ctypes.byref(ws), ctypes.byref(plan)),
+           "moe_adapter_workspace_bytes")
+    return ws.value, plan.value
+
+
+def moe_adapter_workspace_bytes(shape: MoEAdapterShape) -> int:
+    return _adapter_bytes(shape)[0]
+
+
+@dataclass
+class AdapterPlan:
+    """The tokens of one batch by adapter.  `ids` has to stay as it is while the plan is in use."""
+    ids: torch.Tensor                 # [T] i32, outside [0, adapters): no adapter
+    table: Optional[torch.Tensor]     # None for few tokens: nothing is sorted
+
+
+def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
+    """Sorts the tokens by adapter, once for all projections of the batch with as many adapters."""
+    assert ids.is_cuda and ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == (shape.T,)
+    nbytes = _adapter_bytes(shape)[1]
+    if nbytes == 0:
+        return AdapterPlan(ids, None)
+    table = ids.new_empty(nbytes // 4)
+    _check(load_library().moe_adapter_plan(ctypes.byref(shape), _ptr(ids), _ptr(table), nbytes, _stream(ids.device)),
+           "moe_adapter_plan")
+    return AdapterPlan(ids, table)
+
+
+def _adapter_rows(t: torch.Tensor, T: int, width: int) -> int:
+    """Elements from one row of t to the next."""
+    assert t.is_cuda and t.dtype == torch.bfloat16 and t.shape == (T, width) and t.stride(1) == 1
+    return t.stride(0) if T > 1 else width
+
+
+def _adapter_operands(shape: MoEAdapterShape, w, a, b, scale, plan: AdapterPlan):
+    K, N, r, n = shape.K, shape.N, shape.rank, shape.adapters
+    for t, size in ((w, (K, N)), (a, (n, r, K)), (b, (n, r, N))):
+        assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.shape == size
+    assert scale is None or (scale.is_cuda and scale.dtype == torch.float32 and scale.is_contiguous() and scale.shape == (n,))
+    assert plan.ids.shape == (shape.T,)
+
+
+def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, scale=None, out_dtype=torch.bfloat16,
+                        h: torch.Tensor | None = None, y: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """y[t] = x[t] w + scale[i] (x[t] a[i]^T) b[i] with i = ids[t]: x [T,K] (rows may be parts of wider ones), w [K,N],
+    a [adapters,rank,K], b [adapters,rank,N], all bf16; scale [adapters] fp32.  h [T,rank] fp32, if given, receives what
+    moe_adapter_backward reads."""
+    ldx = _adapter_rows(x, shape.T, shape.K)
+    _adapter_operands(shape, w, a, b, scale, plan)
+    assert out_dtype in (torch.bfloat16, torch.float32)
+    if y is None:
+        y = x.new_empty((shape.T, shape.N), dtype=out_dtype)
+    assert y.is_cuda and y.dtype == out_dtype and y.is_contiguous() and y.shape == (shape.T, shape.N)
+    if h is not None:
+        assert h.is_cuda and h.dtype == torch.float32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
+    if ws is None:
+        ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
+    _check(load_library().moe_adapter_forward(
+        ctypes.byref(shape), _ptr(x), ldx, _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.ids), _ptr(plan.table), _ptr(y),
+        1 if out_dtype == torch.float32 else 0, _ptr(h), _ptr(ws), ws.numel(), _stream(x.device)), "moe_adapter_forward")
+    return y
+
+
+def moe_adapter_backward(shape: MoEAdapterShape, dy, x, w, a, b, plan: AdapterPlan, h, scale=None, out: dict | None = None,
+                         ws: torch.Tensor | None = None) -> dict:
+    """Gradients of x (bf16) and of every adapter's two factors (fp32); w is frozen.  h as moe_adapter_forward wrote it."""
+    lddy, ldx = _adapter_rows(dy, shape.T, shape.N), _adapter_rows(x, shape.T, shape.K)
+    _adapter_operands(shape, w, a, b, scale, plan)
+    assert h.is_cuda and h.dtype == torch.float32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
+    if out is None:
+        out = {"dx": x.new_empty((shape.T, shape.K)), "da": h.new_empty(a.shape), "db": h.new_empty(b.shape)}
+    for key, dtype, size in (("dx", torch.bfloat16, x.shape), ("da", torch.float32, a.shape), ("db", torch.float32, b.shape)):
+        t = out[key]
+        assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == size
+    if ws is None:
+        ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
+    _check(load_library().moe_adapter_backward(
+        ctypes.byref(shape), _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.ids), _ptr(plan.table),
+        _ptr(h), _ptr(out["dx"]), _ptr(out["da"]), _ptr(out["db"]), _ptr(ws), ws.numel(), _stream(x.device)), "moe_adapter_backward")
+    return out
+
+
+# ---- the router's balance loss and z loss ------------------------------------
+
+class MoEBalanceShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "E", "k", "seqs")] + [(n, ctypes.c_float) for n in ("balance_coef", "z_coef")]
+
+
+class MoEBalanceStatsC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("loss", "counts", "tokens", "prob_sums", "lse")]
+
+
+@dataclass
+class BalanceStats:
+    loss: torch.Tensor        # [3] f32: balance_coef balance + z_coef z, balance, z
+    counts: torch.Tensor      # [seqs,E] i32
+    tokens: torch.Tensor      # [seqs+1] i32: kept tokens of every sequence, then of all
+    prob_sums: torch.Tensor   # [seqs,E] f32
+    lse: torch.Tensor         # [T] f32, -inf where a token is not kept
+
+    def c_struct(self) -> MoEBalanceStatsC:
+        return MoEBalanceStatsC(self.loss.data_ptr(), self.counts.data_ptr(), self.tokens.data_ptr(), self.prob_sums.data_ptr(),
+                                self.lse.data_ptr())
+
+
+def make_balance_shape(T, E, k, seqs=1, balance_coef=0.01, z_coef=0.001) -> MoEBalanceShape:
+    return MoEBalanceShape(T, E, k, seqs, balance_coef, z_coef)
+
+
+def moe_balance_workspace_bytes(shape: MoEBalanceShape) -> int:
+    ws = ctypes.c_size_t(0)
+    _check(load_library().moe_balance_workspace_bytes(ctypes.byref(shape), ctypes.byref(ws)), "moe_balance_workspace_bytes")
+    return ws.value
+
+
+def _balance_inputs(shape: MoEBalanceShape, logits, topk_idx, seq_offsets, mask):
+    assert logits.is_cuda and logits.dtype == torch.float32 and logits.is_contiguous() and logits.shape == (shape.T, shape.E)
+    assert topk_idx.is_cuda and topk_idx.dtype == torch.int32 and topk_idx.is_contiguous() and topk_idx.shape == (shape.T, shape.k)
+    if seq_offsets is not None:
+        assert seq_offsets.is_cuda and seq_offsets.dtype == torch.int32 and seq_offsets.is_contiguous()
+        assert seq_offsets.shape == (shape.seqs + 1,)
+    if mask is not None:
+        assert mask.is_cuda and mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.shape == (shape.T,)
+
+
+def moe_balance_forward(shape: MoEBalanceShape, logits, topk_idx, seq_offsets=None, mask=None, ws: torch.Tensor | None = None) -> BalanceStats:
+    """Balance loss and z loss of a router's logits [T,E] fp32 and its selection [T,k] int32, over the packed sequences that
+    seq_offsets [seqs+1] int32 cuts (one without) and the tokens that mask [T] keeps."""
+    _balance_inputs(shape, logits, topk_idx, seq_offsets, mask)
+    S = shape.seqs
+    counts = topk_idx.new_empty((S, shape.E))
+    st = BalanceStats(logits.new_empty(3), counts, counts.new_empty(S + 1), logits.new_empty((S, shape.E)), logits.new_empty(shape.T))
+    if ws is None:
+        ws = _ws(moe_balance_workspace_bytes(shape), logits.device)
+    cs = st.c_struct()
+    _check(load_library().moe_balance_forward(ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), _ptr(mask),
+                                              ctypes.byref(cs), _ptr(ws), ws.numel(), _stream(logits.device)), "moe_balance_forward")
+    return st
+
+
+def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: BalanceStats, dloss, seq_offsets=None, mask=None, topk_w=None,
+                         dtopk_w=None, out_dtype=torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient [T,E] of the logits for the gradient dloss [1] of stats.loss[0]; with topk_w and dtopk_w also what
+    moe_route_backward would give, added before the one rounding.  mask and seq_offsets as in the forward call."""
+    _balance_inputs(shape, logits, topk_idx, seq_offsets, mask)
+    for t in (topk_w, dtopk_w):
+        if t is not None:
+            assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (shape.T, shape.k)
+    assert dloss.is_cuda and dloss.dtype == torch.float32 and dloss.numel() == 1
+    assert out_dtype in (torch.float32, torch.bfloat16)
+    if out is None:
+        out = logits.new_empty((shape.T, shape.E), dtype=out_dtype)
+    assert out.is_cuda and out.dtype == out_dtype and out.is_contiguous() and out.shape == (shape.T, shape.E)
+    cs = stats.c_struct()
+    _check(load_library().moe_balance_backward(
+        ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), _ptr(mask), ctypes.byref(cs), _ptr(topk_w), _ptr(dtopk_w),
+        _ptr(dloss), _ptr(out), 1 if out_dtype == torch.bfloat16 else 0, _stream(logits.device)), "moe_balance_backward")
+    return out
 
 
 # ---- analytical performance model and configuration search (host only) -------

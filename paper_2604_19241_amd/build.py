@@ -15,7 +15,7 @@ PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libuniep_moe.so"
 BUILD = PKG.parent / "_build"
-SOURCES = ["route.hip", "forward.hip", "backward.hip", "api.hip", "perf_model.hip"]
+SOURCES = ["route.hip", "forward.hip", "backward.hip", "adapter.hip", "balance.hip", "api.hip", "perf_model.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
@@ -39,7 +39,7 @@ def _compile(src: str, save_temps: bool) -> Path:
     return obj
 
 
-def build(save_temps: bool = False, jobs: int = 4) -> Path:
+def build(save_temps: bool = False, jobs: int = 6) -> Path:
     BUILD.mkdir(exist_ok=True)
     with ThreadPoolExecutor(max_workers=jobs) as ex:
         objs = list(ex.map(lambda s: _compile(s, save_temps), SOURCES))

@@ -1,0 +1,1000 @@
+// The shared projection with a low-rank adapter for each request, and its gradients (the mathematics: adapter.hpp).
+//
+// Forward and the gradient of x are one operation: x W + s (x A^T) B and dy W^T + s (dy B^T) A differ in which factor comes
+// first and in the form of W, so `x`, `first` and `second` below are x, A, B or dy, B, A; R is the reduction's length and C
+// the columns of the result.  The gradients of the factors, dA_a = sum_t g[t]^T x[t] with g = s dy B^T and dB_a = sum_t h[t]^T dy[t] with
+// h = s x A^T, are reductions over the tokens of one adapter.
+//
+// Few tokens (kFewTokens): two launches and no plan.  The first computes x W cut along R into fp32 parts, and the likewise cut h of
+// every group of tokens with one adapter, side by side; the second adds the parts, then h B, and rounds once.  Each workgroup finds the
+// tokens of its adapter by itself, from a ballot over the ids.
+// More tokens: a plan sorts them by adapter (stable, one launch), a launch computes h, and the tiles of the product run on over
+// their low-rank part (adapter.hpp).
+// No atomic decides an order anywhere: results are the same bits on every run.
+#include "adapter.hpp"
+
+#include <algorithm>
+
+namespace uniep {
+
+typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4v_t;
+typedef __attribute__((address_space(3))) char* lds_ptr3_t;
+typedef __attribute__((address_space(3))) bf16x4v_t* lds_tr3_t;
+
+constexpr int kFewTokens = 256;
+constexpr int kBlockRows = 32;        // rows of a block of the plan (one fragment)
+constexpr int kUnit = 64;             // rows of which the plan knows the first and the last segment
+
+// ------------------------------------------------------------------ the plan
+// int32 words: [0] blocks, [1] segments, [2] rows without an adapter, then the arrays.
+struct PlanView {
+    int32_t* head;
+    int32_t* order;      // [T] row -> token: those without an adapter, then by adapter, each in the order of the tokens
+    int32_t* start;      // [n + 1] first row of an adapter
+    int32_t* ordinal;    // [n] which segment an adapter is
+    int32_t* seg;        // [n] segment -> adapter
+    int32_t* unit;       // [units][2] segments of the first and the last row of every kUnit rows (-1: no adapter)
+    int32_t* block;      // [blocks][2] first row; rows | (adapter + 1) << 8.  One adapter, one multiple of kBlockRows
+};
+static size_t plan_blocks(const moe_adapter_shape_t& s) { return (size_t)s.T / kBlockRows + s.adapters + 2; }
+static size_t plan_units(const moe_adapter_shape_t& s) { return ((size_t)s.T + kUnit - 1) / kUnit; }
+static size_t plan_words(const moe_adapter_shape_t& s) {
+    return 16 + (size_t)s.T + 3 * (size_t)s.adapters + 1 + 2 * plan_units(s) + 2 * plan_blocks(s);
+}
+static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
+    PlanView v;
+    v.head = (int32_t*)plan;
+    v.block = v.head + 16;                       // (pairs first: 8-byte aligned)
+    v.unit = v.block + 2 * plan_blocks(s);
+    v.order = v.unit + 2 * plan_units(s);
+    v.start = v.order + s.T;
+    v.ordinal = v.start + s.adapters + 1;
+    v.seg = v.ordinal + s.adapters;
+    return v;
+}
+bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= kFewTokens; }
+size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) ? 0 : plan_words(s) * 4; }
+
+// One workgroup: a counting sort.  Every wave counts a contiguous part of the tokens and later gives its tokens their rows, 64 at a
+// time: lanes with the same adapter find each other with a ballot for each bit of the id.
+constexpr int kSortWaves = 16;
+__global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, const int32_t* __restrict__ ids, PlanView v) {
+    __shared__ int32_t hist[kSortWaves][kMaxAdapters + 1];
+    __shared__ int32_t first[kMaxAdapters + 2];     // rows before bin b (bin 0: no adapter, bin a + 1: adapter a)
+    __shared__ int32_t fblock[kMaxAdapters + 2], fseg[kMaxAdapters + 2];
+    __shared__ int32_t carry[3][kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, bins = n + 1;
+    const uint64_t below = (1ull << lane) - 1ull;
+    for (int b = lane; b < bins; b += 64) hist[w][b] = 0;
+    const int part = ((T + kSortWaves - 1) / kSortWaves + 63) & ~63, lo = min(T, w * part), hi = min(T, lo + part);
+    auto bin_of = [&](int t) {
+        const int a = t < hi ? ids[t] : -1;
+        return (unsigned)a < (unsigned)n ? a + 1 : 0;
+    };
+    __syncthreads();
+    for (int t = lo + lane; t < hi; t += 64) atomicAdd(&hist[w][bin_of(t)], 1);
+    __syncthreads();
+    // bins -> first rows, blocks and segments: thread b has bin b (two at most a thread: 1025 bins)
+    int base_rows = 0, base_blocks = 0, base_segs = 0;
+    for (int b0 = 0; b0 < bins; b0 += 64 * kSortWaves) {
+        const int b = b0 + tid;
+        int c = 0;
+        if (b < bins)
+            for (int k = 0; k < kSortWaves; ++k) c += hist[k][b];
+        auto scan = [&](int x, int which, int base, int& total) {
+            int p = x;
+#pragma unroll
+            for (int o = 1; o < 64; o <<= 1) {
+                const int u = __shfl_up(p, o);
+                if (lane >= o) p += u;
+            }
+            if (lane == 63) carry[which][w] = p;
+            __syncthreads();
+            int before = base;
+            total = 0;
+#pragma unroll
+            for (int k = 0; k < kSortWaves; ++k) {
+                if (k < w) before += carry[which][k];
+                total += carry[which][k];
+            }
+            return before + p - x;
+        };
+        int total;
+        const int r0 = scan(c, 0, base_rows, total);
+        base_rows += total;
+        const int nb = c > 0 ? (r0 + c - 1) / kBlockRows - r0 / kBlockRows + 1 : 0;
+        const int k0 = scan(nb, 1, base_blocks, total);
+        base_blocks += total;
+        const int s0 = scan(b > 0 && c > 0 ? 1 : 0, 2, base_segs, total);
+        base_segs += total;
+        if (b < bins) {
+            first[b] = r0;
+            fblock[b] = k0;
+            fseg[b] = s0;
+            int at = r0;
+            for (int k = 0; k < kSortWaves; ++k) {
+                const int h = hist[k][b];
+                hist[k][b] = at;
+                at += h;
+            }
+            if (b > 0) {
+                v.start[b - 1] = r0;
+                v.ordinal[b - 1] = s0;
+                if (c > 0) v.seg[s0] = b - 1;
+            }
+        }
+        __syncthreads();
+    }
+    if (tid == 0) {
+        first[bins] = T;
+        fblock[bins] = base_blocks;
+        v.start[n] = T;
+        v.head[0] = base_blocks;
+        v.head[1] = base_segs;
+        v.head[2] = bins > 1 ? first[1] : T;
+    }
+    __syncthreads();
+    // rows
+    volatile int32_t* mine = hist[w];
+    for (int t0 = lo; t0 < hi; t0 += 64) {
+        const int t = t0 + lane, b = bin_of(t);
+        uint64_t same = __ballot(t < hi);
+        for (int bit = 0; (bins - 1) >> bit; ++bit) {
+            const uint64_t m = __ballot((b >> bit) & 1);
+            same &= (b >> bit) & 1 ? m : ~m;
+        }
+        if (t < hi) {
+            const int at = mine[b];
+            v.order[at + __popcll(same & below)] = t;
+            __builtin_amdgcn_wave_barrier();
+            if ((same >> lane) == 1ull) mine[b] = at + __popcll(same);   // the last of them
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+    // blocks and units, a wave a bin
+    for (int b = w; b < bins; b += kSortWaves) {
+        const int r0 = first[b], r1 = first[b + 1], o = b > 0 ? fseg[b] : -1;
+        if (r1 <= r0) continue;
+        const int q0 = r0 / kBlockRows, q1 = (r1 - 1) / kBlockRows;
+        for (int q = q0 + lane; q <= q1; q += 64) {
+            const int a = max(r0, q * kBlockRows), e = min(r1, (q + 1) * kBlockRows);
+            v.block[2 * (fblock[b] + q - q0)] = a;
+            v.block[2 * (fblock[b] + q - q0) + 1] = (e - a) | b << 8;
+        }
+        for (int u = r0 / kUnit + lane; u <= (r1 - 1) / kUnit; u += 64) {
+            if (u * kUnit >= r0) v.unit[2 * u] = o;
+            if (min(T, (u + 1) * kUnit) <= r1) v.unit[2 * u + 1] = o;
+        }
+    }
+}
+
+int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st) {
+    if (adapter_few(s)) return MOE_OK;
+    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, ids, plan_view(s, plan));
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+// ------------------------------------------------------------------ parameters
+struct ProjParams {
+    int T, R, C, r, n;
+    const char* x;          // [T][ldx bytes]
+    size_t ldx;
+    const char* w;          // KS: [R][C], KC: [C][R]
+    const char* first;      // [n][r][R]
+    const char* second;     // [n][r][C]
+    const float* scale;     // [n] or NULL
+    const int32_t* ids;
+    char* y;                // [T][C] bf16, or fp32
+    int out_f32;
+    float* h;               // [T][r], or NULL where nobody wants it (few tokens)
+    // few tokens
+    float* part;            // [splits][T][C]
+    float* hpart;           // [hsplits][T][r]
+    int splits, per_split, hsplits, hper_split;
+    int col_tiles, row_tiles, rank_tiles;
+    // more
+    PlanView plan;
+    char* hx;               // the low-rank rows of every tile (hx_base)
+    char* second_t;         // [n][C][r] (KC)
+    int tile_rows;
+    int blocks;             // at most, of the plan
+};
+struct GradParams {
+    int T, r, n, few;
+    int W[2];               // columns: dB (of dy, with h), dA (of x, with g)
+    const char* x[2];
+    size_t ldx[2];
+    const float* h[2];      // [T][r]; NULL: hpart (few tokens)
+    float* out[2];          // [n][r][W]
+    int col_tiles[2], rank_tiles;
+};
+
+__device__ __forceinline__ int adapter_of(const int32_t* ids, int t, int n) {
+    const int a = ids[t];
+    return (unsigned)a < (unsigned)n ? a : -1;
+}
+__device__ __forceinline__ Stages stages_of(int R) { return Stages{R / BK, R % BK}; }
+
+// ------------------------------------------------------------------ few tokens
+// Which tokens have adapter `a`: bit t of the four words.  256 threads, two barriers.
+struct Members {
+    uint64_t m[4];
+    __device__ __forceinline__ void find(int T, int n, const int32_t* ids, int a, uint64_t* s_mask) {
+        const int tid = threadIdx.x;
+        const uint64_t b = __ballot(tid < T && adapter_of(ids, tid < T ? tid : 0, n) == a);
+        if ((tid & 63) == 0) s_mask[tid >> 6] = b;
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m[i] = s_mask[i];
+    }
+    __device__ __forceinline__ int before(int t) const {
+        int c = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int k = t - 64 * i;
+            c += __popcll(k <= 0 ? 0ull : k >= 64 ? m[i] : m[i] & ((1ull << k) - 1ull));
+        }
+        return c;
+    }
+    __device__ __forceinline__ int count() const { return before(256); }
+};
+// The tokens from the `skip`-th member on, up to `most`, in list[]; ends with a barrier.
+__device__ __forceinline__ void list_members(const Members& mb, int skip, int most, int32_t* list) {
+    const int tid = threadIdx.x, w = tid >> 6;
+    const uint64_t mine = w == 0 ? mb.m[0] : w == 1 ? mb.m[1] : w == 2 ? mb.m[2] : mb.m[3];
+    if ((mine >> (tid & 63)) & 1) {
+        const int k = mb.before(tid) - skip;
+        if (k >= 0 && k < most) list[k] = tid;
+    }
+    __syncthreads();
+}
+
+// Parts of x W and of h.  Tasks: (column tile, split, row tile), then (token, rank tile, split): a workgroup whose token is not every
+// 32nd of its adapter's has nothing to do.
+template <int NRF, int FORM>
+__global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjParams p) {
+    __shared__ __attribute__((aligned(512))) char smem[SmallTile<NRF, 2>::kLds];
+    __shared__ uint64_t s_mask[4];
+    __shared__ int32_t s_list[32];
+    const Stages all = stages_of(p.R);
+    const int nst = all.full + (all.tail > 0);
+    int id = blockIdx.x;
+    const int pairs = p.col_tiles * p.splits, gemm = pairs * p.row_tiles;
+    auto part_of = [&](int s0, int s1) { return Stages{min(all.full, s1) - s0, s1 > all.full ? all.tail : 0}; };
+    if (id < gemm) {
+        const int pair = id % pairs, rt = id / pairs, ct = pair % p.col_tiles, sp = pair / p.col_tiles;
+        const int s0 = sp * p.per_split, s1 = min(nst, s0 + p.per_split);
+        const int row0 = rt * 32 * NRF, rows = min(32 * NRF, p.T - row0);
+        const Stages st = part_of(s0, s1);
+        f32x16_t acc[NRF][2];
+        {
+            const Lane ln;
+            KcStages<NRF, false> lb;
+            lb.init(ln, rows, st, [&](int r) { return p.x + (size_t)(row0 + r) * p.ldx + (size_t)s0 * (BK * 2); });
+            lb.low.used = 0;
+            if constexpr (FORM == kKs) {
+                KsStages<2, 64> la;
+                la.init(ln, p.w + (size_t)s0 * BK * p.C * 2, 64 * ct, p.C, st);
+                small_loop<NRF, 2, kKs>(lb, la, s1 - s0, smem, acc);
+            } else {
+                KcStages<2, true> la;
+                la.init(ln, min(64, p.C - 64 * ct), st, [&](int c) { return p.w + ((size_t)(64 * ct + c) * p.R + (size_t)s0 * BK) * 2; });
+                small_loop<NRF, 2, kKc>(lb, la, s1 - s0, smem, acc);
+            }
+        }
+        small_sum<NRF, 2>(smem, acc, [&](int row, int col, const float (&v)[8]) {
+            col += 64 * ct;
+            if (row >= rows || col >= p.C) return;
+            f32x4_t* to = (f32x4_t*)(p.part + ((size_t)sp * p.T + row0 + row) * p.C + col);
+            to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+            to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+        });
+        return;
+    }
+    id -= gemm;
+    const int t = id % p.T, rest = id / p.T, rt = rest % p.rank_tiles, sp = rest / p.rank_tiles;
+    const int a = adapter_of(p.ids, t, p.n);
+    if (a < 0) return;
+    Members mb;
+    mb.find(p.T, p.n, p.ids, a, s_mask);
+    const int rank = mb.before(t);
+    if (rank % 32 != 0) return;
+    list_members(mb, rank, 32, s_list);
+    const int rows = min(32, mb.count() - rank);
+    const int s0 = sp * p.hper_split, s1 = min(nst, s0 + p.hper_split);
+    const Stages st = part_of(s0, s1);
+    f32x16_t acc[1][2];
+    {
+        const Lane ln;
+        KcStages<1, false> lb;
+        lb.init(ln, rows, st, [&](int r) { return p.x + (size_t)s_list[r] * p.ldx + (size_t)s0 * (BK * 2); });
+        lb.low.used = 0;
+        KcStages<2, true> la;
+        la.init(ln, min(64, p.r - 64 * rt), st, [&](int j) { return p.first + (((size_t)a * p.r + 64 * rt + j) * p.R + (size_t)s0 * BK) * 2; });
+        small_loop<1, 2, kKc>(lb, la, s1 - s0, smem, acc);
+    }
+    small_sum<1, 2>(smem, acc, [&](int row, int col, const float (&v)[8]) {
+        col += 64 * rt;
+        if (row >= rows || col >= p.r) return;
+        f32x4_t* to = (f32x4_t*)(p.hpart + ((size_t)sp * p.T + s_list[row]) * p.r + col);
+        to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+        to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+    });
+}
+
+// s h[t][j] from its parts
+__device__ __forceinline__ float whole_h(const ProjParams& p, int t, int j, float s) {
+    float v = 0.f;
+    for (int k = 0; k < p.hsplits; ++k) v += p.hpart[((size_t)k * p.T + t) * p.r + j];
+    return v * s;
+}
+__device__ __forceinline__ void fma8(float (&acc)[8], float h, u32x4_t b) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+        acc[2 * q] += h * bf16_lo(b[q]);
+        acc[2 * q + 1] += h * bf16_hi(b[q]);
+    }
+}
+
+// y of up to 4 tokens with one adapter and 512 columns: the waves share the parts and the ranks, and their sums are added in LDS.
+constexpr int kJoinTokens = 4, kJoinCols = 512;
+struct JoinShared {
+    float h[kJoinTokens][kMaxRank];
+    float sums[4][kJoinTokens][kJoinCols];
+    uint64_t mask[4];
+    int32_t list[kJoinTokens];
+};
+__device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, JoinShared& S) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int a = adapter_of(p.ids, t, p.n);
+    Members mb;
+    mb.find(p.T, p.n, p.ids, a, S.mask);
+    const int rank = mb.before(t);
+    if (rank % kJoinTokens != 0) return;
+    list_members(mb, rank, kJoinTokens, S.list);
+    const int rows = min(kJoinTokens, mb.count() - rank);
+    if (a >= 0 || p.h) {
+        const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
+        for (int i = tid; i < rows * p.r; i += 256) {
+            const int m = i / p.r, j = i - m * p.r, tok = S.list[m];
+            const float v = a < 0 ? 0.f : whole_h(p, tok, j, s);
+            S.h[m][j] = v;
+            if (p.h && cb == 0) p.h[(size_t)tok * p.r + j] = v;
+        }
+        __syncthreads();
+    }
+    const int c = cb * kJoinCols + 8 * lane;
+    float acc[kJoinTokens][8] = {};
+    if (c < p.C) {
+        for (int s = w; s < p.splits; s += 4)
+#pragma unroll
+            for (int m = 0; m < kJoinTokens; ++m)
+                if (m < rows) {
+                    const f32x4_t* q = (const f32x4_t*)(p.part + ((size_t)s * p.T + S.list[m]) * p.C + c);
+                    const f32x4_t u = q[0], v = q[1];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        acc[m][j] += u[j];
+                        acc[m][4 + j] += v[j];
+                    }
+                }
+        if (a >= 0) {
+            const char* f = p.second + ((size_t)a * p.r * p.C + c) * 2;
+#pragma unroll 4
+            for (int j = w; j < p.r; j += 4) {
+                const u32x4_t b = *(const u32x4_t*)(f + (size_t)j * p.C * 2);
+#pragma unroll
+                for (int m = 0; m < kJoinTokens; ++m)
+                    if (m < rows) fma8(acc[m], S.h[m][j], b);
+            }
+        }
+#pragma unroll
+        for (int m = 0; m < kJoinTokens; ++m)
+            if (m < rows) {
+                *(f32x4_t*)&S.sums[w][m][8 * lane] = f32x4_t{acc[m][0], acc[m][1], acc[m][2], acc[m][3]};
+                *(f32x4_t*)&S.sums[w][m][8 * lane + 4] = f32x4_t{acc[m][4], acc[m][5], acc[m][6], acc[m][7]};
+            }
+    }
+    __syncthreads();
+    if (w >= rows || c >= p.C) return;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = ((S.sums[0][w][8 * lane + j] + S.sums[1][w][8 * lane + j]) + S.sums[2][w][8 * lane + j]) + S.sums[3][w][8 * lane + j];
+    const size_t at = (size_t)S.list[w] * p.C + c;
+    if (p.out_f32) {
+        f32x4_t* to = (f32x4_t*)(p.y + at * 4);
+        to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+        to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+    } else {
+        *(u32x4_t*)(p.y + at * 2) = pack8f(v);
+    }
+}
+
+// Gradients of 8 ranks a wave and 512 columns of one adapter, token by token: the waves have different ranks, of a low rank different
+// columns.
+struct FewGradShared {
+    float h[32][32];
+    uint64_t mask[4];
+    int32_t list[kFewTokens];
+};
+__host__ __device__ __forceinline__ int few_grad_waves(int r) { return r >= 32 ? 4 : r >= 16 ? 2 : 1; }   // waves with different ranks
+__device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared& S) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    const int of = g.n * g.rank_tiles * g.col_tiles[0], which = id < of ? 0 : 1;
+    if (which) id -= of;
+    const int cb = id % g.col_tiles[which], rest = id / g.col_tiles[which], a = rest % g.n, rb = rest / g.n;
+    const int rw = few_grad_waves(g.r), ranks = 8 * rw, W = g.W[which];
+    Members mb;
+    mb.find(g.T, g.n, p.ids, a, S.mask);
+    list_members(mb, 0, kFewTokens, S.list);
+    const int count = mb.count();
+    const int j0 = rb * ranks, j8 = 8 * (w % rw), c = (cb * (4 / rw) + w / rw) * 512 + 8 * lane;
+    const float s = count == 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
+    const bool works = c < W && j0 + j8 < g.r;
+    float acc[8][8] = {};
+    for (int t0 = 0; t0 < count; t0 += 32) {
+        const int some = min(32, count - t0);
+        __syncthreads();
+        for (int i = tid; i < some * ranks; i += 256) {
+            const int k = i / ranks, j = i - k * ranks, tok = S.list[t0 + k];
+            if (j0 + j < g.r) S.h[k][j] = g.h[which] ? g.h[which][(size_t)tok * g.r + j0 + j] : whole_h(p, tok, j0 + j, s);
+        }
+        __syncthreads();
+        if (works) {
+#pragma unroll 2
+            for (int k = 0; k < some; ++k) {
+                const u32x4_t b = *(const u32x4_t*)(g.x[which] + (size_t)S.list[t0 + k] * g.ldx[which] + (size_t)c * 2);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) fma8(acc[j], S.h[k][j8 + j], b);
+            }
+        }
+    }
+    if (!works) return;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        f32x4_t* to = (f32x4_t*)(g.out[which] + ((size_t)a * g.r + j0 + j8 + j) * W + c);
+        to[0] = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+        to[1] = f32x4_t{acc[j][4], acc[j][5], acc[j][6], acc[j][7]};
+    }
+}
+
+__global__ void __launch_bounds__(256) adapter_few_second_kernel(ProjParams p) {
+    __shared__ JoinShared S;
+    join_task(p, blockIdx.x % p.T, blockIdx.x / p.T, S);
+}
+__global__ void __launch_bounds__(256) adapter_few_second_grad_kernel(ProjParams p, GradParams g, int joins) {
+    union Shared {
+        JoinShared join;
+        FewGradShared grad;
+    };
+    __shared__ Shared S;
+    const int id = blockIdx.x;
+    if (id < joins) join_task(p, id % p.T, id / p.T, S.join);
+    else few_grad_task(p, g, id - joins, S.grad);
+}
+
+// ------------------------------------------------------------------ more tokens
+// The low-rank rows of tile i (tile_rows rows from tile_rows i on): segments first .. first + count - 1 of the plan.  The tiles before
+// it have at most first + i segments together (each may share one with the next), which bounds where it begins.
+struct TileLow {
+    int first, count, used, ld;   // used, ld: columns; ld a multiple of BK
+    size_t at;                    // first element in hx
+};
+__device__ __forceinline__ TileLow tile_low(const ProjParams& p, int tile) {
+    const int u0 = tile * (p.tile_rows / kUnit), u1 = min((tile + 1) * p.tile_rows, p.T) - 1;
+    const int f = p.plan.unit[2 * u0], l = p.plan.unit[2 * (u1 / kUnit) + 1];
+    TileLow t;
+    t.first = max(f, 0);
+    t.count = l < 0 ? 0 : l - t.first + 1;
+    t.used = t.count * 2 * p.r;
+    t.ld = (t.used + BK - 1) / BK * BK;
+    t.at = (size_t)p.tile_rows * ((size_t)tile * (2 * p.r + BK) + (size_t)t.first * 2 * p.r);
+    return t;
+}
+static size_t hx_bytes(const moe_adapter_shape_t& s, int tile_rows) {
+    const size_t tiles = ((size_t)s.T + tile_rows - 1) / tile_rows, segs = (size_t)(s.adapters < s.T ? s.adapters : s.T);
+    return 2 * (size_t)tile_rows * (tiles * (2 * (size_t)s.rank + BK) + segs * 2 * (size_t)s.rank);
+}
+
+// h of one block of the plan, as fp32 and as the rows of its tile's low-rank part; behind the blocks, where the factors are wanted
+// transposed, 64 columns of one adapter's a workgroup.
+template <int NCF>
+__global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p) {
+    using S = SmallTile<1, NCF>;
+    __shared__ __attribute__((aligned(512))) char smem[S::kLds];
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= p.blocks) {
+        const int id = blockIdx.x - p.blocks, tiles = (p.C + 63) / 64, a = id / tiles, c0 = id % tiles * 64;
+        if (p.plan.start[a] == p.plan.start[a + 1]) return;
+        // (a rank's 64 columns as 128 bytes; 2 bytes a lane on both sides of the turn are 4 MB at 64 ranks of 4096 columns and 8 adapters)
+        uint16_t(*s)[66] = (uint16_t(*)[66])smem;   // [r][64]
+        const uint16_t* from = (const uint16_t*)p.second + (size_t)a * p.r * p.C + c0;
+        for (int i = tid; i < p.r * 64; i += kSmallThreads)
+            if (c0 + (i & 63) < p.C) s[i >> 6][i & 63] = from[(size_t)(i >> 6) * p.C + (i & 63)];
+        __syncthreads();
+        uint16_t* to = (uint16_t*)p.second_t + ((size_t)a * p.C + c0) * p.r;
+        for (int i = tid; i < p.r * 64; i += kSmallThreads) {
+            const int c = i / p.r, j = i - c * p.r;
+            if (c0 + c < p.C) to[i] = s[j][c];
+        }
+        return;
+    }
+    if ((int)blockIdx.x >= p.plan.head[0]) return;
+    const int row0 = p.plan.block[2 * blockIdx.x], code = p.plan.block[2 * blockIdx.x + 1], rows = code & 255, a = (code >> 8) - 1;
+    const int tile = row0 / p.tile_rows;
+    const TileLow tl = tile_low(p, tile);
+    uint16_t* const hx = (uint16_t*)p.hx + tl.at + (size_t)(row0 - tile * p.tile_rows) * tl.ld;
+    const int own = a < 0 ? -1 : (p.plan.ordinal[a] - tl.first) * 2 * p.r;   // first column of its segment
+    for (int i = tid; i < rows * (tl.ld / 8); i += kSmallThreads) {
+        const int row = i / (tl.ld / 8), col = 8 * (i - row * (tl.ld / 8));
+        if (a < 0 || col < own || col >= own + 2 * p.r) *(u32x4_t*)(hx + (size_t)row * tl.ld + col) = zero4();
+    }
+    if (a < 0) {
+        for (int i = tid; i < rows * p.r; i += kSmallThreads) p.h[(size_t)p.plan.order[row0 + i / p.r] * p.r + i % p.r] = 0.f;
+        return;
+    }
+    const Stages st = stages_of(p.R);
+    f32x16_t acc[1][NCF];
+    {
+        const Lane ln;
+        KcStages<1, false> lb;
+        lb.init(ln, rows, st, [&](int r) { return p.x + (size_t)p.plan.order[row0 + r] * p.ldx; });
+        lb.low.used = 0;
+        KcStages<NCF, true> la;
+        la.init(ln, p.r, st, [&](int j) { return p.first + ((size_t)a * p.r + j) * p.R * 2; });
+        small_loop<1, NCF, kKc>(lb, la, st.full + (st.tail > 0), smem, acc);
+    }
+    const float s = p.scale ? p.scale[a] : 1.f;
+    small_sum<1, NCF>(smem, acc, [&](int row, int col, const float (&v)[8]) {
+        if (row >= rows || col >= p.r) return;
+        float h[8], hi[8], lo[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            h[j] = v[j] * s;
+            hi[j] = bf16_round(h[j]);
+            lo[j] = fabsf(hi[j]) < INFINITY ? h[j] - hi[j] : 0.f;   // an infinite h stays one
+        }
+        f32x4_t* to = (f32x4_t*)(p.h + (size_t)p.plan.order[row0 + row] * p.r + col);
+        to[0] = f32x4_t{h[0], h[1], h[2], h[3]};
+        to[1] = f32x4_t{h[4], h[5], h[6], h[7]};
+        uint16_t* x = hx + (size_t)row * tl.ld + own + col;
+        *(u32x4_t*)x = pack8f(hi);
+        *(u32x4_t*)(x + p.r) = pack8f(lo);
+    });
+}
+
+// sum_j h[j] second[a][j][col ..]: the low-rank part of 8 columns of one row, for tiles in which something is not finite
+__device__ __forceinline__ void add_low(const ProjParams& p, int row, int col, float (&v)[8]) {
+    const int t = p.plan.order[row], a = adapter_of(p.ids, t, p.n);
+    if (a < 0) return;
+    for (int j = 0; j < p.r; ++j) fma8(v, p.h[(size_t)t * p.r + j], *(const u32x4_t*)(p.second + (((size_t)a * p.r + j) * p.C + col) * 2));
+}
+__device__ __forceinline__ void store_y(const ProjParams& p, int row, int col, const float (&v)[8]) {
+    const size_t at = (size_t)p.plan.order[row] * p.C + col;
+    if (p.out_f32) {
+        f32x4_t* to = (f32x4_t*)(p.y + at * 4);
+        to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+        to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+    } else {
+        *(u32x4_t*)(p.y + at * 2) = pack8f(v);
+    }
+}
+__device__ __forceinline__ bool all_finite(const f32x16_t& a) {
+    // (a sum of 0 v: 0 where every v is finite, else NaN)
+    float s = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s += 0.f * a[v];
+    return s == 0.f;
+}
+__device__ __forceinline__ LowRank low_of(const ProjParams& p, const TileLow& t, bool transposed) {
+    return LowRank{p.hx + t.at * 2, (uint32_t)t.ld * 2, transposed ? p.second_t : p.second, p.plan.seg + t.first, t.used, p.r, p.C};
+}
+
+// Tiles of 64 x 64.
+// A factor with an infinity or NaN must not reach the rows of other adapters, but 0 times it would: a tile whose sums are not all finite
+// is computed again without its low-rank part, which is then added row by row (as is one where x or W is not finite).
+template <int FORM>
+__global__ void __launch_bounds__(kSmallThreads) adapter_small_kernel(ProjParams p) {
+    __shared__ __attribute__((aligned(512))) char smem[SmallTile<2, 2>::kLds];
+    __shared__ int s_bad;
+    const int rt = blockIdx.x % p.row_tiles, ct = blockIdx.x / p.row_tiles;
+    const int row0 = rt * 64, rows = min(64, p.T - row0), col0 = ct * 64;
+    const TileLow tl = tile_low(p, rt);
+    const Stages st = stages_of(p.R);
+    const int dense = st.full + (st.tail > 0);
+    if (threadIdx.x == 0) s_bad = 0;
+    f32x16_t acc[2][2];
+    for (int low = 1;; low = 0) {
+        {
+            const Lane ln;
+            KcStages<2, false> lb;
+            lb.init(ln, rows, st, [&](int r) { return p.x + (size_t)p.plan.order[row0 + r] * p.ldx; });
+            lb.low = low_of(p, tl, FORM == kKc);
+            const int nk = dense + (low ? tl.ld / BK : 0);
+            if constexpr (FORM == kKs) {
+                KsStages<2, 64> la;
+                la.init(ln, p.w, col0, p.C, st);
+                la.low = lb.low;
+                small_loop<2, 2, kKs>(lb, la, nk, smem, acc);
+            } else {
+                KcStages<2, true> la;
+                la.init(ln, min(64, p.C - col0), st, [&](int c) { return p.w + (size_t)(col0 + c) * p.R * 2; });
+                la.low = lb.low;
+                la.first = col0;
+                small_loop<2, 2, kKc>(lb, la, nk, smem, acc);
+            }
+        }
+        if (!low || tl.count == 0) break;
+        const bool ok = all_finite(acc[0][0]) && all_finite(acc[0][1]) && all_finite(acc[1][0]) && all_finite(acc[1][1]);
+        if (!ok) s_bad = 1;
+        __syncthreads();
+        if (!s_bad) break;
+    }
+    const bool bad = s_bad;
+    small_sum<2, 2>(smem, acc, [&](int row, int col, float (&v)[8]) {
+        col += col0;
+        if (row >= rows || col >= p.C) return;
+        if (bad) add_low(p, row0 + row, col, v);
+        store_y(p, row0 + row, col, v);
+    });
+}
+
+// Tiles of 256 columns and up to 256 rows (mma.hpp's loops).
+template <int FORM, class LA>
+__device__ __forceinline__ void big_gemm(const ProjParams& p, LA& la, const Lane& ln, int row0, int rows, Stages st, const LowRank& low, int nk, char* smem,
+                                         Acc& acc) {
+    FragAddr fa;
+    frag_addresses<FORM, false>(fa, lds_addr(smem), ln);
+    auto row_of = [&](int r) { return p.x + (size_t)p.plan.order[row0 + r] * p.ldx; };
+    zero_acc(acc, false);
+    const int ntf = active_row_frags(rows);
+    if (rows <= kLowRows) {
+        KcStages<2, false> lb;
+        lb.init(ln, rows, st, row_of);
+        lb.low = low;
+        if (ntf > 2) mma_low<4, FORM>(lb, la, nk, smem, fa, acc);
+        else if (ntf > 0) mma_low<2, FORM>(lb, la, nk, smem, fa, acc);
+        else mma_low<0, FORM>(lb, la, nk, smem, fa, acc);
+    } else {
+        KcStages<4, false> lb;
+        lb.init(ln, rows, st, row_of);
+        lb.low = low;
+        if (ntf > 2) mma_loop<4, 0, FORM, false>(lb, la, nk, smem, fa, acc);
+        else mma_loop<2, 0, FORM, false>(lb, la, nk, smem, fa, acc);
+    }
+}
+template <int FORM>
+__global__ void __launch_bounds__(kMmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) adapter_big_kernel(ProjParams p) {
+    __shared__ __attribute__((aligned(512))) char smem[kMmaSmem];
+    __shared__ int s_bad;
+    const int rt = blockIdx.x % p.row_tiles, ct = blockIdx.x / p.row_tiles;
+    const int row0 = rt * p.tile_rows, rows = min(p.tile_rows, p.T - row0), col0 = ct * BN;
+    const TileLow tl = tile_low(p, rt);
+    const Stages st = stages_of(p.R);
+    const int dense = st.full + (st.tail > 0);
+    if (threadIdx.x == 0) s_bad = 0;
+    Acc acc;
+    for (int low = 1;; low = 0) {
+        const Lane ln;
+        const LowRank lr = low_of(p, tl, FORM == kKc);
+        const int nk = dense + (low ? tl.ld / BK : 0);
+        if constexpr (FORM == kKs) {
+            KsStages<4, 256> la;
+            la.init(ln, p.w, col0, p.C, st);
+            la.low = lr;
+            big_gemm<kKs>(p, la, ln, row0, rows, st, lr, nk, smem, acc);
+        } else {
+            KcStages<4, true> la;
+            la.init(ln, min(BN, p.C - col0), st, [&](int c) { return p.w + (size_t)(col0 + c) * p.R * 2; });
+            la.low = lr;
+            la.first = col0;
+            big_gemm<kKc>(p, la, ln, row0, rows, st, lr, nk, smem, acc);
+        }
+        if (!low || tl.count == 0) break;
+        bool ok = true;
+#pragma unroll
+        for (int tf = 0; tf < 4; ++tf) ok = ok && all_finite(acc.a[tf][0]) && all_finite(acc.a[tf][1]);
+        if (!ok) s_bad = 1;
+        __syncthreads();
+        if (!s_bad) break;
+    }
+    if (!s_bad && !p.out_f32) {
+        store_subtile_bf16<false>(acc, smem, rows, p.C - col0, [&](int row, int col, u32x4_t v) {
+            *(u32x4_t*)(p.y + ((size_t)p.plan.order[row0 + row] * p.C + col0 + col) * 2) = v;
+        });
+        return;
+    }
+    const Lane ln;
+    const bool bad = s_bad;
+#pragma unroll
+    for (int tf = 0; tf < 4; ++tf)
+#pragma unroll
+        for (int af = 0; af < 2; ++af)
+#pragma unroll
+            for (int vg = 0; vg < 2; ++vg) {
+                const int row = acc_row(ln, tf), col = col0 + acc_col8(ln, af, vg);
+                float v[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) v[j] = acc.a[tf][af][8 * vg + j];
+                if (row < rows && col < p.C) {
+                    if (bad) add_low(p, row0 + row, col, v);
+                    store_y(p, row0 + row, col, v);
+                }
+            }
+}
+
+// ------------------------------------------------------------------ gradients of the factors, more tokens
+// out[a][j][c] = sum over the adapter's rows of h[row][j] x[row][c]: h as three bf16 terms (the whole 24 bits of the fp32 value: these sums are
+// returned in fp32), x as it is.  A stage is 64 rows, gathered through the plan into registers and from there into LDS; wave w takes
+// its k-sub-step w for the whole tile of 32 NRF ranks by 32 NCF columns, as in small_loop.
+template <int NRF, int NCF>
+struct GradTile {
+    static constexpr int kXRow = 64 * NCF, kHRow = 64 * NRF;
+    static constexpr int kX = BK * kXRow, kH = BK * kHRow, kStage = kX + 3 * kH;
+    static constexpr int kSums = 16384 * NCF;   // one fragment of ranks at a time
+    static constexpr int kLds = 2 * kStage > kSums ? 2 * kStage : kSums;
+    static constexpr int kXLoads = kX / (16 * kSmallThreads);
+    static constexpr int kHUnits = NRF;         // 8 values each, of a thread, at most
+};
+// swizzle of a KS image with rows of `bytes`
+template <int BYTES>
+__device__ __forceinline__ int ks_swz(int k) { return BYTES == 64 ? 0 : BYTES == 128 ? (k & 2) << 1 : (k & 3) << 2; }
+
+template <int NRF, int NCF>
+__global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams p, GradParams g) {
+    using G = GradTile<NRF, NCF>;
+    __shared__ __attribute__((aligned(512))) char smem[G::kLds];
+    const int tid = threadIdx.x;
+    int id = blockIdx.x;
+    const int of = g.n * g.col_tiles[0], which = id < of ? 0 : 1;
+    if (which) id -= of;
+    const int ct = id % g.col_tiles[which], a = id / g.col_tiles[which];
+    const int W = g.W[which], c0 = ct * 32 * NCF, r = g.r;
+    const int row0 = p.plan.start[a], count = p.plan.start[a + 1] - row0;
+    const int32_t* order = p.plan.order + row0;
+    const int nst = (count + BK - 1) / BK;
+    const char* x = g.x[which];
+    const size_t ldx = g.ldx[which];
+    const float* h = g.h[which];
+    constexpr int kLanes = 4 * NCF;              // lanes of an x row
+    const int xk = tid / kLanes, xc = tid % kLanes, xcol = min(c0 + 8 * xc, W - 8);
+    constexpr int kStep = kSmallThreads / kLanes;
+    const int hw = r / 8;                        // units of a row of h
+    u32x4_t rx[G::kXLoads];
+    f32x4_t rh[G::kHUnits][2];
+    // rows at and past `count` are zeros on both sides
+    auto load = [&](int s) {
+#pragma unroll
+        for (int i = 0; i < G::kXLoads; ++i) {
+            const int k = s * BK + xk + i * kStep;
+            const int t = order[min(k, count - 1)];
+            rx[i] = *(const u32x4_t*)(x + (size_t)t * ldx + (size_t)xcol * 2);
+            if (k >= count) rx[i] = zero4();
+        }
+#pragma unroll
+        for (int i = 0; i < G::kHUnits; ++i) {
+            const int u = tid + i * kSmallThreads, k = u / hw, j = u - k * hw;
+            if (k < BK) {
+                const int row = s * BK + k, t = order[min(row, count - 1)];
+                const f32x4_t* q = (const f32x4_t*)(h + (size_t)t * r + 8 * j);
+                rh[i][0] = q[0];
+                rh[i][1] = q[1];
+                if (row >= count) rh[i][0] = rh[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+    };
+    auto put = [&](int image) {
+        char* base = smem + image * G::kStage;
+#pragma unroll
+        for (int i = 0; i < G::kXLoads; ++i) {
+            const int k = xk + i * kStep;
+            *(u32x4_t*)(base + k * G::kXRow + ((xc ^ ks_swz<G::kXRow>(k)) << 4)) = rx[i];
+        }
+#pragma unroll
+        for (int i = 0; i < G::kHUnits; ++i) {
+            const int u = tid + i * kSmallThreads, k = u / hw, j = u - k * hw;
+            if (k < BK) {
+                float v[8], e[8];
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    v[q] = rh[i][0][q];
+                    v[4 + q] = rh[i][1][q];
+                }
+                char* at = base + G::kX + k * G::kHRow + ((j ^ ks_swz<G::kHRow>(k)) << 4);
+#pragma unroll
+                for (int term = 0; term < 3; ++term) {
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) e[q] = bf16_round(v[q]);
+                    *(u32x4_t*)(at + term * G::kH) = pack8f(e);
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) v[q] = fabsf(e[q]) < INFINITY ? v[q] - e[q] : 0.f;
+                }
+            }
+        }
+    };
+    f32x16_t acc[NRF][NCF];
+#pragma unroll
+    for (int tf = 0; tf < NRF; ++tf)
+#pragma unroll
+        for (int af = 0; af < NCF; ++af)
+#pragma unroll
+            for (int v = 0; v < 16; ++v) acc[tf][af][v] = 0.f;
+    const Lane ln;
+    const int gg = (ln.l >> 4) & 1, e = (ln.l & 15) >> 2, q = ln.l & 3, sq = ((q & 1) << 1) | (q >> 1), krow = 16 * ln.w + 8 * ln.hf + e;
+    if (nst > 0) load(0);
+    for (int s = 0; s < nst; ++s) {
+        put(s & 1);
+        if (s + 1 < nst) load(s + 1);
+        __syncthreads();
+        const lds_ptr3_t base = (lds_ptr3_t)smem + (s & 1) * G::kStage;
+        auto read = [&](lds_ptr3_t at, int row_bytes) {
+            const bf16x4v_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_tr3_t)at);
+            const bf16x4v_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_tr3_t)(at + 4 * row_bytes));
+            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        };
+        bf16x8_t fx[NCF];
+#pragma unroll
+        for (int af = 0; af < NCF; ++af)
+            fx[af] = read(base + krow * G::kXRow + (((4 * af + 2 * gg + (sq >> 1)) ^ ks_swz<G::kXRow>(e)) << 4) + (sq & 1) * 8, G::kXRow);
+#pragma unroll
+        for (int term = 0; term < 3; ++term)
+#pragma unroll
+            for (int tf = 0; tf < NRF; ++tf) {
+                const bf16x8_t fh = read(base + G::kX + term * G::kH + krow * G::kHRow + (((4 * tf + 2 * gg + (q >> 1)) ^ ks_swz<G::kHRow>(e)) << 4) + (q & 1) * 8,
+                                         G::kHRow);
+#pragma unroll
+                for (int af = 0; af < NCF; ++af) acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[af], fh, acc[tf][af], 0, 0, 0);
+            }
+    }
+#pragma unroll
+    for (int tf = 0; tf < NRF; ++tf) {
+        __syncthreads();
+        f32x16_t one[1][NCF];
+#pragma unroll
+        for (int af = 0; af < NCF; ++af) one[0][af] = acc[tf][af];
+        small_sum<1, NCF>(smem, one, [&](int row, int col, const float (&v)[8]) {
+            row += 32 * tf;
+            col += c0;
+            if (row >= r || col >= W) return;
+            f32x4_t* to = (f32x4_t*)(g.out[which] + ((size_t)a * r + row) * W + col);
+            to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+            to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+        });
+    }
+}
+
+// ------------------------------------------------------------------ launches
+static int stages_in(int R) { return (R + BK - 1) / BK; }
+struct FewPlan {
+    int row_frags, col_tiles, row_tiles, rank_tiles, splits, per_split, hsplits, hper_split;
+};
+// Parts of at least 4 stages, as many as give the chip two workgroups a CU.
+static FewPlan few_plan(int T, int R, int C, int r) {
+    FewPlan f;
+    f.row_frags = T <= 32 ? 1 : 2;
+    f.col_tiles = (C + 63) / 64;
+    f.row_tiles = (T + 32 * f.row_frags - 1) / (32 * f.row_frags);
+    f.rank_tiles = (r + 63) / 64;
+    const int nst = stages_in(R), tiles = f.col_tiles * f.row_tiles;
+    const int want = tiles >= 512 ? 1 : 512 / tiles;
+    f.per_split = (nst + want - 1) / want;
+    if (f.per_split < 4) f.per_split = 4;
+    f.splits = (nst + f.per_split - 1) / f.per_split;
+    f.hper_split = 8;
+    f.hsplits = (nst + f.hper_split - 1) / f.hper_split;
+    return f;
+}
+static size_t few_bytes(int T, int R, int C, int r) {
+    const FewPlan f = few_plan(T, R, C, r);
+    return align_up((size_t)f.splits * T * C * 4, 256) + align_up((size_t)f.hsplits * T * r * 4, 256);
+}
+// Rows of a tile, 256 columns wide, or 64 for tiles of 64 x 64.
+static int tile_rows_of(int T, int C) {
+    auto tiles = [&](int rows, int cols) { return ((long long)T + rows - 1) / rows * ((C + cols - 1) / cols); };
+    if (tiles(256, 256) >= 192) return 256;
+    if (tiles(128, 256) >= 128) return 128;
+    return 64;
+}
+static size_t many_bytes(const moe_adapter_shape_t& s) {
+    const size_t hx = std::max(hx_bytes(s, tile_rows_of(s.T, s.N)), hx_bytes(s, tile_rows_of(s.T, s.K)));
+    return align_up(hx, 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256);
+}
+size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
+    if (s.T == 0) return 256;
+    if (!adapter_few(s)) return many_bytes(s);
+    return std::max(few_bytes(s.T, s.K, s.N, s.rank), few_bytes(s.T, s.N, s.K, s.rank));
+}
+
+static void few_params(ProjParams& p, char* ws, FewPlan& f) {
+    f = few_plan(p.T, p.R, p.C, p.r);
+    p.part = (float*)ws;
+    p.hpart = (float*)(ws + align_up((size_t)f.splits * p.T * p.C * 4, 256));
+    p.splits = f.splits, p.per_split = f.per_split, p.hsplits = f.hsplits, p.hper_split = f.hper_split;
+    p.col_tiles = f.col_tiles, p.row_tiles = f.row_tiles, p.rank_tiles = f.rank_tiles;
+}
+template <int FORM>
+static void few_first(const ProjParams& p, const FewPlan& f, hipStream_t st) {
+    const dim3 grid((unsigned)(f.col_tiles * f.splits * f.row_tiles + p.T * f.rank_tiles * f.hsplits));
+    if (f.row_frags == 1) hipLaunchKernelGGL((adapter_few_first_kernel<1, FORM>), grid, dim3(kSmallThreads), 0, st, p);
+    else hipLaunchKernelGGL((adapter_few_first_kernel<2, FORM>), grid, dim3(kSmallThreads), 0, st, p);
+}
+static int few_joins(const ProjParams& p) { return p.T * ((p.C + kJoinCols - 1) / kJoinCols); }
+
+template <int FORM>
+static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
+    p.plan = plan_view(s, plan);
+    p.tile_rows = tile_rows_of(p.T, p.C);
+    p.blocks = (int)plan_blocks(s);
+    const size_t hx = std::max(hx_bytes(s, tile_rows_of(s.T, s.N)), hx_bytes(s, tile_rows_of(s.T, s.K)));
+    p.hx = ws;
+    char* rest = ws + align_up(hx, 256);
+    if (!p.h) p.h = (float*)rest;
+    p.second_t = rest + align_up((size_t)s.T * s.rank * 4, 256);
+    const dim3 low((unsigned)(p.blocks + (FORM == kKc ? p.n * ((p.C + 63) / 64) : 0)));
+    if (p.r <= 32) hipLaunchKernelGGL((adapter_low_kernel<1>), low, dim3(kSmallThreads), 0, st, p);
+    else if (p.r <= 64) hipLaunchKernelGGL((adapter_low_kernel<2>), low, dim3(kSmallThreads), 0, st, p);
+    else hipLaunchKernelGGL((adapter_low_kernel<4>), low, dim3(kSmallThreads), 0, st, p);
+    const int cols = p.tile_rows == 64 ? 64 : BN;
+    p.row_tiles = (p.T + p.tile_rows - 1) / p.tile_rows;
+    p.col_tiles = (p.C + cols - 1) / cols;
+    const dim3 grid((unsigned)(p.row_tiles * p.col_tiles));
+    if (p.tile_rows == 64) hipLaunchKernelGGL((adapter_small_kernel<FORM>), grid, dim3(kSmallThreads), 0, st, p);
+    else hipLaunchKernelGGL((adapter_big_kernel<FORM>), grid, dim3(kMmaThreads), 0, st, p);
+}
+
+int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t ldx, const void* w, const void* a, const void* b, const float* scale,
+                           const int32_t* ids, void* plan, void* y, int out_f32, float* h, char* ws, hipStream_t st) {
+    if (s.T == 0) return MOE_OK;
+    ProjParams p = {};
+    p.T = s.T, p.R = s.K, p.C = s.N, p.r = s.rank, p.n = s.adapters;
+    p.x = (const char*)x, p.ldx = ldx * 2, p.w = (const char*)w, p.first = (const char*)a, p.second = (const char*)b;
+    p.scale = scale, p.ids = ids, p.y = (char*)y, p.out_f32 = out_f32, p.h = h;
+    if (adapter_few(s)) {
+        FewPlan f;
+        few_params(p, ws, f);
+        few_first<kKs>(p, f, st);
+        hipLaunchKernelGGL(adapter_few_second_kernel, dim3((unsigned)few_joins(p)), dim3(256), 0, st, p);
+    } else {
+        many_launch<kKs>(p, s, plan, ws, st);
+    }
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t lddy, const void* x, size_t ldx, const void* w, const void* a, const void* b,
+                            const float* scale, const int32_t* ids, void* plan, const float* h, void* dx, float* da, float* db, char* ws, hipStream_t st) {
+    ProjParams p = {};
+    p.T = s.T, p.R = s.N, p.C = s.K, p.r = s.rank, p.n = s.adapters;
+    p.x = (const char*)dy, p.ldx = lddy * 2, p.w = (const char*)w, p.first = (const char*)b, p.second = (const char*)a;
+    p.scale = scale, p.ids = ids, p.y = (char*)dx;
+    GradParams g = {};
+    g.T = s.T, g.r = s.rank, g.n = s.adapters, g.few = adapter_few(s);
+    g.W[0] = s.N, g.W[1] = s.K;
+    g.x[0] = (const char*)dy, g.x[1] = (const char*)x;
+    g.ldx[0] = lddy * 2, g.ldx[1] = ldx * 2;
+    g.h[0] = h;
+    g.out[0] = db, g.out[1] = da;
+    if (g.few) {
+        FewPlan f;
+        if (s.T > 0) {
+            few_params(p, ws, f);
+            few_first<kKc>(p, f, st);
+        }
+        const int cols = 512 * (4 / few_grad_waves(g.r)), joins = s.T > 0 ? few_joins(p) : 0;
+        g.rank_tiles = (g.r + 8 * few_grad_waves(g.r) - 1) / (8 * few_grad_waves(g.r));
+        for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
+        hipLaunchKernelGGL(adapter_few_second_grad_kernel, dim3((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st,
+                           p, g, joins);
+    } else {
+        many_launch<kKc>(p, s, plan, ws, st);
+        g.h[1] = p.h;
+        const int cols = p.r > 64 ? 64 : 128;
+        for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
+        const dim3 grid((unsigned)(g.n * (g.col_tiles[0] + g.col_tiles[1])));
+        if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kSmallThreads), 0, st, p, g);
+        else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kSmallThreads), 0, st, p, g);
+        else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kSmallThreads), 0, st, p, g);
+    }
+    return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
+}
+
+}  // namespace uniep

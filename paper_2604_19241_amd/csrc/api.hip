@@ -25,6 +25,23 @@ int bwd_launch(const moe_shape_t& s, const void* dy, const void* x, const void* 
                const void* w_up, const void* w_down, const moe_routing_t& r, const char* gu,
                const char* h, const char* o, void* dx, void* dw_gate, void* dw_up, void* dw_down,
                float* dtopk_w, char* ws, const moe_opts_t& opts, hipStream_t st);
+size_t adapter_plan_bytes(const moe_adapter_shape_t& s);
+size_t adapter_workspace_bytes(const moe_adapter_shape_t& s);
+int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st);
+int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t ldx, const void* w, const void* a,
+                           const void* b, const float* scale, const int32_t* ids, void* plan, void* y, int out_f32,
+                           float* h, char* ws, hipStream_t st);
+int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t lddy, const void* x, size_t ldx,
+                            const void* w, const void* a, const void* b, const float* scale, const int32_t* ids,
+                            void* plan, const float* h, void* dx, float* da, float* db, char* ws, hipStream_t st);
+size_t balance_workspace_bytes(const moe_balance_shape_t& s);
+int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, const int32_t* idx,
+                           const int32_t* offsets, const uint8_t* mask, const moe_balance_stats_t& out, char* ws,
+                           hipStream_t st);
+int balance_backward_launch(const moe_balance_shape_t& s, const float* logits, const int32_t* idx,
+                            const int32_t* offsets, const uint8_t* mask, const moe_balance_stats_t& stats,
+                            const float* w, const float* dw, const float* dloss, void* dlogits, int out_bf16,
+                            hipStream_t st);
 }  // namespace uniep
 
 using namespace uniep;
@@ -71,6 +88,45 @@ int check_opts(const moe_opts_t* o, moe_opts_t* out) {
         return MOE_ERR_ARG;
     if (d.reserved[0] != 0) return MOE_ERR_ARG;
     *out = d;
+    return MOE_OK;
+}
+
+int check_adapter_shape(const moe_adapter_shape_t* s) {
+    if (!s) return MOE_ERR_ARG;
+    if (s->T < 0 || s->T > 1 << 26 || s->adapters < 1 || s->adapters > kMaxAdapters) return MOE_ERR_SHAPE;
+    if (s->rank < 8 || s->rank > kMaxRank || s->rank % 8 != 0) return MOE_ERR_SHAPE;
+    for (int width : {s->K, s->N}) {
+        if (width < 8 || width > 1 << 17 || width % 8 != 0) return MOE_ERR_SHAPE;
+        if ((int64_t)s->T * width > (1ll << 38)) return MOE_ERR_SHAPE;
+    }
+    return MOE_OK;
+}
+int check_balance_shape(const moe_balance_shape_t* s) {
+    if (!s) return MOE_ERR_ARG;
+    if (s->T < 0 || s->E < 1 || s->E > kMaxExperts || s->k < 1 || s->k > kMaxTopK || s->k > s->E) return MOE_ERR_SHAPE;
+    if ((int64_t)s->T * s->k >= (1ll << 30) || s->seqs < 1 || s->seqs > 65536) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+// What both directions of the projection have to be given.
+int check_adapter(const moe_adapter_shape_t& s, const void* w, const void* a, const void* b, const float* scale, const int32_t* ids,
+                  const void* plan, const void* ws, size_t ws_bytes) {
+    if (!w || !a || !b || !ws) return MOE_ERR_ARG;
+    if (s.T > 0 && (!ids || (adapter_plan_bytes(s) > 0 && !plan))) return MOE_ERR_ARG;
+    if (!aligned(w, 16) || !aligned(a, 16) || !aligned(b, 16) || !aligned(scale, 4) || !aligned(ids, 4) || !aligned(plan, 16) || !aligned(ws, 256))
+        return MOE_ERR_ARG;
+    return ws_bytes < adapter_workspace_bytes(s) ? MOE_ERR_WORKSPACE : MOE_OK;
+}
+bool bad_rows(const moe_adapter_shape_t& s, const void* p, int64_t ld, int width) {
+    if (s.T == 0) return false;
+    return !p || !aligned(p, 16) || ld < width || ld % 8 != 0 || ld > (1ll << 40) / s.T;
+}
+int check_balance(const moe_balance_shape_t& s, const float* logits, const int32_t* idx, const int32_t* offsets, const moe_balance_stats_t* st) {
+    if (!st || !st->counts || !st->tokens) return MOE_ERR_ARG;
+    if (s.T > 0 && (!logits || !idx || !st->lse)) return MOE_ERR_ARG;
+    if (!offsets && s.seqs != 1) return MOE_ERR_ARG;
+    const void* ptrs[] = {logits, idx, offsets, st->counts, st->tokens, st->lse};
+    for (const void* p : ptrs)
+        if (!aligned(p, 4)) return MOE_ERR_ARG;
     return MOE_OK;
 }
 
@@ -310,6 +366,82 @@ int moe_global_map(const moe_shape_t* shape, int32_t W, int32_t rank, const moe_
         if (!aligned(q, 4)) return MOE_ERR_ARG;
     if (ws_bytes < (size_t)shape->E * 8) return MOE_ERR_WORKSPACE;
     return global_map_launch(*shape, W, rank, *routing, c_all, *out, ws, (hipStream_t)stream);
+}
+
+int moe_adapter_workspace_bytes(const moe_adapter_shape_t* shape, size_t* ws_bytes, size_t* plan_bytes) {
+    const int rc = check_adapter_shape(shape);
+    if (rc != MOE_OK) return rc;
+    if (ws_bytes) *ws_bytes = adapter_workspace_bytes(*shape);
+    if (plan_bytes) *plan_bytes = adapter_plan_bytes(*shape);
+    return MOE_OK;
+}
+
+int moe_adapter_plan(const moe_adapter_shape_t* shape, const int32_t* ids, void* plan, size_t plan_bytes, void* stream) {
+    const int rc = check_adapter_shape(shape);
+    if (rc != MOE_OK) return rc;
+    const size_t need = adapter_plan_bytes(*shape);
+    if (need == 0) return MOE_OK;
+    if (!ids || !plan || !aligned(ids, 4) || !aligned(plan, 16)) return MOE_ERR_ARG;
+    if (plan_bytes < need) return MOE_ERR_WORKSPACE;
+    return adapter_plan_launch(*shape, ids, plan, (hipStream_t)stream);
+}
+
+int moe_adapter_forward(const moe_adapter_shape_t* shape, const void* x, int64_t ldx, const void* w, const void* a, const void* b,
+                        const float* scale, const int32_t* ids, const void* plan, void* y, int32_t out_f32, float* h, void* ws,
+                        size_t ws_bytes, void* stream) {
+    int rc = check_adapter_shape(shape);
+    if (rc != MOE_OK) return rc;
+    if (bad_rows(*shape, x, ldx, shape->K) || (out_f32 != 0 && out_f32 != 1)) return MOE_ERR_ARG;
+    if ((shape->T > 0 && !y) || !aligned(y, 16) || !aligned(h, 16)) return MOE_ERR_ARG;
+    rc = check_adapter(*shape, w, a, b, scale, ids, plan, ws, ws_bytes);
+    if (rc != MOE_OK) return rc;
+    return adapter_forward_launch(*shape, x, (size_t)ldx, w, a, b, scale, ids, (void*)plan, y, out_f32, h, (char*)ws, (hipStream_t)stream);
+}
+
+int moe_adapter_backward(const moe_adapter_shape_t* shape, const void* dy, int64_t lddy, const void* x, int64_t ldx, const void* w,
+                         const void* a, const void* b, const float* scale, const int32_t* ids, const void* plan, const float* h,
+                         void* dx, float* da, float* db, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_adapter_shape(shape);
+    if (rc != MOE_OK) return rc;
+    if (bad_rows(*shape, dy, lddy, shape->N) || bad_rows(*shape, x, ldx, shape->K)) return MOE_ERR_ARG;
+    if (!da || !db || (shape->T > 0 && (!dx || !h))) return MOE_ERR_ARG;
+    if (!aligned(dx, 16) || !aligned(da, 16) || !aligned(db, 16) || !aligned(h, 16)) return MOE_ERR_ARG;
+    rc = check_adapter(*shape, w, a, b, scale, ids, plan, ws, ws_bytes);
+    if (rc != MOE_OK) return rc;
+    return adapter_backward_launch(*shape, dy, (size_t)lddy, x, (size_t)ldx, w, a, b, scale, ids, (void*)plan, h, dx, da, db, (char*)ws,
+                                   (hipStream_t)stream);
+}
+
+int moe_balance_workspace_bytes(const moe_balance_shape_t* shape, size_t* ws_bytes) {
+    const int rc = check_balance_shape(shape);
+    if (rc != MOE_OK) return rc;
+    if (ws_bytes) *ws_bytes = balance_workspace_bytes(*shape);
+    return MOE_OK;
+}
+
+int moe_balance_forward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
+                        const uint8_t* mask, const moe_balance_stats_t* out, void* ws, size_t ws_bytes, void* stream) {
+    int rc = check_balance_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_balance(*shape, logits, topk_idx, seq_offsets, out);
+    if (rc != MOE_OK) return rc;
+    if (!out->loss || !out->prob_sums || !aligned(out->loss, 4) || !aligned(out->prob_sums, 4) || !ws || !aligned(ws, 256)) return MOE_ERR_ARG;
+    if (ws_bytes < balance_workspace_bytes(*shape)) return MOE_ERR_WORKSPACE;
+    return balance_forward_launch(*shape, logits, topk_idx, seq_offsets, mask, *out, (char*)ws, (hipStream_t)stream);
+}
+
+int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
+                         const uint8_t* mask, const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w,
+                         const float* dloss, void* dlogits, int32_t out_bf16, void* stream) {
+    int rc = check_balance_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_balance(*shape, logits, topk_idx, seq_offsets, stats);
+    if (rc != MOE_OK) return rc;
+    if ((topk_w == nullptr) != (dtopk_w == nullptr) || !aligned(topk_w, 4) || !aligned(dtopk_w, 4)) return MOE_ERR_ARG;
+    if (!dloss || !aligned(dloss, 4) || (out_bf16 != 0 && out_bf16 != 1)) return MOE_ERR_ARG;
+    if ((shape->T > 0 && !dlogits) || !aligned(dlogits, out_bf16 ? 2 : 4)) return MOE_ERR_ARG;
+    return balance_backward_launch(*shape, logits, topk_idx, seq_offsets, mask, *stats, topk_w, dtopk_w, dloss, dlogits, out_bf16,
+                                   (hipStream_t)stream);
 }
 
 int moe_device_status(const void* ws, void* stream) {

@@ -17,6 +17,8 @@ typedef __attribute__((ext_vector_type(2))) uint32_t u32x2_t;
 
 constexpr int kMaxTopK = 16;
 constexpr int kMaxExperts = 1024;
+constexpr int kMaxAdapters = 1024;
+constexpr int kMaxRank = 128;                             // of an adapter
 constexpr int kWave = 64;
 constexpr int kMaxDevices = 64;                           // per-device host caches are indexed by the HIP device id
 constexpr size_t kRouteStaticScratchBytes = 4u << 20;     // file-scope scratch of moe_route_static

@@ -729,8 +729,8 @@ __device__ __forceinline__ int active_row_frags(int rows) {
 // half of the time that its requests take to arrive: with two buffers such a tile took a round trip to memory a stage
 // (training step of 256 tokens on 8 experts of 512 x 1024, 64 rows each, 135 -> 123 us; 4099 tokens on 64 experts of
 // 2048 x 1408, tiles of 256 and 128 rows, forward 510 -> 502 us; Zipf(1.2) routing of 8001 tokens 2444 -> 2419 us).
-template <int NTF, int A_FORM, class LA>
-__device__ __forceinline__ void mma_low(LowRowLoader& lb, LA& la, int nk, char* smem, const FragAddr& fa, Acc& acc) {
+template <int NTF, int A_FORM, class LB, class LA>
+__device__ __forceinline__ void mma_low(LB& lb, LA& la, int nk, char* smem, const FragAddr& fa, Acc& acc) {
     constexpr int kRequests = 6;   // of a wave, a stage
     constexpr uint32_t kA = kLowRowBytes - kRowBytes;   // fa.a is made for the larger row image
 #pragma unroll

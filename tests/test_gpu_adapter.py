@@ -1,0 +1,164 @@
+"""The shared projection with low-rank adapters, forward and backward, against the plain form in 64 bits."""
+import pytest
+import torch
+
+import adapter_cases as ac
+import paper_2604_19241_amd as moe
+from helpers import say
+
+pytestmark = pytest.mark.gpu
+
+
+def run(s, r, n, out_dtype=torch.bfloat16, backward=True, scale=True):
+    T, K = s["x"].shape
+    N = s["dy"].shape[1]
+    shape = moe.make_adapter_shape(T, K, N, r, n)
+    plan = moe.moe_adapter_plan(shape, s["ids"])
+    h = torch.full((T, r), float("nan"), device="cuda")
+    sc = s["scale"] if scale else None
+    out = {"y": moe.moe_adapter_forward(shape, s["x"], s["w"], s["a"], s["b"], plan, scale=sc, out_dtype=out_dtype, h=h), "h": h}
+    if backward:
+        out |= moe.moe_adapter_backward(shape, s["dy"], s["x"], s["w"], s["a"], s["b"], plan, h, scale=sc)
+    return out
+
+
+CASES = [  # T, K, N, rank, adapters, ids, pad, out
+    (1, 64, 64, 8, 1, "one", 0, "bf16"), (1, 2048, 512, 16, 8, "one", 0, "bf16"), (1, 8, 8, 8, 3, "none", 8, "f32"),
+    (2, 72, 24, 8, 5, "each", 0, "bf16"), (31, 200, 136, 24, 4, "packed", 8, "bf16"), (32, 520, 1032, 40, 3, "scattered", 0, "f32"),
+    (33, 1000, 88, 16, 64, "each", 64, "bf16"), (64, 4096, 40, 128, 2, "scattered", 0, "bf16"), (65, 328, 640, 72, 7, "outside", 0, "bf16"),
+    (200, 136, 2056, 8, 256, "each", 0, "bf16"), (256, 448, 264, 128, 1, "one", 0, "f32"), (256, 512, 1024, 8, 2, "packed", 0, "bf16"),
+    # more tokens: sorted by adapter
+    (257, 64, 64, 8, 1, "one", 0, "bf16"), (257, 8, 16, 8, 300, "each", 0, "f32"), (300, 328, 200, 24, 5, "outside", 8, "bf16"),
+    (511, 136, 72, 16, 256, "scattered", 0, "bf16"), (640, 1000, 520, 64, 3, "packed", 64, "f32"), (1021, 264, 712, 128, 2, "scattered", 0, "bf16"),
+    (1000, 200, 104, 40, 1024, "scattered", 0, "bf16"), (2049, 512, 128, 8, 4, "packed", 0, "f32"), (777, 72, 640, 96, 6, "none", 0, "bf16"),
+    # tiles of 128 and of 256 rows, in each direction
+    (4100, 136, 1032, 16, 9, "packed", 0, "bf16"), (4100, 1032, 72, 16, 300, "scattered", 0, "bf16"), (8200, 72, 1544, 24, 6, "scattered", 8, "bf16"),
+    (8200, 1544, 136, 64, 5, "packed", 0, "f32"), (16500, 584, 1032, 8, 40, "scattered", 0, "f32"), (16500, 1032, 584, 128, 3, "packed", 0, "bf16"),
+]
+
+
+@pytest.mark.parametrize("case", CASES, ids=lambda c: "-".join(map(str, c)))
+def test_against_the_plain_form(case):
+    T, K, N, r, n, pattern, pad, out = case
+    say(f"[adapter] {case}")
+    s = ac.make(T, K, N, r, n, pattern, pad)
+    got = run(s, r, n, torch.float32 if out == "f32" else torch.bfloat16)
+    torch.cuda.synchronize()
+    v, m = ac.plain(s)
+    e = ac.bounds(s, v, m, out == "f32")
+    for key in ("h", "y", "dx", "da", "db"):
+        ac.check(got[key], v[key], e[key], (case, key))
+
+
+def test_without_scale_and_without_the_stash():
+    for T in (40, 400):
+        s = ac.make(T, 136, 200, 16, 3, "packed")
+        got = run(s, 16, 3, scale=False)
+        v, m = ac.plain(s, scale=False)
+        e = ac.bounds(s, v, m, False)
+        for key in ("h", "y", "dx", "da", "db"):
+            ac.check(got[key], v[key], e[key], (T, key))
+        shape = moe.make_adapter_shape(T, 136, 200, 16, 3)
+        assert torch.equal(moe.moe_adapter_forward(shape, s["x"], s["w"], s["a"], s["b"], moe.moe_adapter_plan(shape, s["ids"])), got["y"])
+
+
+def test_no_tokens():
+    s = ac.make(0, 64, 128, 8, 3, "one")
+    got = run(s, 8, 3)
+    assert got["y"].shape == (0, 128) and got["dx"].shape == (0, 64)
+    assert not got["da"].any() and not got["db"].any() and got["da"].shape == (3, 8, 64)
+
+
+@pytest.mark.parametrize("T,K,N", [(48, 264, 392), (256, 64, 512), (700, 264, 392), (4200, 72, 1032), (4200, 1032, 72), (8300, 72, 1544), (8300, 1544, 72)])
+def test_an_adapter_that_is_not_finite_stays_with_its_tokens(T, K, N):
+    """Rows, and factors' gradients, of every other adapter are the same bits as with a finite one in its place."""
+    r, n = 16, 4
+    s = ac.make(T, K, N, r, n, "scattered")
+    clean = run(s, r, n)
+    for name, value in (("b", float("nan")), ("b", float("inf")), ("a", float("inf")), ("a", float("nan"))):
+        say(f"[adapter] {T} {K} {N}: {name} holds {value}")
+        bad = dict(s)
+        bad[name] = s[name].clone()
+        bad[name][2, 3, 5] = value
+        got = run(bad, r, n)
+        others = s["ids"] != 2
+        for key in ("y", "h"):
+            assert torch.isfinite(got[key][others].float()).all()
+        # (a tile that is added up again without its low-rank part rounds another fp32 sum)
+        v, m = ac.plain(s)
+        e = ac.bounds(s, v, m, False)
+        for key in ("y", "dx"):
+            ac.check(got[key][others], v[key][others], e[key][others], (T, name, value, key))
+            assert not torch.isfinite(got["y"][~others].float()).all() or not torch.isfinite(got["dx"][~others].float()).all()
+        assert torch.equal(got["h"][others], clean["h"][others])
+        for i in (0, 1, 3):
+            assert torch.equal(got["da"][i], clean["da"][i]) and torch.equal(got["db"][i], clean["db"][i])
+
+
+@pytest.mark.parametrize("T", [37, 900, 8300])
+def test_the_same_bits_every_time(T):
+    K, N, r, n = 264, 1544, 24, 5
+    s = ac.make(T, K, N, r, n, "packed")
+    one, two = run(s, r, n), run(s, r, n)
+    assert all(torch.equal(one[key], two[key]) for key in one)
+
+
+def test_gradients_are_the_differences_of_the_forward_pass():
+    """y is linear in each factor, so that a difference over any step is the slope: of sum(dy y) by single elements."""
+    for T in (20, 300):
+        K, N, r, n = 64, 72, 8, 3
+        s = ac.make(T, K, N, r, n, "packed", seed=3)
+        got = run(s, r, n, torch.float32)
+        v, m = ac.plain(s)
+        e = ac.bounds(s, v, m, True)
+
+        def loss(part):
+            return float((run(part, r, n, torch.float32, backward=False)["y"].double() * s["dy"].double()).sum())
+
+        err = float((e["y"] * s["dy"].double().abs()).sum())
+        for name, grad in (("a", "da"), ("b", "db")):
+            for at in ((0, 0, 0), (2, 7, 63), (1, 3, 17)):
+                step = 4.0
+                up, down = dict(s), dict(s)
+                up[name], down[name] = s[name].clone(), s[name].clone()
+                up[name][at] = step
+                down[name][at] = -step
+                slope = (loss(up) - loss(down)) / (2 * step)
+                # (the perturbed forward passes are off by what theirs is: a few times the unperturbed bound)
+                assert abs(slope - float(got[grad][at])) <= 8 * err / step + float(e[grad][at]), (T, name, at)
+
+
+def test_in_a_graph_and_behind_other_work_of_the_stream():
+    for T, N in ((48, 392), (700, 392), (4200, 1032)):
+        K, r, n = 264, 16, 4
+        s = ac.make(T, K, N, r, n, "scattered")
+        shape = moe.make_adapter_shape(T, K, N, r, n)
+        want = run(s, r, n)
+        torch.cuda.synchronize()
+        buf = {k: torch.zeros_like(v) for k, v in s.items()}
+        ws = torch.empty(moe.moe_adapter_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
+        h = torch.empty((T, r), device="cuda")
+
+        def step():
+            plan = moe.moe_adapter_plan(shape, buf["ids"])
+            y = moe.moe_adapter_forward(shape, buf["x"], buf["w"], buf["a"], buf["b"], plan, scale=buf["scale"], h=h, ws=ws)
+            return {"y": y} | moe.moe_adapter_backward(shape, buf["dy"], buf["x"], buf["w"], buf["a"], buf["b"], plan, h, scale=buf["scale"], ws=ws)
+
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            torch.cuda._sleep(20_000_000)
+            for k, v in s.items():
+                buf[k].copy_(v)
+            eager = step()
+        stream.synchronize()
+        assert all(torch.equal(eager[k], want[k]) for k in eager), T
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = step()
+        for turn in range(3):
+            for t in out.values():
+                t.zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(out[k], want[k]) for k in out), (T, turn)
+            assert all(torch.equal(v, want[k]) for k, v in step().items()), (T, turn)

@@ -1,0 +1,216 @@
+"""The router's balance loss and z loss with their gradient, against the formulas in 64 bits."""
+import random
+
+import pytest
+import torch
+
+import paper_2604_19241_amd as moe
+from helpers import say
+
+pytestmark = pytest.mark.gpu
+BC, ZC = 0.02, 0.003
+
+
+def make(T, E, k, S=1, masked=0.0, gates=True, seed=0, empty=False):
+    g = torch.Generator(device="cuda").manual_seed(seed + 17 * T + E)
+    rng = random.Random(seed + T)
+    logits = 2 * torch.randn((T, E), generator=g, device="cuda") + torch.randn((1, E), generator=g, device="cuda")
+    top, idx = torch.topk(logits, k, dim=1)
+    s = {"T": T, "E": E, "k": k, "S": S, "logits": logits, "idx": idx.to(torch.int32), "w": torch.softmax(top, 1)}
+    if S > 1 or empty:
+        cuts = sorted(rng.randint(0, T) for _ in range(S - 1))   # (some of them equal: empty sequences)
+        s["offsets"] = torch.tensor([0] + cuts + [T], dtype=torch.int32, device="cuda")
+    else:
+        s["offsets"] = None
+    s["mask"] = None if masked == 0.0 else torch.rand(T, generator=g, device="cuda") >= masked
+    s["dw"] = torch.randn((T, k), generator=g, device="cuda") if gates else None
+    s["u"] = torch.full((1,), 0.75, device="cuda")
+    return s
+
+
+def run(s, out_dtype=torch.float32):
+    shape = moe.make_balance_shape(s["T"], s["E"], s["k"], s["S"], BC, ZC)
+    st = moe.moe_balance_forward(shape, s["logits"], s["idx"], seq_offsets=s["offsets"], mask=s["mask"])
+    d = moe.moe_balance_backward(shape, s["logits"], s["idx"], st, s["u"], seq_offsets=s["offsets"], mask=s["mask"],
+                                 topk_w=s["w"] if s["dw"] is not None else None, dtopk_w=s["dw"], out_dtype=out_dtype)
+    return st, d
+
+
+def plain(s):
+    T, E, k, S = s["T"], s["E"], s["k"], s["S"]
+    dev = s["logits"].device
+    keep = torch.ones(T, dtype=torch.bool, device=dev) if s["mask"] is None else s["mask"]
+    z = torch.where(keep[:, None], s["logits"], torch.zeros_like(s["logits"])).double()
+    lse = torch.logsumexp(z, 1)
+    p = torch.exp(z - lse[:, None]) * keep[:, None]
+    at = [0, T] if s["offsets"] is None else s["offsets"].tolist()
+    n = int(keep.sum())
+    P, C, N, bal = [], [], [], 0.0
+    d = torch.zeros((T, E), dtype=torch.float64, device=dev)
+    u = float(s["u"])
+    for a, b in zip(at, at[1:]):
+        kept = keep[a:b]
+        slots = s["idx"][a:b][kept].long().view(-1)
+        slots = slots[(slots >= 0) & (slots < E)]
+        c = torch.bincount(slots, minlength=E)
+        m = int(kept.sum())
+        f = c.double() / (k * max(m, 1))
+        q = p[a:b]
+        P.append(q.sum(0)), C.append(c), N.append(m)
+        bal += float((f * q.sum(0)).sum())
+        d[a:b] = q * (u * BC * E / max(n, 1) * (f[None] - (q @ f)[:, None]) + u * ZC * 2 / max(n, 1) * lse[a:b, None])
+    if s["dw"] is not None:
+        w, dw = s["w"].double(), s["dw"].double()
+        ok = (s["idx"] >= 0) & (s["idx"] < E)
+        w = torch.where(ok, w, 0.0)
+        val = w * (dw - (w * dw).sum(1, keepdim=True))
+        d.scatter_add_(1, torch.where(ok, s["idx"], 0).long(), val)
+    bal *= E / max(n, 1)
+    zl = float((lse * lse * keep).sum()) / max(n, 1)
+    return {"loss": [BC * bal + ZC * zl, bal, zl], "counts": torch.stack(C), "tokens": N + [n], "prob_sums": torch.stack(P),
+            "lse": torch.where(keep, lse, -float("inf")), "dlogits": d, "p": p}
+
+
+def check(s, out_dtype=torch.float32):
+    st, d = run(s, out_dtype)
+    torch.cuda.synchronize()
+    v = plain(s)
+    # An exponential of the argument y is off by about (|y| + 4) 2^-23 of itself (the argument's rounding and the instruction's own), here |y| < 40; lse
+    # and the sums over up to 1024 experts add as much.  Sums of positive terms keep that, over tokens as well.
+    rel = 64 * 2.0 ** -23
+    assert st.counts.tolist() == v["counts"].tolist()
+    assert st.tokens.tolist() == v["tokens"]
+    fin = torch.isfinite(v["lse"])
+    assert torch.equal(torch.isfinite(st.lse), fin) and (st.lse[~fin] == -float("inf")).all()
+    assert ((st.lse.double() - v["lse"])[fin].abs() <= 8 * 2.0 ** -23 * (v["lse"][fin].abs() + 2)).all()
+    assert ((st.prob_sums.double() - v["prob_sums"]).abs() <= rel * v["prob_sums"] + 1e-30).all()
+    for got, want in zip(st.loss.tolist(), v["loss"]):
+        assert abs(got - want) <= rel * (v["loss"][1] + v["loss"][2]) + 1e-30, (got, want)
+    scale = v["p"] * (0.75 * BC * s["E"] * 2 + 0.75 * ZC * 2 * 64) / max(v["tokens"][-1], 1)   # |f| <= 1, |lse| < 64
+    err = rel * scale + 16 * 2.0 ** -23 * (v["dlogits"].abs() + (s["dw"].abs().sum(1, keepdim=True).double() if s["dw"] is not None else 0.0))
+    if out_dtype == torch.bfloat16:
+        err = err + 2.0 ** -8 * v["dlogits"].abs()
+    assert ((d.double() - v["dlogits"]).abs() <= err + 1e-30).all()
+    return st, d
+
+
+@pytest.mark.parametrize("E,k", [(1, 1), (2, 1), (5, 3), (8, 2), (9, 2), (20, 4), (32, 16), (64, 6), (65, 6), (128, 8), (129, 1), (160, 6),
+                                 (256, 8), (257, 10), (384, 16), (512, 8), (1000, 8), (1024, 16)])
+@pytest.mark.parametrize("T", [1, 63, 1000])
+def test_every_number_of_experts(T, E, k):
+    say(f"[balance] {T} {E} {k}")
+    check(make(T, E, k))
+    check(make(T, E, k, S=3, masked=0.3, gates=k % 2 == 0, seed=1), torch.bfloat16 if E % 3 else torch.float32)
+
+
+@pytest.mark.parametrize("T,E,k,S,masked", [(64, 8, 2, 64, 0.0), (300, 129, 4, 400, 0.2), (5000, 64, 8, 7, 0.5), (70000, 20, 4, 300, 0.1),
+                                            (140000, 8, 2, 1, 0.0), (40001, 256, 8, 61, 0.1), (4, 128, 8, 1, 0.0), (2, 8, 2, 1, 0.0)])
+def test_sequences_of_any_length(T, E, k, S, masked):
+    say(f"[balance] {T} {E} {k} {S} {masked}")
+    s = make(T, E, k, S, masked)
+    one, d1 = check(s)
+    two, d2 = run(s)
+    for a, b in ((one.loss, two.loss), (one.prob_sums, two.prob_sums), (d1, d2)):
+        assert torch.equal(a, b)   # the same bits every time
+
+
+def test_masked_tokens_are_not_looked_at():
+    s = make(500, 64, 4, S=5, masked=0.4)
+    at = s["offsets"].tolist()
+    s["mask"][at[1]:at[2]] = False   # a sequence of which nothing is left
+    st, d = check(s)
+    bad = dict(s, logits=s["logits"].clone())
+    rows = torch.nonzero(~s["mask"])[:, 0]
+    bad["logits"][rows[0::3]] = float("nan")
+    bad["logits"][rows[1::3]] = float("inf")
+    bad["logits"][rows[2::3]] = torch.finfo(torch.float32).min
+    st2, d2 = run(bad)
+    assert torch.equal(st.loss, st2.loss) and torch.equal(st.prob_sums, st2.prob_sums) and torch.equal(d, d2) and torch.equal(st.lse, st2.lse)
+    none = dict(s, mask=torch.zeros_like(s["mask"]))
+    st, d = check(none)
+    assert st.loss.tolist() == [0.0, 0.0, 0.0] and st.tokens.tolist() == [0] * 6
+
+
+def test_experts_that_are_switched_off():
+    s = make(200, 40, 3, S=2)
+    for value in (-float("inf"), torch.finfo(torch.float32).min):
+        off = dict(s, logits=s["logits"].clone())
+        off["logits"][:, 30:] = value
+        top, idx = torch.topk(off["logits"], 3, dim=1)
+        off["idx"], off["w"] = idx.to(torch.int32), torch.softmax(top, 1)
+        st, _ = check(off)
+        assert not st.prob_sums[:, 30:].any()
+
+
+def test_slots_without_an_expert_and_selection_of_the_router():
+    s = make(150, 24, 4, S=3)
+    s["idx"][3, 1] = s["idx"][70, 0] = 2 ** 31 - 1
+    s["idx"][149, 3] = -1
+    check(s)
+    shape = moe.make_shape(T=150, d=64, E=24, k=4, I=64)
+    r = moe.moe_route(shape, s["logits"])
+    st, d = check(dict(s, idx=r.topk_idx, w=r.topk_w, offsets=None, S=1))
+    assert torch.equal(st.counts[0], r.counts)
+    only = moe.moe_route_backward(shape, r, s["dw"])
+    zero = moe.make_balance_shape(150, 24, 4, 1, 0.0, 0.0)
+    gates = moe.moe_balance_backward(zero, s["logits"], r.topk_idx, st, s["u"], topk_w=r.topk_w, dtopk_w=s["dw"])
+    assert ((only - gates).abs() <= 16 * 2.0 ** -23 * s["dw"].abs().sum(1, keepdim=True)).all()
+
+
+def test_no_tokens():
+    s = make(0, 16, 2, S=2)
+    st, d = run(s)
+    assert st.loss.tolist() == [0.0] * 3 and st.tokens.tolist() == [0, 0, 0] and not st.counts.any() and not st.prob_sums.any() and d.shape == (0, 16)
+
+
+def test_the_gradient_is_the_slope_of_the_loss():
+    """Central differences of the formulas in 64 bits, the counts held."""
+    s = make(40, 12, 3, S=3, masked=0.2, gates=False)
+    _, d = run(s)
+    base = s["logits"].double()
+    at = s["offsets"].tolist()
+    keep = s["mask"]
+    n = max(int(keep.sum()), 1)
+    f = []
+    for a, b in zip(at, at[1:]):
+        c = torch.bincount(s["idx"][a:b][keep[a:b]].long().view(-1), minlength=12).double()
+        f.append(c / (3 * max(int(keep[a:b].sum()), 1)))
+
+    def loss(z):
+        lse = torch.logsumexp(z, 1)
+        p = torch.exp(z - lse[:, None]) * keep[:, None]
+        bal = sum(float((fi * p[a:b].sum(0)).sum()) for fi, a, b in zip(f, at, at[1:])) * 12 / n
+        return BC * bal + ZC * float((lse * lse * keep).sum()) / n
+
+    step = 1e-4   # the third derivative makes it off by 1e-8 of the loss' size, rounding by 1e-16 / 1e-4
+    for t, e in ((0, 0), (7, 11), (20, 5), (39, 3)):
+        up, down = base.clone(), base.clone()
+        up[t, e] += step
+        down[t, e] -= step
+        slope = 0.75 * (loss(up) - loss(down)) / (2 * step)
+        assert abs(slope - float(d[t, e])) <= 1e-7 + 64 * 2.0 ** -23 * abs(slope)
+
+
+def test_in_a_graph():
+    s = make(3000, 64, 8, S=9, masked=0.1)
+    want, dwant = run(s)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    buf = torch.zeros_like(s["logits"])
+    t = dict(s, logits=buf)
+    with torch.cuda.stream(stream):
+        torch.cuda._sleep(20_000_000)
+        buf.copy_(s["logits"])
+        got, d = run(t)
+    stream.synchronize()
+    assert torch.equal(got.loss, want.loss) and torch.equal(d, dwant)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        st, d = run(t)
+    for _ in range(3):
+        d.zero_(), st.loss.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(st.loss, want.loss) and torch.equal(st.counts, want.counts) and torch.equal(d, dwant)
+        again, dagain = run(t)
+        assert torch.equal(again.loss, want.loss) and torch.equal(dagain, dwant)

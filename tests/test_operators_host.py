@@ -1,0 +1,118 @@
+"""What the projection with adapters and the balance loss refuse, before anything reaches a device."""
+import ctypes
+
+import pytest
+import torch
+
+import paper_2604_19241_amd as moe
+from paper_2604_19241_amd import binding as b
+
+FAKE = 0x1000
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not b.LIB_PATH.exists():
+        from paper_2604_19241_amd import build
+        build.build()
+    return b.load_library()
+
+
+def test_struct_sizes():
+    assert ctypes.sizeof(b.MoEAdapterShape) == 20 and ctypes.sizeof(b.MoEBalanceShape) == 24 and ctypes.sizeof(b.MoEBalanceStatsC) == 40
+
+
+GOOD = dict(T=300, K=64, N=128, rank=16, adapters=4)
+
+
+def adapter_calls(lib, s, **kw):
+    """Return codes of plan, forward and backward."""
+    a = dict(ids=FAKE, plan=FAKE, pbytes=1 << 30, x=FAKE, ldx=s.K, w=FAKE, a=FAKE, b=FAKE, scale=None, y=FAKE, f32=0, h=FAKE, ws=FAKE, nbytes=1 << 40,
+             dy=FAKE, lddy=s.N, dx=FAKE, da=FAKE, db=FAKE)
+    a.update(kw)
+    r = ctypes.byref(s)
+    return {
+        "plan": lambda: lib.moe_adapter_plan(r, a["ids"], a["plan"], a["pbytes"], None),
+        "forward": lambda: lib.moe_adapter_forward(r, a["x"], a["ldx"], a["w"], a["a"], a["b"], a["scale"], a["ids"], a["plan"], a["y"], a["f32"], a["h"],
+                                                   a["ws"], a["nbytes"], None),
+        "backward": lambda: lib.moe_adapter_backward(r, a["dy"], a["lddy"], a["x"], a["ldx"], a["w"], a["a"], a["b"], a["scale"], a["ids"], a["plan"],
+                                                     a["h"], a["dx"], a["da"], a["db"], a["ws"], a["nbytes"], None)}
+
+
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(T=(1 << 26) + 1), dict(K=0), dict(K=60), dict(K=(1 << 17) + 8), dict(N=4), dict(N=129), dict(rank=0), dict(rank=12),
+                                dict(rank=136), dict(adapters=0), dict(adapters=1025), dict(T=1 << 26, K=8192)])
+def test_adapter_shapes_outside_the_limits(lib, kw):
+    s = moe.make_adapter_shape(**(GOOD | kw))
+    assert lib.moe_adapter_workspace_bytes(ctypes.byref(s), None, None) == b.MOE_ERR_SHAPE
+    for call in adapter_calls(lib, s).values():
+        assert call() == b.MOE_ERR_SHAPE
+
+
+def test_adapter_arguments(lib):
+    s = moe.make_adapter_shape(**GOOD)
+    assert lib.moe_adapter_workspace_bytes(None, None, None) == b.MOE_ERR_ARG
+    need, plan = b._adapter_bytes(s)
+    assert need > 0 and plan >= 4 * 300 and plan % 4 == 0
+    for kw in (dict(ids=None), dict(plan=None), dict(ids=0x1002), dict(plan=0x1004)):
+        for call in adapter_calls(lib, s, **kw).values():
+            assert call() == b.MOE_ERR_ARG, kw
+    assert adapter_calls(lib, s, pbytes=plan - 1)["plan"]() == b.MOE_ERR_WORKSPACE
+    both = (dict(x=None), dict(x=0x1008), dict(ldx=56), dict(ldx=68), dict(ldx=1 << 60), dict(ldx=-64), dict(w=None), dict(a=None), dict(b=None), dict(ws=None),
+            dict(w=0x1008), dict(a=0x1008), dict(b=0x1008), dict(scale=0x1002), dict(ws=0x1080), dict(h=0x1008))
+    for kw in both + (dict(y=None), dict(y=0x1008), dict(f32=2)):
+        assert adapter_calls(lib, s, **kw)["forward"]() == b.MOE_ERR_ARG, kw
+    for kw in both + (dict(dy=None), dict(lddy=120), dict(dx=None), dict(da=None), dict(db=None), dict(h=None), dict(dx=0x1008), dict(da=0x1008), dict(db=0x1008)):
+        assert adapter_calls(lib, s, **kw)["backward"]() == b.MOE_ERR_ARG, kw
+    for name in ("forward", "backward"):
+        assert adapter_calls(lib, s, nbytes=need - 1)[name]() == b.MOE_ERR_WORKSPACE
+
+
+def test_few_tokens_need_no_plan(lib):
+    s = moe.make_adapter_shape(T=256, K=64, N=128, rank=16, adapters=4)
+    assert b._adapter_bytes(s)[1] == 0
+    assert adapter_calls(lib, s, ids=None, plan=None)["plan"]() == b.MOE_OK   # nothing to do
+    assert adapter_calls(lib, s, ids=None, plan=None)["forward"]() == b.MOE_ERR_ARG
+
+
+BAL = dict(T=100, E=16, k=2, seqs=2)
+
+
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(E=0), dict(E=1025), dict(k=0), dict(k=17, E=64), dict(k=3, E=2), dict(seqs=0), dict(seqs=65537), dict(T=1 << 30)])
+def test_balance_shapes_outside_the_limits(lib, kw):
+    s = moe.make_balance_shape(**(BAL | kw))
+    assert lib.moe_balance_workspace_bytes(ctypes.byref(s), None) == b.MOE_ERR_SHAPE
+    st = b.MoEBalanceStatsC(*[FAKE] * 5)
+    assert lib.moe_balance_forward(ctypes.byref(s), FAKE, FAKE, FAKE, None, ctypes.byref(st), FAKE, 1 << 40, None) == b.MOE_ERR_SHAPE
+    assert lib.moe_balance_backward(ctypes.byref(s), FAKE, FAKE, FAKE, None, ctypes.byref(st), None, None, FAKE, FAKE, 0, None) == b.MOE_ERR_SHAPE
+
+
+def test_balance_arguments(lib):
+    s = moe.make_balance_shape(**BAL)
+    need = moe.moe_balance_workspace_bytes(s)
+
+    def both(logits=FAKE, idx=FAKE, offsets=FAKE, mask=None, stats=(FAKE,) * 5, ws=FAKE, nbytes=need, w=None, dw=None, u=FAKE, d=FAKE, bf16=0):
+        st = ctypes.byref(b.MoEBalanceStatsC(*stats)) if stats else None
+        return (lib.moe_balance_forward(ctypes.byref(s), logits, idx, offsets, mask, st, ws, nbytes, None),
+                lib.moe_balance_backward(ctypes.byref(s), logits, idx, offsets, mask, st, w, dw, u, d, bf16, None))
+
+    for kw in (dict(logits=None), dict(idx=None), dict(offsets=None), dict(stats=None), dict(stats=(FAKE, None, FAKE, FAKE, FAKE)),
+               dict(stats=(FAKE, FAKE, None, FAKE, FAKE)), dict(stats=(FAKE, FAKE, FAKE, FAKE, None)), dict(logits=0x1002), dict(idx=0x1001), dict(offsets=0x1002)):
+        assert both(**kw) == (b.MOE_ERR_ARG,) * 2, kw
+    small = ctypes.byref(s)
+    st = ctypes.byref(b.MoEBalanceStatsC(*[FAKE] * 5))
+    for ws, n, code in ((None, need, b.MOE_ERR_ARG), (0x1080, need, b.MOE_ERR_ARG), (FAKE, need - 1, b.MOE_ERR_WORKSPACE)):
+        assert lib.moe_balance_forward(small, FAKE, FAKE, FAKE, None, st, ws, n, None) == code
+    for stats in ((None, FAKE, FAKE, FAKE, FAKE), (FAKE, FAKE, FAKE, None, FAKE)):
+        st2 = ctypes.byref(b.MoEBalanceStatsC(*stats))
+        assert lib.moe_balance_forward(small, FAKE, FAKE, FAKE, None, st2, FAKE, need, None) == b.MOE_ERR_ARG
+    for w, dw, u, d, bf16 in ((FAKE, None, FAKE, FAKE, 0), (None, FAKE, FAKE, FAKE, 0), (None, None, None, FAKE, 0), (None, None, FAKE, None, 0),
+                              (None, None, FAKE, FAKE, 2), (None, None, FAKE, 0x1002, 0), (0x1001, FAKE, FAKE, FAKE, 0)):
+        assert lib.moe_balance_backward(small, FAKE, FAKE, FAKE, None, st, w, dw, u, d, bf16, None) == b.MOE_ERR_ARG
+
+
+def test_the_binding_refuses_other_tensors():
+    s = moe.make_adapter_shape(**GOOD)
+    with pytest.raises(AssertionError):
+        moe.moe_adapter_plan(s, torch.zeros(300, dtype=torch.int32))   # not on the GPU
+    with pytest.raises(AssertionError):
+        moe.moe_balance_forward(moe.make_balance_shape(4, 8, 2), torch.zeros((4, 8)), torch.zeros((4, 2), dtype=torch.int32))
