@@ -344,11 +344,11 @@ int moe_balance_forward(const moe_balance_shape_t* shape, const float* logits, c
                         const uint8_t* mask, const moe_balance_stats_t* out, void* ws, size_t ws_bytes, void* stream);
 
 /* Gradient of the logits, every element written: with u = dloss[0] (fp32, device) the gradient of `loss`, counts being constants,
- *   dlogits[t,e] = p (u balance_coef E / n (f[s,e] - sum_j f[s,j] p[t,j]) + u z_coef 2 / n lse[t])   for kept tokens, else 0,
+ *   dlogits[t,e] = p (u balance_coef E / n (f[s,e] - sum_j f[s,j] p[t,j]) + u z_coef 2 / n lse[t])   for kept tokens (lse > -inf), else 0,
  * and, where topk_w and dtopk_w [T,k] fp32 are given (both or neither), for every token what moe_route_backward computes from them.
  *   dlogits      [T,E] fp32, or bf16 with out_bf16 = 1 */
 int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
-                         const uint8_t* mask, const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w,
+                         const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w,
                          const float* dloss, void* dlogits, int32_t out_bf16, void* stream);
 
 /* Synchronises `stream`, reads the status word a forward/backward call left in

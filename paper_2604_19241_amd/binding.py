@@ -68,7 +68,7 @@ _ARGTYPES = {
     "moe_adapter_forward": [_P, _P, _L, _P, _P, _P, _P, _P, _P, _P, _I, _P, _P, _N, _P],
     "moe_adapter_backward": [_P, _P, _L, _P, _L] + [_P] * 10 + [_P, _N, _P],
     "moe_balance_forward": [_P] * 7 + [_N, _P],
-    "moe_balance_backward": [_P] * 10 + [_I, _P],
+    "moe_balance_backward": [_P] * 9 + [_I, _P],
 }
 _lib = None
 
@@ -506,11 +506,11 @@ def moe_balance_forward(shape: MoEBalanceShape, logits, topk_idx, seq_offsets=No
     return st
 
 
-def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: BalanceStats, dloss, seq_offsets=None, mask=None, topk_w=None,
+def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: BalanceStats, dloss, seq_offsets=None, topk_w=None,
                          dtopk_w=None, out_dtype=torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient [T,E] of the logits for the gradient dloss [1] of stats.loss[0]; with topk_w and dtopk_w also what
-    moe_route_backward would give, added before the one rounding.  mask and seq_offsets as in the forward call."""
-    _balance_inputs(shape, logits, topk_idx, seq_offsets, mask)
+    moe_route_backward would give, added before the one rounding.  seq_offsets as in the forward call; tokens that it did not keep have stats.lse = -inf."""
+    _balance_inputs(shape, logits, topk_idx, seq_offsets, None)
     for t in (topk_w, dtopk_w):
         if t is not None:
             assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (shape.T, shape.k)
@@ -521,7 +521,7 @@ def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: Balanc
     assert out.is_cuda and out.dtype == out_dtype and out.is_contiguous() and out.shape == (shape.T, shape.E)
     cs = stats.c_struct()
     _check(load_library().moe_balance_backward(
-        ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), _ptr(mask), ctypes.byref(cs), _ptr(topk_w), _ptr(dtopk_w),
+        ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), ctypes.byref(cs), _ptr(topk_w), _ptr(dtopk_w),
         _ptr(dloss), _ptr(out), 1 if out_dtype == torch.bfloat16 else 0, _stream(logits.device)), "moe_balance_backward")
     return out
 

@@ -39,8 +39,7 @@ int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, co
                            const int32_t* offsets, const uint8_t* mask, const moe_balance_stats_t& out, char* ws,
                            hipStream_t st);
 int balance_backward_launch(const moe_balance_shape_t& s, const float* logits, const int32_t* idx,
-                            const int32_t* offsets, const uint8_t* mask, const moe_balance_stats_t& stats,
-                            const float* w, const float* dw, const float* dloss, void* dlogits, int out_bf16,
+                            const int32_t* offsets, const moe_balance_stats_t& stats, const float* w, const float* dw, const float* dloss, void* dlogits, int out_bf16,
                             hipStream_t st);
 }  // namespace uniep
 
@@ -431,8 +430,7 @@ int moe_balance_forward(const moe_balance_shape_t* shape, const float* logits, c
 }
 
 int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
-                         const uint8_t* mask, const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w,
-                         const float* dloss, void* dlogits, int32_t out_bf16, void* stream) {
+                         const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w, const float* dloss, void* dlogits, int32_t out_bf16, void* stream) {
     int rc = check_balance_shape(shape);
     if (rc != MOE_OK) return rc;
     rc = check_balance(*shape, logits, topk_idx, seq_offsets, stats);
@@ -440,7 +438,7 @@ int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, 
     if ((topk_w == nullptr) != (dtopk_w == nullptr) || !aligned(topk_w, 4) || !aligned(dtopk_w, 4)) return MOE_ERR_ARG;
     if (!dloss || !aligned(dloss, 4) || (out_bf16 != 0 && out_bf16 != 1)) return MOE_ERR_ARG;
     if ((shape->T > 0 && !dlogits) || !aligned(dlogits, out_bf16 ? 2 : 4)) return MOE_ERR_ARG;
-    return balance_backward_launch(*shape, logits, topk_idx, seq_offsets, mask, *stats, topk_w, dtopk_w, dloss, dlogits, out_bf16,
+    return balance_backward_launch(*shape, logits, topk_idx, seq_offsets, *stats, topk_w, dtopk_w, dloss, dlogits, out_bf16,
                                    (hipStream_t)stream);
 }
 

@@ -314,7 +314,8 @@ __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams
         float d[L::kValues];
 #pragma unroll
         for (int v = 0; v < L::kValues; ++v) d[v] = 0.f;
-        if (there && (!p.mask || p.mask[t])) {
+        const float lse = there ? p.lse[t] : -INFINITY;
+        if (lse != -INFINITY) {   // (a token that is not kept)
             if (s < 0 || t >= end) {
                 s = seq_of(p, t);
                 end = seq_begin(p, s + 1);
@@ -325,7 +326,6 @@ __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams
                 for (int v = 0; v < L::kValues; ++v) f[v] = scale * (float)cnt[v];
             }
             ln.template load<f32x4_t>(p.logits + (size_t)t * E, E, -INFINITY, d);
-            const float lse = p.lse[t];
             float inner = 0.f;
 #pragma unroll
             for (int v = 0; v < L::kValues; ++v) {
@@ -471,13 +471,12 @@ int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, co
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
-int balance_backward_launch(const moe_balance_shape_t& s, const float* logits, const int32_t* idx, const int32_t* offsets, const uint8_t* mask,
-                            const moe_balance_stats_t& stats, const float* w, const float* dw, const float* dloss, void* dlogits, int out_bf16,
+int balance_backward_launch(const moe_balance_shape_t& s, const float* logits, const int32_t* idx, const int32_t* offsets, const moe_balance_stats_t& stats, const float* w, const float* dw, const float* dloss, void* dlogits, int out_bf16,
                             hipStream_t st) {
     if (s.T == 0) return MOE_OK;
     BalParams p = {};
     bal_params(p, s);
-    p.logits = logits, p.idx = idx, p.offsets = offsets, p.mask = mask;
+    p.logits = logits, p.idx = idx, p.offsets = offsets;
     p.counts = stats.counts, p.tokens = stats.tokens, p.lse = stats.lse;
     p.w = w, p.dw = dw, p.dloss = dloss, p.dlogits = dlogits, p.out_bf16 = out_bf16;
     p.chunk = 32;

@@ -31,7 +31,7 @@ def make(T, E, k, S=1, masked=0.0, gates=True, seed=0, empty=False):
 def run(s, out_dtype=torch.float32):
     shape = moe.make_balance_shape(s["T"], s["E"], s["k"], s["S"], BC, ZC)
     st = moe.moe_balance_forward(shape, s["logits"], s["idx"], seq_offsets=s["offsets"], mask=s["mask"])
-    d = moe.moe_balance_backward(shape, s["logits"], s["idx"], st, s["u"], seq_offsets=s["offsets"], mask=s["mask"],
+    d = moe.moe_balance_backward(shape, s["logits"], s["idx"], st, s["u"], seq_offsets=s["offsets"],
                                  topk_w=s["w"] if s["dw"] is not None else None, dtopk_w=s["dw"], out_dtype=out_dtype)
     return st, d
 

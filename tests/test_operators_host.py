@@ -83,7 +83,7 @@ def test_balance_shapes_outside_the_limits(lib, kw):
     assert lib.moe_balance_workspace_bytes(ctypes.byref(s), None) == b.MOE_ERR_SHAPE
     st = b.MoEBalanceStatsC(*[FAKE] * 5)
     assert lib.moe_balance_forward(ctypes.byref(s), FAKE, FAKE, FAKE, None, ctypes.byref(st), FAKE, 1 << 40, None) == b.MOE_ERR_SHAPE
-    assert lib.moe_balance_backward(ctypes.byref(s), FAKE, FAKE, FAKE, None, ctypes.byref(st), None, None, FAKE, FAKE, 0, None) == b.MOE_ERR_SHAPE
+    assert lib.moe_balance_backward(ctypes.byref(s), FAKE, FAKE, FAKE, ctypes.byref(st), None, None, FAKE, FAKE, 0, None) == b.MOE_ERR_SHAPE
 
 
 def test_balance_arguments(lib):
@@ -93,7 +93,7 @@ def test_balance_arguments(lib):
     def both(logits=FAKE, idx=FAKE, offsets=FAKE, mask=None, stats=(FAKE,) * 5, ws=FAKE, nbytes=need, w=None, dw=None, u=FAKE, d=FAKE, bf16=0):
         st = ctypes.byref(b.MoEBalanceStatsC(*stats)) if stats else None
         return (lib.moe_balance_forward(ctypes.byref(s), logits, idx, offsets, mask, st, ws, nbytes, None),
-                lib.moe_balance_backward(ctypes.byref(s), logits, idx, offsets, mask, st, w, dw, u, d, bf16, None))
+                lib.moe_balance_backward(ctypes.byref(s), logits, idx, offsets, st, w, dw, u, d, bf16, None))
 
     for kw in (dict(logits=None), dict(idx=None), dict(offsets=None), dict(stats=None), dict(stats=(FAKE, None, FAKE, FAKE, FAKE)),
                dict(stats=(FAKE, FAKE, None, FAKE, FAKE)), dict(stats=(FAKE, FAKE, FAKE, FAKE, None)), dict(logits=0x1002), dict(idx=0x1001), dict(offsets=0x1002)):
@@ -107,7 +107,7 @@ def test_balance_arguments(lib):
         assert lib.moe_balance_forward(small, FAKE, FAKE, FAKE, None, st2, FAKE, need, None) == b.MOE_ERR_ARG
     for w, dw, u, d, bf16 in ((FAKE, None, FAKE, FAKE, 0), (None, FAKE, FAKE, FAKE, 0), (None, None, None, FAKE, 0), (None, None, FAKE, None, 0),
                               (None, None, FAKE, FAKE, 2), (None, None, FAKE, 0x1002, 0), (0x1001, FAKE, FAKE, FAKE, 0)):
-        assert lib.moe_balance_backward(small, FAKE, FAKE, FAKE, None, st, w, dw, u, d, bf16, None) == b.MOE_ERR_ARG
+        assert lib.moe_balance_backward(small, FAKE, FAKE, FAKE, st, w, dw, u, d, bf16, None) == b.MOE_ERR_ARG
 
 
 def test_the_binding_refuses_other_tensors():
