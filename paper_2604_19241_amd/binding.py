@@ -394,17 +394,23 @@ def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
     return AdapterPlan(ids, table)
 
 
+_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
+
+
 def _adapter_rows(t: torch.Tensor, T: int, width: int) -> int:
     """Elements from one row of t to the next."""
-    assert t.is_cuda and t.dtype == torch.bfloat16 and t.shape == (T, width) and t.stride(1) == 1
-    return t.stride(0) if T > 1 else width
+    ld, one = t.stride()
+    assert t.is_cuda and t.dtype is _BF16 and t.shape == (T, width) and one == 1
+    return ld if T > 1 else width
 
 
 def _adapter_operands(shape: MoEAdapterShape, w, a, b, scale, plan: AdapterPlan):
     K, N, r, n = shape.K, shape.N, shape.rank, shape.adapters
-    for t, size in ((w, (K, N)), (a, (n, r, K)), (b, (n, r, N))):
-        assert t.is_cuda and t.dtype == torch.bfloat16 and t.is_contiguous() and t.shape == size
-    assert scale is None or (scale.is_cuda and scale.dtype == torch.float32 and scale.is_contiguous() and scale.shape == (n,))
+    # (written out: a generator over the operands took as long as half a launch)
+    assert w.is_cuda and w.dtype is _BF16 and w.is_contiguous() and w.shape == (K, N)
+    assert a.is_cuda and a.dtype is _BF16 and a.is_contiguous() and a.shape == (n, r, K)
+    assert b.is_cuda and b.dtype is _BF16 and b.is_contiguous() and b.shape == (n, r, N)
+    assert scale is None or (scale.is_cuda and scale.dtype is _F32 and scale.is_contiguous() and scale.shape == (n,))
     assert plan.ids.shape == (shape.T,)
 
 
@@ -415,17 +421,18 @@ def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, s
     moe_adapter_backward reads."""
     ldx = _adapter_rows(x, shape.T, shape.K)
     _adapter_operands(shape, w, a, b, scale, plan)
-    assert out_dtype in (torch.bfloat16, torch.float32)
-    if y is None:
-        y = x.new_empty((shape.T, shape.N), dtype=out_dtype)
-    assert y.is_cuda and y.dtype == out_dtype and y.is_contiguous() and y.shape == (shape.T, shape.N)
+    assert out_dtype is _BF16 or out_dtype is _F32
+    if y is None:   # (new_empty with a type takes a microsecond more)
+        y = x.new_empty((shape.T, shape.N)) if out_dtype is _BF16 else torch.empty((shape.T, shape.N), dtype=_F32, device=x.device)
+    else:
+        assert y.is_cuda and y.dtype is out_dtype and y.is_contiguous() and y.shape == (shape.T, shape.N)
     if h is not None:
-        assert h.is_cuda and h.dtype == torch.float32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
+        assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
     if ws is None:
         ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
     _check(load_library().moe_adapter_forward(
         ctypes.byref(shape), _ptr(x), ldx, _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.ids), _ptr(plan.table), _ptr(y),
-        1 if out_dtype == torch.float32 else 0, _ptr(h), _ptr(ws), ws.numel(), _stream(x.device)), "moe_adapter_forward")
+        1 if out_dtype is _F32 else 0, _ptr(h), _ptr(ws), ws.numel(), _stream(x.device)), "moe_adapter_forward")
     return y
 
 
@@ -434,12 +441,13 @@ def moe_adapter_backward(shape: MoEAdapterShape, dy, x, w, a, b, plan: AdapterPl
     """Gradients of x (bf16) and of every adapter's two factors (fp32); w is frozen.  h as moe_adapter_forward wrote it."""
     lddy, ldx = _adapter_rows(dy, shape.T, shape.N), _adapter_rows(x, shape.T, shape.K)
     _adapter_operands(shape, w, a, b, scale, plan)
-    assert h.is_cuda and h.dtype == torch.float32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
+    assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
     if out is None:
         out = {"dx": x.new_empty((shape.T, shape.K)), "da": h.new_empty(a.shape), "db": h.new_empty(b.shape)}
-    for key, dtype, size in (("dx", torch.bfloat16, x.shape), ("da", torch.float32, a.shape), ("db", torch.float32, b.shape)):
-        t = out[key]
-        assert t.is_cuda and t.dtype == dtype and t.is_contiguous() and t.shape == size
+    else:
+        for key, dtype, size in (("dx", _BF16, x.shape), ("da", _F32, a.shape), ("db", _F32, b.shape)):
+            t = out[key]
+            assert t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.shape == size
     if ws is None:
         ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
     _check(load_library().moe_adapter_backward(
@@ -482,8 +490,8 @@ def moe_balance_workspace_bytes(shape: MoEBalanceShape) -> int:
 
 
 def _balance_inputs(shape: MoEBalanceShape, logits, topk_idx, seq_offsets, mask):
-    assert logits.is_cuda and logits.dtype == torch.float32 and logits.is_contiguous() and logits.shape == (shape.T, shape.E)
-    assert topk_idx.is_cuda and topk_idx.dtype == torch.int32 and topk_idx.is_contiguous() and topk_idx.shape == (shape.T, shape.k)
+    assert logits.is_cuda and logits.dtype is _F32 and logits.is_contiguous() and logits.shape == (shape.T, shape.E)
+    assert topk_idx.is_cuda and topk_idx.dtype is _I32 and topk_idx.is_contiguous() and topk_idx.shape == (shape.T, shape.k)
     if seq_offsets is not None:
         assert seq_offsets.is_cuda and seq_offsets.dtype == torch.int32 and seq_offsets.is_contiguous()
         assert seq_offsets.shape == (shape.seqs + 1,)
@@ -515,10 +523,11 @@ def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: Balanc
         if t is not None:
             assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (shape.T, shape.k)
     assert dloss.is_cuda and dloss.dtype == torch.float32 and dloss.numel() == 1
-    assert out_dtype in (torch.float32, torch.bfloat16)
+    assert out_dtype is _F32 or out_dtype is _BF16
     if out is None:
-        out = logits.new_empty((shape.T, shape.E), dtype=out_dtype)
-    assert out.is_cuda and out.dtype == out_dtype and out.is_contiguous() and out.shape == (shape.T, shape.E)
+        out = torch.empty_like(logits) if out_dtype is _F32 else torch.empty((shape.T, shape.E), dtype=_BF16, device=logits.device)
+    else:
+        assert out.is_cuda and out.dtype is out_dtype and out.is_contiguous() and out.shape == (shape.T, shape.E)
     cs = stats.c_struct()
     _check(load_library().moe_balance_backward(
         ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), ctypes.byref(cs), _ptr(topk_w), _ptr(dtopk_w),

@@ -410,51 +410,64 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
     }
 }
 
-// Gradients of 8 ranks a wave and 512 columns of one adapter, token by token: the waves have different ranks, of a low rank different
-// columns.
+// Gradients of 8 ranks and 256 columns of one adapter, token by token; the waves share the tokens and their sums are added in LDS.  (With 512 columns a
+// wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4 workgroups that took 128 tokens one after
+// the other: 48 us.)
+constexpr int kGradRanks = 8, kGradCols = 256;
 struct FewGradShared {
-    float h[32][32];
+    float h[kFewTokens][kGradRanks];
+    float sums[4][kGradRanks][kGradCols];
     uint64_t mask[4];
     int32_t list[kFewTokens];
 };
-__host__ __device__ __forceinline__ int few_grad_waves(int r) { return r >= 32 ? 4 : r >= 16 ? 2 : 1; }   // waves with different ranks
 __device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared& S) {
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
     const int of = g.n * g.rank_tiles * g.col_tiles[0], which = id < of ? 0 : 1;
     if (which) id -= of;
-    const int cb = id % g.col_tiles[which], rest = id / g.col_tiles[which], a = rest % g.n, rb = rest / g.n;
-    const int rw = few_grad_waves(g.r), ranks = 8 * rw, W = g.W[which];
+    const int cb = id % g.col_tiles[which], rest = id / g.col_tiles[which], a = rest % g.n, j0 = rest / g.n * kGradRanks, W = g.W[which];
     Members mb;
     mb.find(g.T, g.n, p.ids, a, S.mask);
     list_members(mb, 0, kFewTokens, S.list);
-    const int count = mb.count();
-    const int j0 = rb * ranks, j8 = 8 * (w % rw), c = (cb * (4 / rw) + w / rw) * 512 + 8 * lane;
-    const float s = count == 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
-    const bool works = c < W && j0 + j8 < g.r;
-    float acc[8][8] = {};
-    for (int t0 = 0; t0 < count; t0 += 32) {
-        const int some = min(32, count - t0);
-        __syncthreads();
-        for (int i = tid; i < some * ranks; i += 256) {
-            const int k = i / ranks, j = i - k * ranks, tok = S.list[t0 + k];
-            if (j0 + j < g.r) S.h[k][j] = g.h[which] ? g.h[which][(size_t)tok * g.r + j0 + j] : whole_h(p, tok, j0 + j, s);
+    const int count = mb.count(), c = cb * kGradCols + 4 * lane;
+    float acc[kGradRanks][4] = {};
+    if (count > 0) {
+        const float s = p.scale ? p.scale[a] : 1.f;
+        for (int i = tid; i < count * kGradRanks; i += 256) {
+            const int k = i / kGradRanks, j = i % kGradRanks, tok = S.list[k];
+            S.h[k][j] = g.h[which] ? g.h[which][(size_t)tok * g.r + j0 + j] : whole_h(p, tok, j0 + j, s);
         }
         __syncthreads();
-        if (works) {
-#pragma unroll 2
-            for (int k = 0; k < some; ++k) {
-                const u32x4_t b = *(const u32x4_t*)(g.x[which] + (size_t)S.list[t0 + k] * g.ldx[which] + (size_t)c * 2);
+        if (c < W) {
+            const char* x = g.x[which] + (size_t)c * 2;
+#pragma unroll 8
+            for (int k = w; k < count; k += 4) {
+                const u32x2_t b = *(const u32x2_t*)(x + (size_t)S.list[k] * g.ldx[which]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) fma8(acc[j], S.h[k][j8 + j], b);
+                for (int j = 0; j < kGradRanks; ++j) {
+                    const float h = S.h[k][j];
+                    acc[j][0] += h * bf16_lo(b[0]);
+                    acc[j][1] += h * bf16_hi(b[0]);
+                    acc[j][2] += h * bf16_lo(b[1]);
+                    acc[j][3] += h * bf16_hi(b[1]);
+                }
             }
         }
     }
-    if (!works) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        f32x4_t* to = (f32x4_t*)(g.out[which] + ((size_t)a * g.r + j0 + j8 + j) * W + c);
-        to[0] = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
-        to[1] = f32x4_t{acc[j][4], acc[j][5], acc[j][6], acc[j][7]};
+    for (int j = 0; j < kGradRanks; ++j) *(f32x4_t*)&S.sums[w][j][4 * lane] = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+    __syncthreads();
+    if (c >= W) return;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {   // wave w adds up ranks w and w + 4
+        const int j = w + 4 * i;
+        f32x4_t v = *(const f32x4_t*)&S.sums[0][j][4 * lane];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+            const f32x4_t o = *(const f32x4_t*)&S.sums[k][j][4 * lane];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) v[q] += o[q];
+        }
+        *(f32x4_t*)(g.out[which] + ((size_t)a * g.r + j0 + j) * W + c) = v;
     }
 }
 
@@ -979,9 +992,9 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
             few_params(p, ws, f);
             few_first<kKc>(p, f, st);
         }
-        const int cols = 512 * (4 / few_grad_waves(g.r)), joins = s.T > 0 ? few_joins(p) : 0;
-        g.rank_tiles = (g.r + 8 * few_grad_waves(g.r) - 1) / (8 * few_grad_waves(g.r));
-        for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
+        const int joins = s.T > 0 ? few_joins(p) : 0;
+        g.rank_tiles = g.r / kGradRanks;
+        for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols - 1) / kGradCols;
         hipLaunchKernelGGL(adapter_few_second_grad_kernel, dim3((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st,
                            p, g, joins);
     } else {

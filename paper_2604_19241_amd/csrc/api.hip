@@ -95,7 +95,7 @@ int check_adapter_shape(const moe_adapter_shape_t* s) {
     if (s->T < 0 || s->T > 1 << 26 || s->adapters < 1 || s->adapters > kMaxAdapters) return MOE_ERR_SHAPE;
     if (s->rank < 8 || s->rank > kMaxRank || s->rank % 8 != 0) return MOE_ERR_SHAPE;
     for (int width : {s->K, s->N}) {
-        if (width < 8 || width > 1 << 17 || width % 8 != 0) return MOE_ERR_SHAPE;
+        if (width < 8 || width > 1 << 16 || width % 8 != 0) return MOE_ERR_SHAPE;
         if ((int64_t)s->T * width > (1ll << 38)) return MOE_ERR_SHAPE;
     }
     return MOE_OK;

@@ -61,6 +61,28 @@ __device__ __forceinline__ int seq_of(const BalParams& p, int t) {
     return lo;
 }
 
+// v = f over aligned groups of G lanes.  Lane exchanges of the vector unit (16 lanes by DPP, then rows and halves swapped), not through LDS: a shuffle each
+// took half of the kernels' time.
+template <int CTRL, class F>
+__device__ __forceinline__ void across_dpp(float& v, F f) {
+    v = f(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true)));
+}
+template <int G, class F>
+__device__ __forceinline__ void across(float& v, F f) {
+    if (G > 1) across_dpp<0xb1>(v, f);    // quad_perm [1, 0, 3, 2]
+    if (G > 2) across_dpp<0x4e>(v, f);    // quad_perm [2, 3, 0, 1]
+    if (G > 4) across_dpp<0x141>(v, f);   // row_half_mirror
+    if (G > 8) across_dpp<0x140>(v, f);   // row_mirror
+    if (G > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (G > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+}
+
 // G lanes share a token, each with 4 NV of its experts: runs of 4 where rows are 16-byte aligned, else every G-th.
 template <int G, int NV, bool VEC>
 struct TokenLanes {
@@ -92,14 +114,13 @@ struct TokenLanes {
             }
         }
     }
+    // over the lanes of a token, the same bits in each
     static __device__ __forceinline__ float sum(float v) {
-#pragma unroll
-        for (int o = G / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
+        across<G>(v, [](float a, float b) { return a + b; });
         return v;
     }
     static __device__ __forceinline__ float most(float v) {
-#pragma unroll
-        for (int o = G / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
+        across<G>(v, [](float a, float b) { return fmaxf(a, b); });
         return v;
     }
 };
@@ -108,7 +129,7 @@ typedef __attribute__((ext_vector_type(4))) int32_t i32x4_t;
 template <int G, int NV, bool VEC>
 __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams p) {
     using L = TokenLanes<G, NV, VEC>;
-    constexpr int kMost = 4 * G * NV, kGroups = 64 / G;
+    constexpr int kMost = 4 * G * NV, kGroups = 64 / G, kU = NV == 1 ? 4 : 1;
     __shared__ float s_p[kBalWaves][kMost];
     __shared__ int32_t s_c[kMost];
     __shared__ float s_z[kBalWaves];
@@ -130,32 +151,43 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
         }
         float sums[L::kValues] = {}, z = 0.f;
         int n = 0;
-        for (int t = a + w * kGroups + lane / G; t < b; t += kBalWaves * kGroups) {
-            const bool keep = !p.mask || p.mask[t];
-            float m = -INFINITY, total = 1.f, x[L::kValues];
-            if (keep) {
-                ln.template load<f32x4_t>(p.logits + (size_t)t * E, E, -INFINITY, x);
+        // U tokens a turn: their loads are on their way together
+        for (int t0 = a + w * kGroups + lane / G; t0 < b; t0 += kU * kBalWaves * kGroups) {
+            float x[kU][L::kValues];
+            bool keep[kU];
 #pragma unroll
-                for (int v = 0; v < L::kValues; ++v) m = fmaxf(m, x[v]);
-                m = L::most(m);
-                float q = 0.f;
-#pragma unroll
-                for (int v = 0; v < L::kValues; ++v) {
-                    x[v] = ln.expert(v) < E ? __expf(x[v] - m) : 0.f;
-                    q += x[v];
-                }
-                total = L::sum(q);
-                const float inv = 1.f / total;
-#pragma unroll
-                for (int v = 0; v < L::kValues; ++v) sums[v] += x[v] * inv;
+            for (int u = 0; u < kU; ++u) {
+                const int t = t0 + u * kBalWaves * kGroups;
+                keep[u] = t < b && (!p.mask || p.mask[t]);
             }
-            const float lse = keep ? m + logf(total) : -INFINITY;
-            if (ln.g == 0) {
-                p.lse[t] = lse;
-                if (keep) {
-                    z += lse * lse;
-                    ++n;
+#pragma unroll
+            for (int u = 0; u < kU; ++u)
+                if (keep[u]) ln.template load<f32x4_t>(p.logits + (size_t)(t0 + u * kBalWaves * kGroups) * E, E, -INFINITY, x[u]);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                const int t = t0 + u * kBalWaves * kGroups;
+                float lse = -INFINITY;
+                if (keep[u]) {
+                    float m = x[u][0];
+#pragma unroll
+                    for (int v = 1; v < L::kValues; ++v) m = fmaxf(m, x[u][v]);
+                    m = L::most(m);
+                    float q = 0.f;
+#pragma unroll
+                    for (int v = 0; v < L::kValues; ++v) {
+                        x[u][v] = ln.expert(v) < E ? __expf(x[u][v] - m) : 0.f;
+                        q += x[u][v];
+                    }
+                    const float total = L::sum(q), inv = 1.f / total;
+#pragma unroll
+                    for (int v = 0; v < L::kValues; ++v) sums[v] += x[u][v] * inv;
+                    lse = m + logf(total);
+                    if (ln.g == 0) {
+                        z += lse * lse;
+                        ++n;
+                    }
                 }
+                if (ln.g == 0 && t < b) p.lse[t] = lse;
             }
         }
         // the groups of a wave, then the waves
@@ -188,29 +220,30 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
     }
 }
 
-// Sums the parts of one sequence and 32 experts; the workgroup that is last to end adds up the losses.
-constexpr int kSumThreads = 1024, kSumExperts = 32, kSumGroups = kSumThreads / kSumExperts;
-__global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p) {
-    __shared__ float s_p[kSumGroups][kSumExperts];
-    __shared__ int32_t s_c[kSumGroups][kSumExperts];
-    __shared__ double s_d[2][kSumThreads / kWave];
-    __shared__ int32_t s_i[kSumThreads / kWave];
+// Sums the parts of one sequence and `wide` experts (a power of two), 1024 / wide threads an expert; where there are several workgroups, the one that is last
+// to end adds up the losses.  What it reads of the others they have written through to memory: a fence each, which writes back an L2, took
+// most of the time (61 sequences of 256 experts, 488 workgroups of 32 experts 24 us).
+constexpr int kSumThreads = 1024, kSumWaves = kSumThreads / kWave;
+__global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p, int wide, int blocks) {
+    __shared__ float s_p[kSumThreads];
+    __shared__ int32_t s_c[kSumThreads];
+    __shared__ double s_d[3][kSumWaves];
+    __shared__ int32_t s_i[2][kSumWaves];
     __shared__ int s_last;
-    const int tid = threadIdx.x, blocks = (p.E + kSumExperts - 1) / kSumExperts, s = blockIdx.x / blocks, eb = blockIdx.x % blocks;
+    const int tid = threadIdx.x, s = blockIdx.x / blocks, eb = blockIdx.x % blocks;
     const int from = seq_begin(p, s), to = seq_begin(p, s + 1);
     const int first = from / p.chunk, count = to > from ? (to - 1) / p.chunk - first + 1 : 0;
-    const int e = eb * kSumExperts + tid % kSumExperts, grp = tid / kSumExperts;
-    float sum = 0.f;
-    int c = 0;
-    if (e < p.E)
-#pragma unroll 4
-        for (int i = grp; i < count; i += kSumGroups) {
-            const size_t slot = (size_t)first + i + s;
-            sum += p.part_p[slot * p.E + e];
-            c += p.part_c[slot * p.E + e];
-        }
-    s_p[grp][tid % kSumExperts] = sum;
-    s_c[grp][tid % kSumExperts] = c;
+    const int lane = tid & (wide - 1), e = eb * wide + lane, grp = tid / wide, groups = kSumThreads / wide;
+    auto sum_d = [&](double x, int which) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+        if ((tid & 63) == 0) s_d[which][tid >> 6] = x;
+    };
+    auto sum_i = [&](int x, int which) {
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
+        if ((tid & 63) == 0) s_i[which][tid >> 6] = x;
+    };
     // the kept tokens of the sequence, and its z
     int n = 0;
     double z = 0.0;
@@ -219,75 +252,73 @@ __global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p) {
         n += p.part_n[slot];
         z += (double)p.part_z[slot];
     }
-    auto block_sum = [&](double& x, int which) {
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-        if ((tid & 63) == 0) s_d[which][tid >> 6] = x;
-    };
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-    if ((tid & 63) == 0) s_i[tid >> 6] = n;
-    block_sum(z, 0);
-    __syncthreads();
-    n = 0;
-    z = 0.0;
-    for (int i = 0; i < kSumThreads / kWave; ++i) {
-        n += s_i[i];
-        z += s_d[0][i];
-    }
-    if (tid < kWave) {
-        double b = 0.0;
-        if (tid < kSumExperts && e < p.E) {
-            float ps = 0.f;
-            int cs = 0;
-#pragma unroll
-            for (int i = 0; i < kSumGroups; ++i) {
-                ps += s_p[i][tid];
-                cs += s_c[i][tid];
-            }
-            p.prob_sums[(size_t)s * p.E + e] = ps;
-            p.counts[(size_t)s * p.E + e] = cs;
-            b = (double)cs * ps;
+    float sum = 0.f;
+    int c = 0;
+    if (e < p.E)
+#pragma unroll 8
+        for (int i = grp; i < count; i += groups) {
+            const size_t at = ((size_t)first + i + s) * p.E + e;
+            sum += p.part_p[at];
+            c += p.part_c[at];
         }
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) b += __shfl_xor(b, o);
-        if (tid == 0) {
-            p.sum_b[blockIdx.x] = n > 0 ? b / ((double)p.k * n) : 0.0;
-            if (eb == 0) {
-                p.sum_z[s] = z;
-                p.tokens[s] = n;
-            }
-            __threadfence();
-            s_last = atomicAdd(p.ticket, 1) == (int)gridDim.x - 1;
-        }
-    }
+    s_p[tid] = sum;
+    s_c[tid] = c;
+    sum_i(n, 0);
+    sum_d(z, 0);
     __syncthreads();
-    if (!s_last) return;
-    __threadfence();
     double b = 0.0;
-    z = 0.0;
-    n = 0;
-    for (int i = tid; i < (int)gridDim.x; i += kSumThreads) b += __hip_atomic_load(p.sum_b + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int i = tid; i < p.S; i += kSumThreads) {
-        z += __hip_atomic_load(p.sum_z + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        n += __hip_atomic_load(p.tokens + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (tid < wide && e < p.E) {
+        sum = 0.f;
+        c = 0;
+        for (int i = 0; i < groups; ++i) {
+            sum += s_p[i * wide + tid];
+            c += s_c[i * wide + tid];
+        }
+        p.prob_sums[(size_t)s * p.E + e] = sum;
+        p.counts[(size_t)s * p.E + e] = c;
+        b = (double)c * sum;
     }
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
-    block_sum(b, 0);
-    block_sum(z, 1);
-    if ((tid & 63) == 0) s_i[tid >> 6] = n;
+    sum_d(b, 1);
     __syncthreads();
-    if (tid == 0) {
+    b = z = 0.0;
+    n = 0;
+    for (int i = 0; i < kSumWaves; ++i) {
+        b += s_d[1][i];
+        z += s_d[0][i];
+        n += s_i[0][i];
+    }
+    if (n > 0) b /= (double)p.k * n;
+    if (tid == 0 && eb == 0) __hip_atomic_store(p.tokens + s, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (gridDim.x > 1) {
+        if (tid == 0) {
+            store_wt8(p.sum_b + blockIdx.x, __builtin_bit_cast(u32x2_t, b));
+            if (eb == 0) store_wt8(p.sum_z + s, __builtin_bit_cast(u32x2_t, z));
+            wait_stores();
+            s_last = __hip_atomic_fetch_add(p.ticket, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+        }
+        __syncthreads();
+        if (!s_last) return;
         b = z = 0.0;
         n = 0;
-        for (int i = 0; i < kSumThreads / kWave; ++i) {
-            b += s_d[0][i];
-            z += s_d[1][i];
-            n += s_i[i];
+        for (int i = tid; i < (int)gridDim.x; i += kSumThreads) b += __hip_atomic_load(p.sum_b + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int i = tid; i < p.S; i += kSumThreads) {
+            z += __hip_atomic_load(p.sum_z + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            n += __hip_atomic_load(p.tokens + i, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         }
-        const double per = 1.0 / (n > 0 ? n : 1);
-        const double balance = p.E * per * b;
+        sum_i(n, 1);
+        sum_d(b, 1);
+        sum_d(z, 2);
+        __syncthreads();
+        b = z = 0.0;
+        n = 0;
+        for (int i = 0; i < kSumWaves; ++i) {
+            b += s_d[1][i];
+            z += s_d[2][i];
+            n += s_i[1][i];
+        }
+    }
+    if (tid == 0) {
+        const double per = 1.0 / (n > 0 ? n : 1), balance = p.E * per * b;
         z *= per;
         p.tokens[p.S] = n;
         p.loss[0] = (float)(p.balance_coef * balance + p.z_coef * z);
@@ -296,103 +327,118 @@ __global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p) {
     }
 }
 
+// The gates' part goes to its experts through a row of LDS that is all zeros between tokens: the lanes of the slots add to it and clear their
+// entries again once every lane has read its own.
 template <int G, int NV, bool VEC>
 __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams p) {
     using L = TokenLanes<G, NV, VEC>;
-    constexpr int kGroups = 64 / G, kSlots = (kMaxTopK + G - 1) / G;
+    constexpr int kGroups = 64 / G, kSlots = (kMaxTopK + G - 1) / G, kMost = 4 * G * NV, kU = NV == 1 && G > 8 ? 2 : 1;
+    __shared__ __attribute__((aligned(16))) float s_row[kBalWaves * kGroups][kMost];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, E = p.E;
     const L ln(lane);
+    float* const row = s_row[w * kGroups + lane / G];
     const int c0 = blockIdx.x * p.chunk, c1 = min(p.T, c0 + p.chunk);
     const int all = p.tokens[p.S];
-    const float u = *p.dloss, per = 1.f / (float)max(all, 1);
-    const float cb = u * p.balance_coef * (float)E * per, cz = u * p.z_coef * 2.f * per;
+    const float up = *p.dloss, per = 1.f / (float)max(all, 1);
+    const float cb = up * p.balance_coef * (float)E * per, cz = up * p.z_coef * 2.f * per;
+    if (p.w)
+#pragma unroll
+        for (int v = 0; v < L::kValues; ++v) row[ln.expert(v)] = 0.f;
     int s = -1, end = 0;
     float f[L::kValues];   // cb f[s]
-    for (int t0 = c0 + w * kGroups; t0 < c1; t0 += kBalWaves * kGroups) {
-        const int t = t0 + lane / G;
-        const bool there = t < c1;   // (the lanes of a wave stay together: they exchange the slots)
-        float d[L::kValues];
+    for (int t0 = c0 + w * kGroups + lane / G; t0 < c1; t0 += kU * kBalWaves * kGroups) {
+        float d[kU][L::kValues], lse[kU], g[kU][kSlots], dw[kU][kSlots];
+        int e[kU][kSlots];
 #pragma unroll
-        for (int v = 0; v < L::kValues; ++v) d[v] = 0.f;
-        const float lse = there ? p.lse[t] : -INFINITY;
-        if (lse != -INFINITY) {   // (a token that is not kept)
-            if (s < 0 || t >= end) {
-                s = seq_of(p, t);
-                end = seq_begin(p, s + 1);
-                const float scale = cb / ((float)p.k * (float)max(p.tokens[s], 1));
-                int32_t cnt[L::kValues];
-                ln.template load<i32x4_t>(p.counts + (size_t)s * E, E, 0, cnt);
-#pragma unroll
-                for (int v = 0; v < L::kValues; ++v) f[v] = scale * (float)cnt[v];
-            }
-            ln.template load<f32x4_t>(p.logits + (size_t)t * E, E, -INFINITY, d);
-            float inner = 0.f;
-#pragma unroll
-            for (int v = 0; v < L::kValues; ++v) {
-                d[v] = ln.expert(v) < E ? __expf(d[v] - lse) : 0.f;
-                inner += f[v] * d[v];
-            }
-            inner = L::sum(inner);
-            const float add = cz * lse - inner;
-#pragma unroll
-            for (int v = 0; v < L::kValues; ++v) d[v] *= f[v] + add;
-        }
-        if (p.w) {
-            int e[kSlots];
-            float g[kSlots], mean = 0.f;
+        for (int u = 0; u < kU; ++u) {
+            const int t = t0 + u * kBalWaves * kGroups;
+            lse[u] = t < c1 ? p.lse[t] : -INFINITY;   // -inf: a token that is not kept
+            if (t < c1) ln.template load<f32x4_t>(p.logits + (size_t)t * E, E, -INFINITY, d[u]);
 #pragma unroll
             for (int i = 0; i < kSlots; ++i) {
                 const int j = i * G + ln.g;
-                e[i] = -1;
-                g[i] = 0.f;
-                if (there && j < p.k) {
+                e[u][i] = -1;
+                g[u][i] = dw[u][i] = 0.f;
+                if (p.w && t < c1 && j < p.k) {
                     const size_t at = (size_t)t * p.k + j;
-                    const int x = p.idx[at];
-                    if ((unsigned)x < (unsigned)E) {
-                        e[i] = x;
-                        g[i] = p.w[at];
-                        mean += g[i] * p.dw[at];
-                    }
+                    e[u][i] = p.idx[at];
+                    g[u][i] = p.w[at];
+                    dw[u][i] = p.dw[at];
                 }
             }
-            mean = L::sum(mean);
-#pragma unroll
-            for (int i = 0; i < kSlots; ++i)
-                if (e[i] >= 0) g[i] *= p.dw[(size_t)t * p.k + i * G + ln.g] - mean;
-#pragma unroll
-            for (int i = 0; i < kSlots; ++i)
-                for (int j = 0; j < min(G, p.k - i * G); ++j) {
-                    int ej;
-                    float gj;
-                    if (G == 64) {
-                        ej = __builtin_amdgcn_readlane(e[i], j);
-                        gj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g[i]), j));
-                    } else {
-                        ej = __shfl(e[i], j, G);
-                        gj = __shfl(g[i], j, G);
-                    }
-#pragma unroll
-                    for (int v = 0; v < L::kValues; ++v) d[v] += ln.expert(v) == ej ? gj : 0.f;
-                }
         }
-        if (!there) continue;
-        if (VEC) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int e = 4 * (G * i + ln.g);
-                if (e >= E) continue;
-                if (p.out_bf16)
-                    *(u32x2_t*)((uint16_t*)p.dlogits + (size_t)t * E + e) = u32x2_t{pack_bf16x2(d[4 * i], d[4 * i + 1]), pack_bf16x2(d[4 * i + 2], d[4 * i + 3])};
-                else
-                    *(f32x4_t*)((float*)p.dlogits + (size_t)t * E + e) = f32x4_t{d[4 * i], d[4 * i + 1], d[4 * i + 2], d[4 * i + 3]};
+        for (int u = 0; u < kU; ++u) {
+            const int t = t0 + u * kBalWaves * kGroups;
+            if (t >= c1) break;
+            if (lse[u] != -INFINITY) {
+                if (s < 0 || t >= end) {
+                    s = seq_of(p, t);
+                    end = seq_begin(p, s + 1);
+                    const float scale = cb / ((float)p.k * (float)max(p.tokens[s], 1));
+                    int32_t cnt[L::kValues];
+                    ln.template load<i32x4_t>(p.counts + (size_t)s * E, E, 0, cnt);
+#pragma unroll
+                    for (int v = 0; v < L::kValues; ++v) f[v] = scale * (float)cnt[v];
+                }
+                float inner = 0.f;
+#pragma unroll
+                for (int v = 0; v < L::kValues; ++v) {
+                    d[u][v] = ln.expert(v) < E ? __expf(d[u][v] - lse[u]) : 0.f;
+                    inner += f[v] * d[u][v];
+                }
+                const float add = cz * lse[u] - L::sum(inner);
+#pragma unroll
+                for (int v = 0; v < L::kValues; ++v) d[u][v] *= f[v] + add;
+            } else {
+#pragma unroll
+                for (int v = 0; v < L::kValues; ++v) d[u][v] = 0.f;
             }
-        } else {
+            if (p.w) {
+                float mean = 0.f;
 #pragma unroll
-            for (int v = 0; v < L::kValues; ++v) {
-                const int e = ln.expert(v);
-                if (e >= E) continue;
-                if (p.out_bf16) ((uint16_t*)p.dlogits)[(size_t)t * E + e] = (uint16_t)(pack_bf16x2(d[v], 0.f) & 0xffffu);
-                else ((float*)p.dlogits)[(size_t)t * E + e] = d[v];
+                for (int i = 0; i < kSlots; ++i) {
+                    if ((unsigned)e[u][i] >= (unsigned)E) g[u][i] = 0.f;
+                    mean += (unsigned)e[u][i] < (unsigned)E ? g[u][i] * dw[u][i] : 0.f;
+                }
+                mean = L::sum(mean);
+#pragma unroll
+                for (int i = 0; i < kSlots; ++i)
+                    if ((unsigned)e[u][i] < (unsigned)E) atomicAdd(&row[e[u][i]], g[u][i] * (dw[u][i] - mean));
+                asm volatile("" ::: "memory");   // (one wave's LDS operations are done in order)
+#pragma unroll
+                for (int v = 0; v < L::kValues; v += VEC ? 4 : 1) {
+                    if (VEC) {
+                        const f32x4_t r = *(const f32x4_t*)&row[ln.expert(v)];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) d[u][v + c] += r[c];
+                    } else {
+                        d[u][v] += row[ln.expert(v)];
+                    }
+                }
+                asm volatile("" ::: "memory");
+#pragma unroll
+                for (int i = 0; i < kSlots; ++i)
+                    if ((unsigned)e[u][i] < (unsigned)E) row[e[u][i]] = 0.f;
+                asm volatile("" ::: "memory");
+            }
+            if (VEC) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i) {
+                    const int x = 4 * (G * i + ln.g);
+                    if (x >= E) continue;
+                    const float* v = &d[u][4 * i];
+                    if (p.out_bf16) *(u32x2_t*)((uint16_t*)p.dlogits + (size_t)t * E + x) = u32x2_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+                    else *(f32x4_t*)((float*)p.dlogits + (size_t)t * E + x) = f32x4_t{v[0], v[1], v[2], v[3]};
+                }
+            } else {
+#pragma unroll
+                for (int v = 0; v < L::kValues; ++v) {
+                    const int x = ln.expert(v);
+                    if (x >= E) continue;
+                    if (p.out_bf16) ((uint16_t*)p.dlogits)[(size_t)t * E + x] = (uint16_t)(pack_bf16x2(d[u][v], 0.f) & 0xffffu);
+                    else ((float*)p.dlogits)[(size_t)t * E + x] = d[u][v];
+                }
             }
         }
     }
@@ -406,7 +452,14 @@ static int chunk_of(const moe_balance_shape_t& s) {
     while (chunk > 4 && (long long)chunk * s.seqs > 4ll * s.T) chunk /= 2;   // a part is a turn of the workgroup: few sequences a chunk
     return chunk;
 }
-static int sum_blocks(const moe_balance_shape_t& s) { return (s.E + kSumExperts - 1) / kSumExperts; }
+// Experts of a workgroup of the sum: as many as leave a thread up to 16 parts.
+static int sum_wide(const moe_balance_shape_t& s) {
+    const long long parts = (s.T + chunk_of(s) - 1) / chunk_of(s) / s.seqs + 1;
+    int wide = 32;
+    while (wide < s.E && wide * 2 * parts <= 16 * kSumThreads) wide *= 2;
+    return wide;
+}
+static int sum_blocks(const moe_balance_shape_t& s) { return (s.E + sum_wide(s) - 1) / sum_wide(s); }
 struct BalLayout {
     size_t p, c, z, n, b, sz, ticket, total;
 };
@@ -467,7 +520,7 @@ int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, co
             hipLaunchKernelGGL((balance_forward_kernel<g.value, nv.value, vec.value>), dim3((unsigned)p.chunks), dim3(kBalThreads), 0, st, p);
         });
     else hipLaunchKernelGGL(balance_ticket_kernel, dim3(1), dim3(1), 0, st, p.ticket);
-    hipLaunchKernelGGL(balance_sum_kernel, dim3((unsigned)(s.seqs * sum_blocks(s))), dim3(kSumThreads), 0, st, p);
+    hipLaunchKernelGGL(balance_sum_kernel, dim3((unsigned)(s.seqs * sum_blocks(s))), dim3(kSumThreads), 0, st, p, sum_wide(s), sum_blocks(s));
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -480,7 +533,7 @@ int balance_backward_launch(const moe_balance_shape_t& s, const float* logits, c
     p.counts = stats.counts, p.tokens = stats.tokens, p.lse = stats.lse;
     p.w = w, p.dw = dw, p.dloss = dloss, p.dlogits = dlogits, p.out_bf16 = out_bf16;
     p.chunk = 32;
-    while (p.chunk < 128 && (s.T + p.chunk - 1) / p.chunk > 1024) p.chunk *= 2;
+    while (p.chunk < 64 && (s.T + p.chunk - 1) / p.chunk > 2048) p.chunk *= 2;
     p.chunks = (s.T + p.chunk - 1) / p.chunk;
     const bool vec = rows_aligned(logits, dlogits, s.E) && ((uintptr_t)stats.counts & 15) == 0;
     by_experts(s.E, vec, [&](auto g, auto nv, auto v) {

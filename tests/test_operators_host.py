@@ -39,7 +39,7 @@ def adapter_calls(lib, s, **kw):
                                                      a["h"], a["dx"], a["da"], a["db"], a["ws"], a["nbytes"], None)}
 
 
-@pytest.mark.parametrize("kw", [dict(T=-1), dict(T=(1 << 26) + 1), dict(K=0), dict(K=60), dict(K=(1 << 17) + 8), dict(N=4), dict(N=129), dict(rank=0), dict(rank=12),
+@pytest.mark.parametrize("kw", [dict(T=-1), dict(T=(1 << 26) + 1), dict(K=0), dict(K=60), dict(K=(1 << 16) + 8), dict(N=4), dict(N=129), dict(rank=0), dict(rank=12),
                                 dict(rank=136), dict(adapters=0), dict(adapters=1025), dict(T=1 << 26, K=8192)])
 def test_adapter_shapes_outside_the_limits(lib, kw):
     s = moe.make_adapter_shape(**(GOOD | kw))
