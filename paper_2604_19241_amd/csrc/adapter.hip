@@ -14,15 +14,13 @@
 #include "adapter.hpp"
 
 #include <algorithm>
+#include <type_traits>
 
 namespace uniep {
 
-typedef __attribute__((ext_vector_type(4))) __bf16 bf16x4v_t;
-typedef __attribute__((address_space(3))) char* lds_ptr3_t;
-typedef __attribute__((address_space(3))) bf16x4v_t* lds_tr3_t;
-
 constexpr int kFewTokens = 256;
-constexpr int kBlockRows = 32;        // rows of a block of the plan (one fragment)
+// Rows of a block of the plan: as many tokens of one adapter share the fetch of its first factor.
+static int block_rows(int T) { return T >= 16384 ? 64 : 32; }
 constexpr int kUnit = 64;             // rows of which the plan knows the first and the last segment
 
 // ------------------------------------------------------------------ the plan
@@ -34,9 +32,9 @@ struct PlanView {
     int32_t* ordinal;    // [n] which segment an adapter is
     int32_t* seg;        // [n] segment -> adapter
     int32_t* unit;       // [units][2] segments of the first and the last row of every kUnit rows (-1: no adapter)
-    int32_t* block;      // [blocks][2] first row; rows | (adapter + 1) << 8.  One adapter, one multiple of kBlockRows
+    int32_t* block;      // [blocks][2] first row; rows | (adapter + 1) << 8.  One adapter, one multiple of block_rows
 };
-static size_t plan_blocks(const moe_adapter_shape_t& s) { return (size_t)s.T / kBlockRows + s.adapters + 2; }
+static size_t plan_blocks(const moe_adapter_shape_t& s) { return (size_t)s.T / block_rows(s.T) + s.adapters + 2; }
 static size_t plan_units(const moe_adapter_shape_t& s) { return ((size_t)s.T + kUnit - 1) / kUnit; }
 static size_t plan_words(const moe_adapter_shape_t& s) {
     return 16 + (size_t)s.T + 3 * (size_t)s.adapters + 1 + 2 * plan_units(s) + 2 * plan_blocks(s);
@@ -58,7 +56,7 @@ size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) 
 // One workgroup: a counting sort.  Every wave counts a contiguous part of the tokens and later gives its tokens their rows, 64 at a
 // time: lanes with the same adapter find each other with a ballot for each bit of the id.
 constexpr int kSortWaves = 16;
-__global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, const int32_t* __restrict__ ids, PlanView v) {
+__global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, int brows, const int32_t* __restrict__ ids, PlanView v) {
     __shared__ int32_t hist[kSortWaves][kMaxAdapters + 1];
     __shared__ int32_t first[kMaxAdapters + 2];     // rows before bin b (bin 0: no adapter, bin a + 1: adapter a)
     __shared__ int32_t fblock[kMaxAdapters + 2], fseg[kMaxAdapters + 2];
@@ -102,7 +100,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         int total;
         const int r0 = scan(c, 0, base_rows, total);
         base_rows += total;
-        const int nb = c > 0 ? (r0 + c - 1) / kBlockRows - r0 / kBlockRows + 1 : 0;
+        const int nb = c > 0 ? (r0 + c - 1) / brows - r0 / brows + 1 : 0;
         const int k0 = scan(nb, 1, base_blocks, total);
         base_blocks += total;
         const int s0 = scan(b > 0 && c > 0 ? 1 : 0, 2, base_segs, total);
@@ -155,9 +153,9 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
     for (int b = w; b < bins; b += kSortWaves) {
         const int r0 = first[b], r1 = first[b + 1], o = b > 0 ? fseg[b] : -1;
         if (r1 <= r0) continue;
-        const int q0 = r0 / kBlockRows, q1 = (r1 - 1) / kBlockRows;
+        const int q0 = r0 / brows, q1 = (r1 - 1) / brows;
         for (int q = q0 + lane; q <= q1; q += 64) {
-            const int a = max(r0, q * kBlockRows), e = min(r1, (q + 1) * kBlockRows);
+            const int a = max(r0, q * brows), e = min(r1, (q + 1) * brows);
             v.block[2 * (fblock[b] + q - q0)] = a;
             v.block[2 * (fblock[b] + q - q0) + 1] = (e - a) | b << 8;
         }
@@ -170,7 +168,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
 
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st) {
     if (adapter_few(s)) return MOE_OK;
-    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, ids, plan_view(s, plan));
+    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T), ids, plan_view(s, plan));
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -196,6 +194,8 @@ struct ProjParams {
     PlanView plan;
     char* hx;               // the low-rank rows of every tile (hx_base)
     char* second_t;         // [n][C][r] (KC)
+    uint16_t* terms[2];     // backward: [T rows][3][r], h (of the forward call) and this h as three bf16 terms, by row
+    const float* h_given;   // the forward call's h
     int tile_rows;
     int blocks;             // at most, of the plan
 };
@@ -253,7 +253,8 @@ __device__ __forceinline__ void list_members(const Members& mb, int skip, int mo
 // 32nd of its adapter's has nothing to do.
 template <int NRF, int FORM>
 __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjParams p) {
-    __shared__ __attribute__((aligned(512))) char smem[SmallTile<NRF, 2>::kLds];
+    constexpr int kLds = SmallTile<NRF, 2>::kLds > SmallTile<1, 2>::kLds ? SmallTile<NRF, 2>::kLds : SmallTile<1, 2>::kLds;   // (h: 32 rows)
+    __shared__ __attribute__((aligned(512))) char smem[kLds];
     __shared__ uint64_t s_mask[4];
     __shared__ int32_t s_list[32];
     const Stages all = stages_of(p.R);
@@ -511,9 +512,21 @@ static size_t hx_bytes(const moe_adapter_shape_t& s, int tile_rows) {
 
 // h of one block of the plan, as fp32 and as the rows of its tile's low-rank part; behind the blocks, where the factors are wanted
 // transposed, 64 columns of one adapter's a workgroup.
-template <int NCF>
+// v as three bf16 terms: the whole 24 bits of an fp32 value
+__device__ __forceinline__ void store_terms(uint16_t* to, int r, float (&v)[8]) {
+#pragma unroll
+    for (int term = 0; term < 3; ++term) {
+        float e[8];
+#pragma unroll
+        for (int q = 0; q < 8; ++q) e[q] = bf16_round(v[q]);
+        *(u32x4_t*)(to + term * r) = pack8f(e);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) v[q] = fabsf(e[q]) < INFINITY ? v[q] - e[q] : 0.f;   // (an infinite value stays one)
+    }
+}
+template <int NRF, int NCF>
 __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p) {
-    using S = SmallTile<1, NCF>;
+    using S = SmallTile<NRF, NCF>;
     __shared__ __attribute__((aligned(512))) char smem[S::kLds];
     const int tid = threadIdx.x;
     if ((int)blockIdx.x >= p.blocks) {
@@ -532,8 +545,10 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
         }
         return;
     }
-    if ((int)blockIdx.x >= p.plan.head[0]) return;
-    const int row0 = p.plan.block[2 * blockIdx.x], code = p.plan.block[2 * blockIdx.x + 1], rows = code & 255, a = (code >> 8) - 1;
+    // every XCD a run of the blocks: those of one adapter fetch its factor into one L2
+    const int nb = p.plan.head[0], per = (nb + 7) >> 3, slot = blockIdx.x >> 3, blk = (blockIdx.x & 7) * per + slot;
+    if (slot >= per || blk >= nb) return;
+    const int row0 = p.plan.block[2 * blk], code = p.plan.block[2 * blk + 1], rows = code & 255, a = (code >> 8) - 1;
     const int tile = row0 / p.tile_rows;
     const TileLow tl = tile_low(p, tile);
     uint16_t* const hx = (uint16_t*)p.hx + tl.at + (size_t)(row0 - tile * p.tile_rows) * tl.ld;
@@ -547,18 +562,30 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
         return;
     }
     const Stages st = stages_of(p.R);
-    f32x16_t acc[1][NCF];
+    if (p.terms[0])
+        for (int i = tid; i < rows * (p.r / 8); i += kSmallThreads) {
+            const int row = i / (p.r / 8), col = 8 * (i - row * (p.r / 8));
+            const f32x4_t* q = (const f32x4_t*)(p.h_given + (size_t)p.plan.order[row0 + row] * p.r + col);
+            float v[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] = q[0][j];
+                v[4 + j] = q[1][j];
+            }
+            store_terms(p.terms[0] + (size_t)(row0 + row) * 3 * p.r + col, p.r, v);
+        }
+    f32x16_t acc[NRF][NCF];
     {
         const Lane ln;
-        KcStages<1, false> lb;
+        KcStages<NRF, false> lb;
         lb.init(ln, rows, st, [&](int r) { return p.x + (size_t)p.plan.order[row0 + r] * p.ldx; });
         lb.low.used = 0;
         KcStages<NCF, true> la;
         la.init(ln, p.r, st, [&](int j) { return p.first + ((size_t)a * p.r + j) * p.R * 2; });
-        small_loop<1, NCF, kKc>(lb, la, st.full + (st.tail > 0), smem, acc);
+        small_loop<NRF, NCF, kKc>(lb, la, st.full + (st.tail > 0), smem, acc);
     }
     const float s = p.scale ? p.scale[a] : 1.f;
-    small_sum<1, NCF>(smem, acc, [&](int row, int col, const float (&v)[8]) {
+    small_sum<NRF, NCF>(smem, acc, [&](int row, int col, const float (&v)[8]) {
         if (row >= rows || col >= p.r) return;
         float h[8], hi[8], lo[8];
 #pragma unroll
@@ -573,6 +600,7 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
         uint16_t* x = hx + (size_t)row * tl.ld + own + col;
         *(u32x4_t*)x = pack8f(hi);
         *(u32x4_t*)(x + p.r) = pack8f(lo);
+        if (p.terms[1]) store_terms(p.terms[1] + (size_t)(row0 + row) * 3 * p.r + col, p.r, h);
     });
 }
 
@@ -603,6 +631,19 @@ __device__ __forceinline__ LowRank low_of(const ProjParams& p, const TileLow& t,
     return LowRank{p.hx + t.at * 2, (uint32_t)t.ld * 2, transposed ? p.second_t : p.second, p.plan.seg + t.first, t.used, p.r, p.C};
 }
 
+// Which tile a workgroup has.  Workgroups go to the eight XCDs in turn; each XCD gets a run of the tiles in an order that has 8 row tiles
+// innermost, so that what it has at a time is about 8 x 4 tiles that meet in its L2.
+struct TileId {
+    int rt, ct;
+    __device__ __forceinline__ TileId(const ProjParams& p) {
+        const int n = p.row_tiles * p.col_tiles, x = blockIdx.x & 7, slot = blockIdx.x >> 3, per = n >> 3, more = n & 7;
+        const int id = x * per + min(x, more) + slot;   // (XCD x has per tiles, the first `more` one more: as many workgroups as go there)
+        const int group = 8 * p.col_tiles, g = id / group, in = id - g * group, rows = min(8, p.row_tiles - 8 * g);
+        ct = in / rows;
+        rt = 8 * g + in - ct * rows;
+    }
+};
+
 // Tiles of 64 x 64.
 // A factor with an infinity or NaN must not reach the rows of other adapters, but 0 times it would: a tile whose sums are not all finite
 // is computed again without its low-rank part, which is then added row by row (as is one where x or W is not finite).
@@ -610,7 +651,8 @@ template <int FORM>
 __global__ void __launch_bounds__(kSmallThreads) adapter_small_kernel(ProjParams p) {
     __shared__ __attribute__((aligned(512))) char smem[SmallTile<2, 2>::kLds];
     __shared__ int s_bad;
-    const int rt = blockIdx.x % p.row_tiles, ct = blockIdx.x / p.row_tiles;
+    const TileId at(p);
+    const int rt = at.rt, ct = at.ct;
     const int row0 = rt * 64, rows = min(64, p.T - row0), col0 = ct * 64;
     const TileLow tl = tile_low(p, rt);
     const Stages st = stages_of(p.R);
@@ -680,7 +722,8 @@ template <int FORM>
 __global__ void __launch_bounds__(kMmaThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) adapter_big_kernel(ProjParams p) {
     __shared__ __attribute__((aligned(512))) char smem[kMmaSmem];
     __shared__ int s_bad;
-    const int rt = blockIdx.x % p.row_tiles, ct = blockIdx.x / p.row_tiles;
+    const TileId at(p);
+    const int rt = at.rt, ct = at.ct;
     const int row0 = rt * p.tile_rows, rows = min(p.tile_rows, p.T - row0), col0 = ct * BN;
     const TileLow tl = tile_low(p, rt);
     const Stages st = stages_of(p.R);
@@ -737,93 +780,91 @@ __global__ void __launch_bounds__(kMmaThreads) __attribute__((amdgpu_waves_per_e
 }
 
 // ------------------------------------------------------------------ gradients of the factors, more tokens
-// out[a][j][c] = sum over the adapter's rows of h[row][j] x[row][c]: h as three bf16 terms (the whole 24 bits of the fp32 value: these sums are
-// returned in fp32), x as it is.  A stage is 64 rows, gathered through the plan into registers and from there into LDS; wave w takes
-// its k-sub-step w for the whole tile of 32 NRF ranks by 32 NCF columns, as in small_loop.
+// out[a][j][c] = sum over the adapter's rows of h[row][j] x[row][c]: h as three bf16 terms (the sums are returned in fp32; adapter_low_kernel
+// has written them row by row), x as it is.  A stage is 64 rows; both operands are KS images, x gathered through the plan; wave w
+// takes k-sub-step w of a stage for the whole tile of 32 NRF ranks by 32 NCF columns, as in small_loop.  Rows at and past the last come from the page of zeros.
 template <int NRF, int NCF>
 struct GradTile {
     static constexpr int kXRow = 64 * NCF, kHRow = 64 * NRF;
     static constexpr int kX = BK * kXRow, kH = BK * kHRow, kStage = kX + 3 * kH;
+    static constexpr int kDepth = NRF == 4 ? 2 : 3;
     static constexpr int kSums = 16384 * NCF;   // one fragment of ranks at a time
-    static constexpr int kLds = 2 * kStage > kSums ? 2 * kStage : kSums;
-    static constexpr int kXLoads = kX / (16 * kSmallThreads);
-    static constexpr int kHUnits = NRF;         // 8 values each, of a thread, at most
+    static constexpr int kLds = kDepth * kStage > kSums ? kDepth * kStage : kSums;
+    static constexpr int kXLoads = kX / 4096, kHLoads = 3 * kH / 4096;   // DMA instructions of a wave
+    static constexpr int kList = 2048;          // rows whose tokens are in LDS
 };
 // swizzle of a KS image with rows of `bytes`
 template <int BYTES>
 __device__ __forceinline__ int ks_swz(int k) { return BYTES == 64 ? 0 : BYTES == 128 ? (k & 2) << 1 : (k & 3) << 2; }
+// N fragments by transposing reads; a fragment's second half lies NEXT bytes behind its first
+template <int N, int NEXT>
+__device__ __forceinline__ void read_tr(u32x4_t (&f)[N], const uint32_t (&at)[N], uint32_t off) {
+    u32x2_t lo[N], hi[N];
+    if constexpr (N == 4) {
+        const uint32_t a0 = at[0] + off, a1 = at[1] + off, a2 = at[2] + off, a3 = at[3] + off;
+        asm volatile("ds_read_b64_tr_b16 %0, %8\n ds_read_b64_tr_b16 %1, %8 offset:%12\n ds_read_b64_tr_b16 %2, %9\n ds_read_b64_tr_b16 %3, %9 offset:%12\n"
+                     "ds_read_b64_tr_b16 %4, %10\n ds_read_b64_tr_b16 %5, %10 offset:%12\n ds_read_b64_tr_b16 %6, %11\n ds_read_b64_tr_b16 %7, %11 offset:%12\n"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]), "=&v"(lo[2]), "=&v"(hi[2]), "=&v"(lo[3]), "=&v"(hi[3])
+                     : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(NEXT) : "memory");
+    } else if constexpr (N == 2) {
+        const uint32_t a0 = at[0] + off, a1 = at[1] + off;
+        asm volatile("ds_read_b64_tr_b16 %0, %4\n ds_read_b64_tr_b16 %1, %4 offset:%6\n ds_read_b64_tr_b16 %2, %5\n ds_read_b64_tr_b16 %3, %5 offset:%6\n"
+                     "s_waitcnt lgkmcnt(0)"
+                     : "=&v"(lo[0]), "=&v"(hi[0]), "=&v"(lo[1]), "=&v"(hi[1]) : "v"(a0), "v"(a1), "n"(NEXT) : "memory");
+    } else {
+        const uint32_t a0 = at[0] + off;
+        asm volatile("ds_read_b64_tr_b16 %0, %2\n ds_read_b64_tr_b16 %1, %2 offset:%3\n s_waitcnt lgkmcnt(0)"
+                     : "=&v"(lo[0]), "=&v"(hi[0]) : "v"(a0), "n"(NEXT) : "memory");
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) f[i] = u32x4_t{lo[i][0], lo[i][1], hi[i][0], hi[i][1]};
+}
 
 template <int NRF, int NCF>
 __global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams p, GradParams g) {
     using G = GradTile<NRF, NCF>;
     __shared__ __attribute__((aligned(512))) char smem[G::kLds];
+    __shared__ int32_t s_tok[G::kList];
     const int tid = threadIdx.x;
-    int id = blockIdx.x;
-    const int of = g.n * g.col_tiles[0], which = id < of ? 0 : 1;
-    if (which) id -= of;
-    const int ct = id % g.col_tiles[which], a = id / g.col_tiles[which];
+    // every XCD a run of the column tiles, adapter by adapter: its workgroups share one adapter's h in their L2, however unlike the adapters are
+    const int tiles = g.col_tiles[0] + g.col_tiles[1], per = (tiles + 7) >> 3, slot = blockIdx.x >> 3, a = slot / per;
+    int ct = (blockIdx.x & 7) * per + slot % per;
+    if (ct >= tiles) return;
+    const int which = ct < g.col_tiles[0] ? 0 : 1;
+    if (which) ct -= g.col_tiles[0];
     const int W = g.W[which], c0 = ct * 32 * NCF, r = g.r;
     const int row0 = p.plan.start[a], count = p.plan.start[a + 1] - row0;
-    const int32_t* order = p.plan.order + row0;
-    const int nst = (count + BK - 1) / BK;
-    const char* x = g.x[which];
+    const Lane ln;
+    const int wave = ln.wave_uniform();
+    // x: an instruction moves kXRows rows of kXLanes lanes
+    constexpr int kXLanes = 4 * NCF, kXRows = 64 / kXLanes, kHLanes = 4 * NRF, kHRows = 64 / kHLanes;
+    const int xk = kXRows * G::kXLoads * wave + ln.l / kXLanes;                                  // (+ kXRows i)
+    const int xc = (ln.l % kXLanes) ^ ks_swz<G::kXRow>(ln.l / kXLanes);                          // (kXRows is 4 or 8: it does not depend on i)
+    const char* const x = g.x[which] + (size_t)min(c0 + 8 * xc, W - 8) * 2;
     const size_t ldx = g.ldx[which];
-    const float* h = g.h[which];
-    constexpr int kLanes = 4 * NCF;              // lanes of an x row
-    const int xk = tid / kLanes, xc = tid % kLanes, xcol = min(c0 + 8 * xc, W - 8);
-    constexpr int kStep = kSmallThreads / kLanes;
-    const int hw = r / 8;                        // units of a row of h
-    u32x4_t rx[G::kXLoads];
-    f32x4_t rh[G::kHUnits][2];
-    // rows at and past `count` are zeros on both sides
-    auto load = [&](int s) {
+    const char* const h = (const char*)(p.terms[which] + (size_t)row0 * 3 * r);
+    const uint32_t tok0 = lds_addr(s_tok) + xk * 4;
+    auto issue = [&](int k0, int left, char* dst) {   // the 64 rows from row k0 of the list on, of which `left` are there
+        int32_t tok[G::kXLoads];
 #pragma unroll
-        for (int i = 0; i < G::kXLoads; ++i) {
-            const int k = s * BK + xk + i * kStep;
-            const int t = order[min(k, count - 1)];
-            rx[i] = *(const u32x4_t*)(x + (size_t)t * ldx + (size_t)xcol * 2);
-            if (k >= count) rx[i] = zero4();
+        for (int i = 0; i < G::kXLoads; ++i)
+            asm volatile("ds_read_b32 %0, %1 offset:%2\n s_waitcnt lgkmcnt(0)" : "=v"(tok[i]) : "v"(tok0 + (k0 % G::kList) * 4), "n"(i * kXRows * 4) : "memory");
+        const char* q[G::kXLoads + G::kHLoads];
+#pragma unroll
+        for (int i = 0; i < G::kXLoads; ++i) q[i] = xk + i * kXRows < left ? x + (size_t)tok[i] * ldx : zero_chunk();
+#pragma unroll
+        for (int i = 0; i < G::kHLoads; ++i) {
+            const int u = G::kHLoads * wave + i, term = u / (4 * NRF), k = (u % (4 * NRF)) * kHRows + ln.l / kHLanes;
+            const int c = (ln.l % kHLanes) ^ ks_swz<G::kHRow>(k);
+            q[G::kXLoads + i] = k < left ? h + ((size_t)(k0 + k) * 3 + term) * r * 2 + min(c * 16, 2 * r - 16) : zero_chunk();
         }
 #pragma unroll
-        for (int i = 0; i < G::kHUnits; ++i) {
-            const int u = tid + i * kSmallThreads, k = u / hw, j = u - k * hw;
-            if (k < BK) {
-                const int row = s * BK + k, t = order[min(row, count - 1)];
-                const f32x4_t* q = (const f32x4_t*)(h + (size_t)t * r + 8 * j);
-                rh[i][0] = q[0];
-                rh[i][1] = q[1];
-                if (row >= count) rh[i][0] = rh[i][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-            }
-        }
-    };
-    auto put = [&](int image) {
-        char* base = smem + image * G::kStage;
+        for (int i = 0; i < G::kXLoads + G::kHLoads; ++i) asm volatile("" : "+v"(q[i]));
 #pragma unroll
-        for (int i = 0; i < G::kXLoads; ++i) {
-            const int k = xk + i * kStep;
-            *(u32x4_t*)(base + k * G::kXRow + ((xc ^ ks_swz<G::kXRow>(k)) << 4)) = rx[i];
-        }
+        for (int i = 0; i < G::kXLoads; ++i) dma16(q[i], dst + (G::kXLoads * wave + i) * 1024);
 #pragma unroll
-        for (int i = 0; i < G::kHUnits; ++i) {
-            const int u = tid + i * kSmallThreads, k = u / hw, j = u - k * hw;
-            if (k < BK) {
-                float v[8], e[8];
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    v[q] = rh[i][0][q];
-                    v[4 + q] = rh[i][1][q];
-                }
-                char* at = base + G::kX + k * G::kHRow + ((j ^ ks_swz<G::kHRow>(k)) << 4);
-#pragma unroll
-                for (int term = 0; term < 3; ++term) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) e[q] = bf16_round(v[q]);
-                    *(u32x4_t*)(at + term * G::kH) = pack8f(e);
-#pragma unroll
-                    for (int q = 0; q < 8; ++q) v[q] = fabsf(e[q]) < INFINITY ? v[q] - e[q] : 0.f;
-                }
-            }
-        }
+        for (int i = 0; i < G::kHLoads; ++i) dma16(q[G::kXLoads + i], dst + G::kX + (G::kHLoads * wave + i) * 1024);
     };
     f32x16_t acc[NRF][NCF];
 #pragma unroll
@@ -832,32 +873,47 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams 
         for (int af = 0; af < NCF; ++af)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[tf][af][v] = 0.f;
-    const Lane ln;
-    const int gg = (ln.l >> 4) & 1, e = (ln.l & 15) >> 2, q = ln.l & 3, sq = ((q & 1) << 1) | (q >> 1), krow = 16 * ln.w + 8 * ln.hf + e;
-    if (nst > 0) load(0);
-    for (int s = 0; s < nst; ++s) {
-        put(s & 1);
-        if (s + 1 < nst) load(s + 1);
+    // fragments: x columns in the A role, ranks in the B role
+    const int gg = (ln.l >> 4) & 1, e = (ln.l & 15) >> 2, q4 = ln.l & 3, sq = ((q4 & 1) << 1) | (q4 >> 1), krow = 16 * wave + 8 * ln.hf + e;
+    uint32_t ax[NCF], ah[NRF];
+#pragma unroll
+    for (int af = 0; af < NCF; ++af)
+        ax[af] = lds_addr(smem) + krow * G::kXRow + (((4 * af + 2 * gg + (sq >> 1)) ^ ks_swz<G::kXRow>(e)) << 4) + (sq & 1) * 8;
+#pragma unroll
+    for (int tf = 0; tf < NRF; ++tf)
+        ah[tf] = lds_addr(smem) + G::kX + krow * G::kHRow + (((4 * tf + 2 * gg + (q4 >> 1)) ^ ks_swz<G::kHRow>(e)) << 4) + (q4 & 1) * 8;
+    for (int base = 0; base < count; base += G::kList) {
+        const int here = min(G::kList, count - base), nst = (here + BK - 1) / BK;
+        __syncthreads();   // the list before has been read
+        for (int i = tid; i < here; i += kSmallThreads) s_tok[i] = p.plan.order[row0 + base + i];
         __syncthreads();
-        const lds_ptr3_t base = (lds_ptr3_t)smem + (s & 1) * G::kStage;
-        auto read = [&](lds_ptr3_t at, int row_bytes) {
-            const bf16x4v_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_tr3_t)at);
-            const bf16x4v_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4bf16((lds_tr3_t)(at + 4 * row_bytes));
-            return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
-        };
-        bf16x8_t fx[NCF];
 #pragma unroll
-        for (int af = 0; af < NCF; ++af)
-            fx[af] = read(base + krow * G::kXRow + (((4 * af + 2 * gg + (sq >> 1)) ^ ks_swz<G::kXRow>(e)) << 4) + (sq & 1) * 8, G::kXRow);
-#pragma unroll
-        for (int term = 0; term < 3; ++term)
-#pragma unroll
-            for (int tf = 0; tf < NRF; ++tf) {
-                const bf16x8_t fh = read(base + G::kX + term * G::kH + krow * G::kHRow + (((4 * tf + 2 * gg + (q >> 1)) ^ ks_swz<G::kHRow>(e)) << 4) + (q & 1) * 8,
-                                         G::kHRow);
-#pragma unroll
-                for (int af = 0; af < NCF; ++af) acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fx[af], fh, acc[tf][af], 0, 0, 0);
+        for (int t = 0; t < G::kDepth - 1; ++t)
+            if (t < nst) issue(base + t * BK, here - t * BK, smem + t * G::kStage);
+        int at = 0, next = (G::kDepth - 1) * G::kStage;
+        for (int t = 0; t < nst; ++t) {
+            if (t + G::kDepth - 2 < nst) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((G::kDepth - 2) * (G::kXLoads + G::kHLoads)) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            if (t + G::kDepth - 1 < nst) {
+                issue(base + (t + G::kDepth - 1) * BK, here - (t + G::kDepth - 1) * BK, smem + next);
+                next = next == (G::kDepth - 1) * G::kStage ? 0 : next + G::kStage;
             }
+            u32x4_t fx[NCF];
+            read_tr<NCF, 4 * G::kXRow>(fx, ax, at);
+#pragma unroll
+            for (int term = 0; term < 3; ++term) {
+                u32x4_t fh[NRF];
+                read_tr<NRF, 4 * G::kHRow>(fh, ah, at + term * G::kH);
+#pragma unroll
+                for (int tf = 0; tf < NRF; ++tf)
+#pragma unroll
+                    for (int af = 0; af < NCF; ++af)
+                        acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[af]), __builtin_bit_cast(bf16x8_t, fh[tf]),
+                                                                              acc[tf][af], 0, 0, 0);
+            }
+            at = at == (G::kDepth - 1) * G::kStage ? 0 : at + G::kStage;
+        }
     }
 #pragma unroll
     for (int tf = 0; tf < NRF; ++tf) {
@@ -910,7 +966,8 @@ static int tile_rows_of(int T, int C) {
 }
 static size_t many_bytes(const moe_adapter_shape_t& s) {
     const size_t hx = std::max(hx_bytes(s, tile_rows_of(s.T, s.N)), hx_bytes(s, tile_rows_of(s.T, s.K)));
-    return align_up(hx, 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256);
+    return align_up(hx, 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256) +
+           2 * align_up((size_t)s.T * s.rank * 6, 256);
 }
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
     if (s.T == 0) return 256;
@@ -937,16 +994,24 @@ template <int FORM>
 static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
     p.plan = plan_view(s, plan);
     p.tile_rows = tile_rows_of(p.T, p.C);
-    p.blocks = (int)plan_blocks(s);
+    p.blocks = ((int)plan_blocks(s) + 7) & ~7;
     const size_t hx = std::max(hx_bytes(s, tile_rows_of(s.T, s.N)), hx_bytes(s, tile_rows_of(s.T, s.K)));
     p.hx = ws;
     char* rest = ws + align_up(hx, 256);
     if (!p.h) p.h = (float*)rest;
     p.second_t = rest + align_up((size_t)s.T * s.rank * 4, 256);
     const dim3 low((unsigned)(p.blocks + (FORM == kKc ? p.n * ((p.C + 63) / 64) : 0)));
-    if (p.r <= 32) hipLaunchKernelGGL((adapter_low_kernel<1>), low, dim3(kSmallThreads), 0, st, p);
-    else if (p.r <= 64) hipLaunchKernelGGL((adapter_low_kernel<2>), low, dim3(kSmallThreads), 0, st, p);
-    else hipLaunchKernelGGL((adapter_low_kernel<4>), low, dim3(kSmallThreads), 0, st, p);
+    if (FORM == kKc) {
+        p.terms[0] = (uint16_t*)(p.second_t + align_up((size_t)s.adapters * s.K * s.rank * 2, 256));
+        p.terms[1] = (uint16_t*)((char*)p.terms[0] + align_up((size_t)s.T * s.rank * 6, 256));
+    }
+    auto low_launch = [&](auto nrf) {
+        if (p.r <= 32) hipLaunchKernelGGL((adapter_low_kernel<nrf.value, 1>), low, dim3(kSmallThreads), 0, st, p);
+        else if (p.r <= 64) hipLaunchKernelGGL((adapter_low_kernel<nrf.value, 2>), low, dim3(kSmallThreads), 0, st, p);
+        else hipLaunchKernelGGL((adapter_low_kernel<nrf.value, 4>), low, dim3(kSmallThreads), 0, st, p);
+    };
+    if (block_rows(p.T) == 64) low_launch(std::integral_constant<int, 2>{});
+    else low_launch(std::integral_constant<int, 1>{});
     const int cols = p.tile_rows == 64 ? 64 : BN;
     p.row_tiles = (p.T + p.tile_rows - 1) / p.tile_rows;
     p.col_tiles = (p.C + cols - 1) / cols;
@@ -998,11 +1063,11 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         hipLaunchKernelGGL(adapter_few_second_grad_kernel, dim3((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st,
                            p, g, joins);
     } else {
+        p.h_given = h;
         many_launch<kKc>(p, s, plan, ws, st);
-        g.h[1] = p.h;
         const int cols = p.r > 64 ? 64 : 128;
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
-        const dim3 grid((unsigned)(g.n * (g.col_tiles[0] + g.col_tiles[1])));
+        const dim3 grid((unsigned)(8 * g.n * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)));
         if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kSmallThreads), 0, st, p, g);
         else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kSmallThreads), 0, st, p, g);
         else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kSmallThreads), 0, st, p, g);

@@ -145,14 +145,16 @@ struct KsStages : PlainLoader<KsStages<NI, TC>> {
 // ------------------------------------------------------------------ small tiles
 // 4 waves, 32 NRF rows by 32 NCF columns.  Every wave has the whole tile in its accumulators and takes one of a stage's four k-sub-steps: a wave with a
 // quarter of the tile instead would read each operand's fragments twice, and the LDS is what a small tile is bound by.  The four
-// sums are added at the end, wave 0 first.  Four stage buffers, three on their way; one barrier a stage.
+// sums are added at the end, wave 0 first.  kDepth stage buffers, all but one on their way; one barrier a stage.  As many buffers as leave
+// room for two workgroups on a CU: what a CU draws from memory is what it has on its way over a latency (the low-rank part of 8192 tokens 7168 wide,
+// a workgroup a CU, with four buffers of 8 KB 28 us).
 constexpr int kSmallThreads = 256;
-constexpr int kSmallDepth = 4;
 template <int NRF, int NCF>
 struct SmallTile {
     static constexpr int kRowsBytes = 4096 * NRF, kStage = 4096 * (NRF + NCF);
+    static constexpr int kDepth = NRF + NCF == 2 ? 8 : NRF + NCF == 3 ? 6 : 4;
     static constexpr int kSums = 16384 * NRF * NCF;   // 4 waves, fp32
-    static constexpr int kLds = kSmallDepth * kStage > kSums ? kSmallDepth * kStage : kSums;
+    static constexpr int kLds = kDepth * kStage > kSums ? kDepth * kStage : kSums;
 };
 
 template <int NRF, int NCF, int FORM>
@@ -190,6 +192,13 @@ struct SmallFrags {
                 asm volatile("ds_read_b128 %0, %5\n ds_read_b128 %1, %6\n ds_read_b128 %2, %6 offset:4096\n ds_read_b128 %3, %6 offset:8192\n"
                              "ds_read_b128 %4, %6 offset:12288\n s_waitcnt lgkmcnt(0)"
                              : "=&v"(rb[0]), "=&v"(ra[0]), "=&v"(ra[1]), "=&v"(ra[2]), "=&v"(ra[3]) : "v"(bo), "v"(ao) : "memory");
+            else if constexpr (NRF == 2 && NCF == 1)
+                asm volatile("ds_read_b128 %0, %3\n ds_read_b128 %1, %3 offset:4096\n ds_read_b128 %2, %4\n"
+                             "s_waitcnt lgkmcnt(0)" : "=&v"(rb[0]), "=&v"(rb[1]), "=&v"(ra[0]) : "v"(bo), "v"(ao) : "memory");
+            else if constexpr (NRF == 2 && NCF == 4)
+                asm volatile("ds_read_b128 %0, %6\n ds_read_b128 %1, %6 offset:4096\n ds_read_b128 %2, %7\n ds_read_b128 %3, %7 offset:4096\n"
+                             "ds_read_b128 %4, %7 offset:8192\n ds_read_b128 %5, %7 offset:12288\n s_waitcnt lgkmcnt(0)"
+                             : "=&v"(rb[0]), "=&v"(rb[1]), "=&v"(ra[0]), "=&v"(ra[1]), "=&v"(ra[2]), "=&v"(ra[3]) : "v"(bo), "v"(ao) : "memory");
             else {
                 static_assert(NRF == 1 && NCF == 1, "");
                 asm volatile("ds_read_b128 %0, %2\n ds_read_b128 %1, %3\n s_waitcnt lgkmcnt(0)" : "=&v"(rb[0]), "=&v"(ra[0]) : "v"(bo), "v"(ao) : "memory");
@@ -217,7 +226,7 @@ struct SmallFrags {
 template <int NRF, int NCF, int FORM, class LB, class LA>
 __device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f32x16_t (&acc)[NRF][NCF]) {
     using S = SmallTile<NRF, NCF>;
-    constexpr int kRequests = NRF + NCF;   // of a wave, a stage
+    constexpr int kRequests = NRF + NCF, kDepth = S::kDepth;   // requests of a wave, a stage
     const Lane ln;
     const SmallFrags<NRF, NCF, FORM> fr(ln, lds_addr(smem));
 #pragma unroll
@@ -227,23 +236,25 @@ __device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[tf][af][v] = 0.f;
 #pragma unroll
-    for (int t = 0; t < kSmallDepth - 1; ++t)
+    for (int t = 0; t < kDepth - 1; ++t)
         if (t < nk) {
             lb.issue(smem + t * S::kStage);
             la.issue(smem + t * S::kStage + S::kRowsBytes);
         }
+    int at = 0, next = (kDepth - 1) * S::kStage;   // buffers of stages t and t + kDepth - 1
     for (int t = 0; t < nk; ++t) {
         // stage t is here when at most those behind it are on their way
-        if (t + kSmallDepth - 2 < nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kSmallDepth - 2) * kRequests) : "memory");
+        if (t + kDepth - 2 < nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kDepth - 2) * kRequests) : "memory");
         else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
-        if (t + kSmallDepth - 1 < nk) {   // into the buffer that every wave has read before the barrier
-            char* d = smem + ((t + kSmallDepth - 1) % kSmallDepth) * S::kStage;
-            lb.issue(d);
-            la.issue(d + S::kRowsBytes);
+        if (t + kDepth - 1 < nk) {   // into the buffer that every wave has read before the barrier
+            lb.issue(smem + next);
+            la.issue(smem + next + S::kRowsBytes);
+            next = next == (kDepth - 1) * S::kStage ? 0 : next + S::kStage;
         }
         u32x4_t rb[NRF], ra[NCF];
-        fr.read((t % kSmallDepth) * S::kStage, rb, ra);
+        fr.read(at, rb, ra);
+        at = at == (kDepth - 1) * S::kStage ? 0 : at + S::kStage;
 #pragma unroll
         for (int tf = 0; tf < NRF; ++tf)
 #pragma unroll

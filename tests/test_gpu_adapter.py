@@ -34,6 +34,7 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     # tiles of 128 and of 256 rows, in each direction
     (4100, 136, 1032, 16, 9, "packed", 0, "bf16"), (4100, 1032, 72, 16, 300, "scattered", 0, "bf16"), (8200, 72, 1544, 24, 6, "scattered", 8, "bf16"),
     (8200, 1544, 136, 64, 5, "packed", 0, "f32"), (16500, 584, 1032, 8, 40, "scattered", 0, "f32"), (16500, 1032, 584, 128, 3, "packed", 0, "bf16"),
+    (16500, 136, 72, 48, 7, "scattered", 0, "bf16"),
 ]
 
 
