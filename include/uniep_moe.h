@@ -287,7 +287,7 @@ typedef struct {
     int32_t adapters;
 } moe_adapter_shape_t;
 
-/* Workspace of the forward and of the backward call, and bytes of the plan (host outputs; either may be NULL).  The plan of up to 256
+/* Workspace of the forward and of the backward call, and bytes of the plan (host outputs; either may be NULL).  The plan of up to 512
  * tokens has 0 bytes: moe_adapter_plan then enqueues nothing, and `plan` may be NULL everywhere. */
 int moe_adapter_workspace_bytes(const moe_adapter_shape_t* shape, size_t* ws_bytes, size_t* plan_bytes);
 

@@ -18,7 +18,8 @@
 
 namespace uniep {
 
-constexpr int kFewTokens = 256;
+constexpr int kFewTokens = 512;
+constexpr int kFewWords = kFewTokens / 64;
 // Rows of a block of the plan: as many tokens of one adapter share the fetch of its first factor.
 static int block_rows(int T) { return T >= 16384 ? 64 : 32; }
 constexpr int kUnit = 64;             // rows of which the plan knows the first and the last segment
@@ -216,37 +217,95 @@ __device__ __forceinline__ int adapter_of(const int32_t* ids, int t, int n) {
 __device__ __forceinline__ Stages stages_of(int R) { return Stages{R / BK, R % BK}; }
 
 // ------------------------------------------------------------------ few tokens
-// Which tokens have adapter `a`: bit t of the four words.  256 threads, two barriers.
+// Which tokens have adapter `a`: a bit each, in scalar registers.  256 threads, two barriers.
 struct Members {
-    uint64_t m[4];
+    uint64_t m[kFewWords];
     __device__ __forceinline__ void find(int T, int n, const int32_t* ids, int a, uint64_t* s_mask) {
         const int tid = threadIdx.x;
-        const uint64_t b = __ballot(tid < T && adapter_of(ids, tid < T ? tid : 0, n) == a);
-        if ((tid & 63) == 0) s_mask[tid >> 6] = b;
+#pragma unroll
+        for (int i = 0; i < kFewWords / 4; ++i) {
+            const int t = tid + 256 * i;
+            const uint64_t b = __ballot(t < T && adapter_of(ids, t < T ? t : 0, n) == a);
+            if ((tid & 63) == 0) s_mask[4 * i + (tid >> 6)] = b;
+        }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) m[i] = s_mask[i];
+        for (int i = 0; i < kFewWords; ++i) {
+            const uint64_t b = s_mask[i];
+            m[i] = (uint64_t)(uint32_t)rfl((int)(b >> 32)) << 32 | (uint32_t)rfl((int)b);
+        }
     }
-    __device__ __forceinline__ int before(int t) const {
+    __device__ __forceinline__ int before(int t) const {   // t the same in all threads
         int c = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = t - 64 * i;
-            c += __popcll(k <= 0 ? 0ull : k >= 64 ? m[i] : m[i] & ((1ull << k) - 1ull));
-        }
+        for (int i = 0; i < kFewWords; ++i) c += __popcll(64 * i + 64 <= t ? m[i] : 64 * i >= t ? 0ull : m[i] & ((1ull << (t & 63)) - 1ull));
         return c;
     }
-    __device__ __forceinline__ int count() const { return before(256); }
-};
-// The tokens from the `skip`-th member on, up to `most`, in list[]; ends with a barrier.
-__device__ __forceinline__ void list_members(const Members& mb, int skip, int most, int32_t* list) {
-    const int tid = threadIdx.x, w = tid >> 6;
-    const uint64_t mine = w == 0 ? mb.m[0] : w == 1 ? mb.m[1] : w == 2 ? mb.m[2] : mb.m[3];
-    if ((mine >> (tid & 63)) & 1) {
-        const int k = mb.before(tid) - skip;
-        if (k >= 0 && k < most) list[k] = tid;
+    __device__ __forceinline__ int count() const { return before(kFewTokens); }
+    // the tokens from the `skip`-th on, up to `most`, into list[]; ends with a barrier
+    __device__ __forceinline__ void list(int skip, int most, int32_t* list) const {
+        const int w = rfl(threadIdx.x >> 6), lane = threadIdx.x & 63;
+#pragma unroll
+        for (int i = 0; i < kFewWords / 4; ++i) {
+            uint64_t mine = 0;
+            int k = -skip;
+#pragma unroll
+            for (int q = 0; q < kFewWords; ++q) {
+                if (q < 4 * i + w) k += __popcll(m[q]);
+                if (q == 4 * i + w) mine = m[q];
+            }
+            k += __builtin_amdgcn_mbcnt_hi((uint32_t)(mine >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mine, 0));
+            if (((mine >> lane) & 1) && k >= 0 && k < most) list[k] = 64 * (4 * i + w) + lane;
+        }
+        __syncthreads();
     }
-    __syncthreads();
+};
+
+// Ranks [j0, j1) of h for up to 4 tokens over [k0, k1) of the reduction, by dot products: wave w has every fourth rank, its lanes 8 elements of 512 each.  For so
+// few tokens the tile of 32 rows by 64 ranks that is used for more moves ten times the bytes (256 tokens of 256 adapters, 8 ranks of 2048: 19 us, with dots
+// FIRST us).
+constexpr int kDotTokens = 4;
+__device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int j1, int rows, const int32_t* list, int k0, int k1, float* out) {
+    constexpr int kRanks = 4;   // of a wave, at a time
+    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+    for (int j = j0 + w; j < j1; j += 4 * kRanks) {
+        const char* const f = p.first + ((size_t)a * p.r + j) * p.R * 2;
+        float acc[kRanks][kDotTokens] = {};
+        for (int kk = k0 + 8 * lane; kk < k1; kk += 1024) {
+            u32x4_t b[2][kRanks], x[2][kDotTokens];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {   // (loads first: two runs of k are on their way together)
+                const int k = kk + 512 * h;
+#pragma unroll
+                for (int i = 0; i < kRanks; ++i) {
+                    b[h][i] = zero4();
+                    if (k < k1 && j + 4 * i < j1) b[h][i] = *(const u32x4_t*)(f + ((size_t)(4 * i) * p.R + k) * 2);
+                }
+#pragma unroll
+                for (int m = 0; m < kDotTokens; ++m) {
+                    x[h][m] = zero4();
+                    if (k < k1 && m < rows) x[h][m] = *(const u32x4_t*)(p.x + (size_t)list[m] * p.ldx + (size_t)k * 2);
+                }
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int m = 0; m < kDotTokens; ++m)
+                    if (m < rows)
+#pragma unroll
+                        for (int i = 0; i < kRanks; ++i)
+#pragma unroll
+                            for (int q = 0; q < 4; ++q) acc[i][m] += bf16_lo(x[h][m][q]) * bf16_lo(b[h][i][q]) + bf16_hi(x[h][m][q]) * bf16_hi(b[h][i][q]);
+        }
+#pragma unroll
+        for (int i = 0; i < kRanks; ++i)
+#pragma unroll
+            for (int m = 0; m < kDotTokens; ++m)
+                if (m < rows && j + 4 * i < j1) {
+                    across<64>(acc[i][m], [](float u, float v) { return u + v; });
+                    if (lane == 0) out[(size_t)list[m] * p.r + j + 4 * i] = acc[i][m];
+                }
+    }
 }
 
 // Parts of x W and of h.  Tasks: (column tile, split, row tile), then (token, rank tile, split): a workgroup whose token is not every
@@ -255,7 +314,7 @@ template <int NRF, int FORM>
 __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjParams p) {
     constexpr int kLds = SmallTile<NRF, 2>::kLds > SmallTile<1, 2>::kLds ? SmallTile<NRF, 2>::kLds : SmallTile<1, 2>::kLds;   // (h: 32 rows)
     __shared__ __attribute__((aligned(512))) char smem[kLds];
-    __shared__ uint64_t s_mask[4];
+    __shared__ uint64_t s_mask[kFewWords];
     __shared__ int32_t s_list[32];
     const Stages all = stages_of(p.R);
     const int nst = all.full + (all.tail > 0);
@@ -300,9 +359,13 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
     mb.find(p.T, p.n, p.ids, a, s_mask);
     const int rank = mb.before(t);
     if (rank % 32 != 0) return;
-    list_members(mb, rank, 32, s_list);
+    mb.list(rank, 32, s_list);
     const int rows = min(32, mb.count() - rank);
     const int s0 = sp * p.hper_split, s1 = min(nst, s0 + p.hper_split);
+    if (rank == 0 && rows <= kDotTokens) {
+        few_dots(p, a, 64 * rt, min(p.r, 64 * rt + 64), rows, s_list, s0 * BK, min(p.R, s1 * BK), p.hpart + (size_t)sp * p.T * p.r);
+        return;
+    }
     const Stages st = part_of(s0, s1);
     f32x16_t acc[1][2];
     {
@@ -326,6 +389,7 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
 // s h[t][j] from its parts
 __device__ __forceinline__ float whole_h(const ProjParams& p, int t, int j, float s) {
     float v = 0.f;
+#pragma unroll 8
     for (int k = 0; k < p.hsplits; ++k) v += p.hpart[((size_t)k * p.T + t) * p.r + j];
     return v * s;
 }
@@ -337,78 +401,97 @@ __device__ __forceinline__ void fma8(float (&acc)[8], float h, u32x4_t b) {
     }
 }
 
-// y of up to 4 tokens with one adapter and 512 columns: the waves share the parts and the ranks, and their sums are added in LDS.
-constexpr int kJoinTokens = 4, kJoinCols = 512;
+// y of G tokens with one adapter (the last group may have fewer) and 1024 columns, 4 a lane.  (Waves that shared 512 columns and their sums in LDS
+// took 11.6 us for 256 tokens of 256 adapters, 8 ranks of 4096 columns each.)
+constexpr int kJoinCols = 1024;
+template <int G>
 struct JoinShared {
-    float h[kJoinTokens][kMaxRank];
-    float sums[4][kJoinTokens][kJoinCols];
-    uint64_t mask[4];
-    int32_t list[kJoinTokens];
+    float h[G][kMaxRank];
+    uint64_t mask[kFewWords];
+    int32_t list[G];
 };
-__device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, JoinShared& S) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int a = adapter_of(p.ids, t, p.n);
-    Members mb;
-    mb.find(p.T, p.n, p.ids, a, S.mask);
-    const int rank = mb.before(t);
-    if (rank % kJoinTokens != 0) return;
-    list_members(mb, rank, kJoinTokens, S.list);
-    const int rows = min(kJoinTokens, mb.count() - rank);
+__device__ __forceinline__ void fma4(float (&acc)[4], float h, u32x2_t b) {
+    acc[0] += h * bf16_lo(b[0]);
+    acc[1] += h * bf16_hi(b[0]);
+    acc[2] += h * bf16_lo(b[1]);
+    acc[3] += h * bf16_hi(b[1]);
+}
+template <int G>
+__device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, JoinShared<G>& S) {
+    const int tid = threadIdx.x;
+    const int a = rfl(adapter_of(p.ids, t, p.n));
+    int rows = 1;
+    if (G > 1) {
+        Members mb;
+        mb.find(p.T, p.n, p.ids, a, S.mask);
+        const int rank = mb.before(t);
+        if (rank % G != 0) return;
+        mb.list(rank, G, S.list);
+        rows = min(G, mb.count() - rank);
+    }
+    auto token = [&](int m) { return G == 1 ? t : S.list[m]; };
+    const int c = cb * kJoinCols + 4 * tid;
+    const bool works = c < p.C;
+    const char* const f = p.second + ((size_t)max(a, 0) * p.r * p.C + c) * 2;
+    const float* const part = p.part + c;
+    // the first loads of everything are on their way together: this kernel is what its dependent loads take
+    constexpr int kPreB = 8, kPreP = 4;
+    u32x2_t b[kPreB];
+    f32x4_t q[kPreP];
+#pragma unroll
+    for (int i = 0; i < kPreB; ++i) {
+        b[i] = u32x2_t{0u, 0u};
+        if (works && a >= 0) b[i] = *(const u32x2_t*)(f + (size_t)i * p.C * 2);   // (there are at least 8 ranks)
+    }
+#pragma unroll
+    for (int i = 0; i < kPreP; ++i) {
+        q[i] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+        if (works && i < p.splits) q[i] = *(const f32x4_t*)(part + ((size_t)i * p.T + t) * p.C);
+    }
     if (a >= 0 || p.h) {
         const float s = a < 0 ? 0.f : p.scale ? p.scale[a] : 1.f;
         for (int i = tid; i < rows * p.r; i += 256) {
-            const int m = i / p.r, j = i - m * p.r, tok = S.list[m];
+            const int m = G == 1 ? 0 : i / p.r, j = i - m * p.r, tok = token(m);
             const float v = a < 0 ? 0.f : whole_h(p, tok, j, s);
             S.h[m][j] = v;
             if (p.h && cb == 0) p.h[(size_t)tok * p.r + j] = v;
         }
         __syncthreads();
     }
-    const int c = cb * kJoinCols + 8 * lane;
-    float acc[kJoinTokens][8] = {};
-    if (c < p.C) {
-        for (int s = w; s < p.splits; s += 4)
+    if (!works) return;
+    float acc[G][4] = {};
 #pragma unroll
-            for (int m = 0; m < kJoinTokens; ++m)
-                if (m < rows) {
-                    const f32x4_t* q = (const f32x4_t*)(p.part + ((size_t)s * p.T + S.list[m]) * p.C + c);
-                    const f32x4_t u = q[0], v = q[1];
+    for (int i = 0; i < kPreP; ++i)
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        acc[m][j] += u[j];
-                        acc[m][4 + j] += v[j];
-                    }
-                }
-        if (a >= 0) {
-            const char* f = p.second + ((size_t)a * p.r * p.C + c) * 2;
+        for (int j = 0; j < 4; ++j) acc[0][j] += q[i][j];
+#pragma unroll
+    for (int m = 0; m < G; ++m)
+        if (m < rows)
 #pragma unroll 4
-            for (int j = w; j < p.r; j += 4) {
-                const u32x4_t b = *(const u32x4_t*)(f + (size_t)j * p.C * 2);
+            for (int s = m == 0 ? kPreP : 0; s < p.splits; ++s) {
+                const f32x4_t u = *(const f32x4_t*)(part + ((size_t)s * p.T + token(m)) * p.C);
 #pragma unroll
-                for (int m = 0; m < kJoinTokens; ++m)
-                    if (m < rows) fma8(acc[m], S.h[m][j], b);
+                for (int j = 0; j < 4; ++j) acc[m][j] += u[j];
             }
+    if (a >= 0) {
+#pragma unroll
+        for (int i = 0; i < kPreB; ++i)
+#pragma unroll
+            for (int m = 0; m < G; ++m) fma4(acc[m], S.h[m][i], b[i]);   // (rows that are not there: never stored)
+#pragma unroll 8
+        for (int j = kPreB; j < p.r; ++j) {
+            const u32x2_t x = *(const u32x2_t*)(f + (size_t)j * p.C * 2);
+#pragma unroll
+            for (int m = 0; m < G; ++m) fma4(acc[m], S.h[m][j], x);
         }
-#pragma unroll
-        for (int m = 0; m < kJoinTokens; ++m)
-            if (m < rows) {
-                *(f32x4_t*)&S.sums[w][m][8 * lane] = f32x4_t{acc[m][0], acc[m][1], acc[m][2], acc[m][3]};
-                *(f32x4_t*)&S.sums[w][m][8 * lane + 4] = f32x4_t{acc[m][4], acc[m][5], acc[m][6], acc[m][7]};
-            }
     }
-    __syncthreads();
-    if (w >= rows || c >= p.C) return;
-    float v[8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = ((S.sums[0][w][8 * lane + j] + S.sums[1][w][8 * lane + j]) + S.sums[2][w][8 * lane + j]) + S.sums[3][w][8 * lane + j];
-    const size_t at = (size_t)S.list[w] * p.C + c;
-    if (p.out_f32) {
-        f32x4_t* to = (f32x4_t*)(p.y + at * 4);
-        to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
-        to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
-    } else {
-        *(u32x4_t*)(p.y + at * 2) = pack8f(v);
-    }
+    for (int m = 0; m < G; ++m)
+        if (m < rows) {
+            const size_t at = (size_t)token(m) * p.C + c;
+            if (p.out_f32) *(f32x4_t*)(p.y + at * 4) = f32x4_t{acc[m][0], acc[m][1], acc[m][2], acc[m][3]};
+            else *(u32x2_t*)(p.y + at * 2) = u32x2_t{pack_bf16x2(acc[m][0], acc[m][1]), pack_bf16x2(acc[m][2], acc[m][3])};
+        }
 }
 
 // Gradients of 8 ranks and 256 columns of one adapter, token by token; the waves share the tokens and their sums are added in LDS.  (With 512 columns a
@@ -418,7 +501,7 @@ constexpr int kGradRanks = 8, kGradCols = 256;
 struct FewGradShared {
     float h[kFewTokens][kGradRanks];
     float sums[4][kGradRanks][kGradCols];
-    uint64_t mask[4];
+    uint64_t mask[kFewWords];
     int32_t list[kFewTokens];
 };
 __device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared& S) {
@@ -428,29 +511,47 @@ __device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradPar
     const int cb = id % g.col_tiles[which], rest = id / g.col_tiles[which], a = rest % g.n, j0 = rest / g.n * kGradRanks, W = g.W[which];
     Members mb;
     mb.find(g.T, g.n, p.ids, a, S.mask);
-    list_members(mb, 0, kFewTokens, S.list);
+    mb.list(0, kFewTokens, S.list);
     const int count = mb.count(), c = cb * kGradCols + 4 * lane;
     float acc[kGradRanks][4] = {};
     if (count > 0) {
         const float s = p.scale ? p.scale[a] : 1.f;
-        for (int i = tid; i < count * kGradRanks; i += 256) {
-            const int k = i / kGradRanks, j = i % kGradRanks, tok = S.list[k];
-            S.h[k][j] = g.h[which] ? g.h[which][(size_t)tok * g.r + j0 + j] : whole_h(p, tok, j0 + j, s);
+        // the first rows of x are on their way while h is fetched
+        constexpr int kPre = 8;
+        const char* const x = g.x[which] + (size_t)min(c, W - 4) * 2;
+        u32x2_t pre[kPre];
+#pragma unroll
+        for (int i = 0; i < kPre; ++i) pre[i] = *(const u32x2_t*)(x + (size_t)S.list[min(w + 4 * i, count - 1)] * g.ldx[which]);
+        for (int i = tid; i < 2 * count; i += 256) {   // 4 ranks of a token
+            const int k = i >> 1, j = 4 * (i & 1), tok = S.list[k];
+            f32x4_t v;
+            if (g.h[which]) {
+                v = *(const f32x4_t*)(g.h[which] + (size_t)tok * g.r + j0 + j);
+            } else {
+                v = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+                for (int q = 0; q < p.hsplits; ++q) {
+                    const f32x4_t u = *(const f32x4_t*)(p.hpart + ((size_t)q * p.T + tok) * p.r + j0 + j);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] += u[e];
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] *= s;
+            }
+            *(f32x4_t*)&S.h[k][j] = v;
         }
         __syncthreads();
         if (c < W) {
-            const char* x = g.x[which] + (size_t)c * 2;
+#pragma unroll
+            for (int i = 0; i < kPre; ++i)
+                if (w + 4 * i < count)
+#pragma unroll
+                    for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[w + 4 * i][j], pre[i]);
 #pragma unroll 8
-            for (int k = w; k < count; k += 4) {
+            for (int k = w + 4 * kPre; k < count; k += 4) {
                 const u32x2_t b = *(const u32x2_t*)(x + (size_t)S.list[k] * g.ldx[which]);
 #pragma unroll
-                for (int j = 0; j < kGradRanks; ++j) {
-                    const float h = S.h[k][j];
-                    acc[j][0] += h * bf16_lo(b[0]);
-                    acc[j][1] += h * bf16_hi(b[0]);
-                    acc[j][2] += h * bf16_lo(b[1]);
-                    acc[j][3] += h * bf16_hi(b[1]);
-                }
+                for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[k][j], b);
             }
         }
     }
@@ -472,18 +573,20 @@ __device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradPar
     }
 }
 
+template <int G>
 __global__ void __launch_bounds__(256) adapter_few_second_kernel(ProjParams p) {
-    __shared__ JoinShared S;
-    join_task(p, blockIdx.x % p.T, blockIdx.x / p.T, S);
+    __shared__ JoinShared<G> S;
+    join_task<G>(p, blockIdx.x % p.T, blockIdx.x / p.T, S);
 }
+template <int G>
 __global__ void __launch_bounds__(256) adapter_few_second_grad_kernel(ProjParams p, GradParams g, int joins) {
     union Shared {
-        JoinShared join;
+        JoinShared<G> join;
         FewGradShared grad;
     };
     __shared__ Shared S;
     const int id = blockIdx.x;
-    if (id < joins) join_task(p, id % p.T, id / p.T, S.join);
+    if (id < joins) join_task<G>(p, id % p.T, id / p.T, S.join);
     else few_grad_task(p, g, id - joins, S.grad);
 }
 
@@ -937,7 +1040,7 @@ static int stages_in(int R) { return (R + BK - 1) / BK; }
 struct FewPlan {
     int row_frags, col_tiles, row_tiles, rank_tiles, splits, per_split, hsplits, hper_split;
 };
-// Parts of at least 4 stages, as many as give the chip two workgroups a CU.
+// Parts of at least 4 stages, as many as give every CU a workgroup; h is cut alike, or into fewer parts where every token may be a group of its own.
 static FewPlan few_plan(int T, int R, int C, int r) {
     FewPlan f;
     f.row_frags = T <= 32 ? 1 : 2;
@@ -945,11 +1048,10 @@ static FewPlan few_plan(int T, int R, int C, int r) {
     f.row_tiles = (T + 32 * f.row_frags - 1) / (32 * f.row_frags);
     f.rank_tiles = (r + 63) / 64;
     const int nst = stages_in(R), tiles = f.col_tiles * f.row_tiles;
-    const int want = tiles >= 512 ? 1 : 512 / tiles;
-    f.per_split = (nst + want - 1) / want;
-    if (f.per_split < 4) f.per_split = 4;
+    const int want = std::max(1, 256 / tiles);
+    f.per_split = std::max(4, (nst + want - 1) / want);
     f.splits = (nst + f.per_split - 1) / f.per_split;
-    f.hper_split = 8;
+    f.hper_split = std::max(std::min(f.per_split, 16), (int)(((long long)nst * T * f.rank_tiles + 511) / 512));
     f.hsplits = (nst + f.hper_split - 1) / f.hper_split;
     return f;
 }
@@ -989,6 +1091,8 @@ static void few_first(const ProjParams& p, const FewPlan& f, hipStream_t st) {
     else hipLaunchKernelGGL((adapter_few_first_kernel<2, FORM>), grid, dim3(kSmallThreads), 0, st, p);
 }
 static int few_joins(const ProjParams& p) { return p.T * ((p.C + kJoinCols - 1) / kJoinCols); }
+// Whether tokens of one adapter share the fetch of its second factor in the second launch.
+static bool join_groups(const ProjParams& p) { return (long long)p.T * p.r * p.C > 32 << 20; }
 
 template <int FORM>
 static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
@@ -1031,7 +1135,8 @@ int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t l
         FewPlan f;
         few_params(p, ws, f);
         few_first<kKs>(p, f, st);
-        hipLaunchKernelGGL(adapter_few_second_kernel, dim3((unsigned)few_joins(p)), dim3(256), 0, st, p);
+        if (join_groups(p)) hipLaunchKernelGGL((adapter_few_second_kernel<4>), dim3((unsigned)few_joins(p)), dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((adapter_few_second_kernel<1>), dim3((unsigned)few_joins(p)), dim3(256), 0, st, p);
     } else {
         many_launch<kKs>(p, s, plan, ws, st);
     }
@@ -1060,8 +1165,9 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         const int joins = s.T > 0 ? few_joins(p) : 0;
         g.rank_tiles = g.r / kGradRanks;
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols - 1) / kGradCols;
-        hipLaunchKernelGGL(adapter_few_second_grad_kernel, dim3((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st,
-                           p, g, joins);
+        const dim3 grid((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1])));
+        if (join_groups(p)) hipLaunchKernelGGL((adapter_few_second_grad_kernel<4>), grid, dim3(256), 0, st, p, g, joins);
+        else hipLaunchKernelGGL((adapter_few_second_grad_kernel<1>), grid, dim3(256), 0, st, p, g, joins);
     } else {
         p.h_given = h;
         many_launch<kKc>(p, s, plan, ws, st);

@@ -235,12 +235,12 @@ __device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f
         for (int af = 0; af < NCF; ++af)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[tf][af][v] = 0.f;
-#pragma unroll
-    for (int t = 0; t < kDepth - 1; ++t)
-        if (t < nk) {
-            lb.issue(smem + t * S::kStage);
-            la.issue(smem + t * S::kStage + S::kRowsBytes);
-        }
+    // (one copy of the requests' code: a launch this short waits for its instructions too)
+#pragma unroll 1
+    for (int t = 0; t < min(kDepth - 1, nk); ++t) {
+        lb.issue(smem + t * S::kStage);
+        la.issue(smem + t * S::kStage + S::kRowsBytes);
+    }
     int at = 0, next = (kDepth - 1) * S::kStage;   // buffers of stages t and t + kDepth - 1
     for (int t = 0; t < nk; ++t) {
         // stage t is here when at most those behind it are on their way

@@ -82,6 +82,28 @@ __device__ __forceinline__ void add_relaxed(int* p, int v) {
     __hip_atomic_fetch_add(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// v = f over aligned groups of G lanes.  Lane exchanges of the vector unit (16 lanes by DPP, then rows and halves swapped), not through LDS: with a shuffle
+// for each step the balance loss and its gradient took twice as long.
+template <int CTRL, class F>
+__device__ __forceinline__ void across_dpp(float& v, F f) {
+    v = f(v, __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, 0xf, 0xf, true)));
+}
+template <int G, class F>
+__device__ __forceinline__ void across(float& v, F f) {
+    if (G > 1) across_dpp<0xb1>(v, f);    // quad_perm [1, 0, 3, 2]
+    if (G > 2) across_dpp<0x4e>(v, f);    // quad_perm [2, 3, 0, 1]
+    if (G > 4) across_dpp<0x141>(v, f);   // row_half_mirror
+    if (G > 8) across_dpp<0x140>(v, f);   // row_mirror
+    if (G > 16) {
+        const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+    if (G > 32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+        v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
+    }
+}
+
 __device__ __forceinline__ int rfl(int v) { return __builtin_amdgcn_readfirstlane(v); }
 
 // ---- work queues -----------------------------------------------------------

@@ -22,7 +22,7 @@ def test_struct_sizes():
     assert ctypes.sizeof(b.MoEAdapterShape) == 20 and ctypes.sizeof(b.MoEBalanceShape) == 24 and ctypes.sizeof(b.MoEBalanceStatsC) == 40
 
 
-GOOD = dict(T=300, K=64, N=128, rank=16, adapters=4)
+GOOD = dict(T=600, K=64, N=128, rank=16, adapters=4)
 
 
 def adapter_calls(lib, s, **kw):
@@ -52,7 +52,7 @@ def test_adapter_arguments(lib):
     s = moe.make_adapter_shape(**GOOD)
     assert lib.moe_adapter_workspace_bytes(None, None, None) == b.MOE_ERR_ARG
     need, plan = b._adapter_bytes(s)
-    assert need > 0 and plan >= 4 * 300 and plan % 4 == 0
+    assert need > 0 and plan >= 4 * 600 and plan % 4 == 0
     for kw in (dict(ids=None), dict(plan=None), dict(ids=0x1002), dict(plan=0x1004)):
         for call in adapter_calls(lib, s, **kw).values():
             assert call() == b.MOE_ERR_ARG, kw
@@ -68,7 +68,7 @@ def test_adapter_arguments(lib):
 
 
 def test_few_tokens_need_no_plan(lib):
-    s = moe.make_adapter_shape(T=256, K=64, N=128, rank=16, adapters=4)
+    s = moe.make_adapter_shape(T=512, K=64, N=128, rank=16, adapters=4)
     assert b._adapter_bytes(s)[1] == 0
     assert adapter_calls(lib, s, ids=None, plan=None)["plan"]() == b.MOE_OK   # nothing to do
     assert adapter_calls(lib, s, ids=None, plan=None)["forward"]() == b.MOE_ERR_ARG
@@ -113,6 +113,6 @@ def test_balance_arguments(lib):
 def test_the_binding_refuses_other_tensors():
     s = moe.make_adapter_shape(**GOOD)
     with pytest.raises(AssertionError):
-        moe.moe_adapter_plan(s, torch.zeros(300, dtype=torch.int32))   # not on the GPU
+        moe.moe_adapter_plan(s, torch.zeros(600, dtype=torch.int32))   # not on the GPU
     with pytest.raises(AssertionError):
         moe.moe_balance_forward(moe.make_balance_shape(4, 8, 2), torch.zeros((4, 8)), torch.zeros((4, 2), dtype=torch.int32))
