@@ -54,9 +54,11 @@ static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
 bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= kFewTokens; }
 size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) ? 0 : plan_words(s) * 4; }
 
+// IT: the ids stay in registers, 64 IT a wave (0: more than that, read twice).
 // One workgroup: a counting sort.  Every wave counts a contiguous part of the tokens and later gives its tokens their rows, 64 at a
 // time: lanes with the same adapter find each other with a ballot for each bit of the id.
 constexpr int kSortWaves = 16;
+template <int IT>
 __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, int brows, const int32_t* __restrict__ ids, PlanView v) {
     __shared__ int32_t hist[kSortWaves][kMaxAdapters + 1];
     __shared__ int32_t first[kMaxAdapters + 2];     // rows before bin b (bin 0: no adapter, bin a + 1: adapter a)
@@ -70,8 +72,22 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         const int a = t < hi ? ids[t] : -1;
         return (unsigned)a < (unsigned)n ? a + 1 : 0;
     };
+    int bins_of[IT > 0 ? IT : 1];
+#pragma unroll
+    for (int i = 0; i < IT; ++i) bins_of[i] = bin_of(lo + 64 * i + lane);
     __syncthreads();
-    for (int t = lo + lane; t < hi; t += 64) atomicAdd(&hist[w][bin_of(t)], 1);
+    auto count = [&](int t, int b) {   // packed requests: mostly 64 tokens with one adapter
+        if (__ballot(t < hi && b == rfl(b)) == ~0ull) {
+            if (lane == 0) hist[w][b] += 64;
+        } else if (t < hi) {
+            atomicAdd(&hist[w][b], 1);
+        }
+    };
+    if (IT > 0)
+#pragma unroll
+        for (int i = 0; i < IT; ++i) count(lo + 64 * i + lane, bins_of[i]);
+    else
+        for (int t0 = lo; t0 < hi; t0 += 64) count(t0 + lane, bin_of(t0 + lane));
     __syncthreads();
     // bins -> first rows, blocks and segments: thread b has bin b (two at most a thread: 1025 bins)
     int base_rows = 0, base_blocks = 0, base_segs = 0;
@@ -135,13 +151,13 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
     __syncthreads();
     // rows
     volatile int32_t* mine = hist[w];
-    for (int t0 = lo; t0 < hi; t0 += 64) {
-        const int t = t0 + lane, b = bin_of(t);
+    auto place = [&](int t, int b) {
         uint64_t same = __ballot(t < hi);
-        for (int bit = 0; (bins - 1) >> bit; ++bit) {
-            const uint64_t m = __ballot((b >> bit) & 1);
-            same &= (b >> bit) & 1 ? m : ~m;
-        }
+        if (__ballot(b == rfl(b)) != ~0ull)
+            for (int bit = 0; (bins - 1) >> bit; ++bit) {
+                const uint64_t m = __ballot((b >> bit) & 1);
+                same &= (b >> bit) & 1 ? m : ~m;
+            }
         if (t < hi) {
             const int at = mine[b];
             v.order[at + __popcll(same & below)] = t;
@@ -149,7 +165,12 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
             if ((same >> lane) == 1ull) mine[b] = at + __popcll(same);   // the last of them
         }
         __builtin_amdgcn_wave_barrier();
-    }
+    };
+    if (IT > 0)
+#pragma unroll
+        for (int i = 0; i < IT; ++i) place(lo + 64 * i + lane, bins_of[i]);
+    else
+        for (int t0 = lo; t0 < hi; t0 += 64) place(t0 + lane, bin_of(t0 + lane));
     // blocks and units, a wave a bin
     for (int b = w; b < bins; b += kSortWaves) {
         const int r0 = first[b], r1 = first[b + 1], o = b > 0 ? fseg[b] : -1;
@@ -169,7 +190,12 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
 
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st) {
     if (adapter_few(s)) return MOE_OK;
-    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T), ids, plan_view(s, plan));
+    auto launch = [&](auto it) {
+        hipLaunchKernelGGL((adapter_plan_kernel<it.value>), dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T), ids, plan_view(s, plan));
+    };
+    if (s.T <= 64 * kSortWaves * 4) launch(std::integral_constant<int, 4>{});
+    else if (s.T <= 64 * kSortWaves * 16) launch(std::integral_constant<int, 16>{});
+    else launch(std::integral_constant<int, 0>{});
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -924,8 +950,11 @@ __device__ __forceinline__ void read_tr(u32x4_t (&f)[N], const uint32_t (&at)[N]
     for (int i = 0; i < N; ++i) f[i] = u32x4_t{lo[i][0], lo[i][1], hi[i][0], hi[i][1]};
 }
 
+// Waves 0..3 multiply, waves 4..7 only move operands: with one wave a SIMD for both, its requests (ten a stage, each with an address of its own)
+// and its products were done one after the other.
+constexpr int kGradThreads = 2 * kSmallThreads;
 template <int NRF, int NCF>
-__global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams p, GradParams g) {
+__global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p, GradParams g) {
     using G = GradTile<NRF, NCF>;
     __shared__ __attribute__((aligned(512))) char smem[G::kLds];
     __shared__ int32_t s_tok[G::kList];
@@ -939,7 +968,8 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams 
     const int W = g.W[which], c0 = ct * 32 * NCF, r = g.r;
     const int row0 = p.plan.start[a], count = p.plan.start[a + 1] - row0;
     const Lane ln;
-    const int wave = ln.wave_uniform();
+    const int wave = ln.wave_uniform() & 3;
+    const bool moves = ln.wave_uniform() >= 4;
     // x: an instruction moves kXRows rows of kXLanes lanes
     constexpr int kXLanes = 4 * NCF, kXRows = 64 / kXLanes, kHLanes = 4 * NRF, kHRows = 64 / kHLanes;
     const int xk = kXRows * G::kXLoads * wave + ln.l / kXLanes;                                  // (+ kXRows i)
@@ -948,19 +978,35 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams 
     const size_t ldx = g.ldx[which];
     const char* const h = (const char*)(p.terms[which] + (size_t)row0 * 3 * r);
     const uint32_t tok0 = lds_addr(s_tok) + xk * 4;
-    auto issue = [&](int k0, int left, char* dst) {   // the 64 rows from row k0 of the list on, of which `left` are there
+    // h: this lane's chunk of its instructions' rows, from the first row of the adapter on
+    uint32_t oh[G::kHLoads];
+    int hk[G::kHLoads];
+#pragma unroll
+    for (int i = 0; i < G::kHLoads; ++i) {
+        const int u = G::kHLoads * wave + i, term = u / (4 * NRF);
+        hk[i] = (u % (4 * NRF)) * kHRows + ln.l / kHLanes;
+        const int c = (ln.l % kHLanes) ^ ks_swz<G::kHRow>(hk[i]);
+        oh[i] = (hk[i] * 3 + term) * r * 2 + min(c * 16, 2 * r - 16);
+    }
+    auto issue = [&](int k0, int left, char* dst) {   // the 64 rows from row k0 on, of which `left` are there
         int32_t tok[G::kXLoads];
-#pragma unroll
-        for (int i = 0; i < G::kXLoads; ++i)
-            asm volatile("ds_read_b32 %0, %1 offset:%2\n s_waitcnt lgkmcnt(0)" : "=v"(tok[i]) : "v"(tok0 + (k0 % G::kList) * 4), "n"(i * kXRows * 4) : "memory");
+        const uint32_t at = tok0 + (k0 % G::kList) * 4;
+        if constexpr (G::kXLoads == 4)
+            asm volatile("ds_read_b32 %0, %4\n ds_read_b32 %1, %4 offset:%5\n ds_read_b32 %2, %4 offset:%6\n ds_read_b32 %3, %4 offset:%7\n s_waitcnt lgkmcnt(0)"
+                         : "=&v"(tok[0]), "=&v"(tok[1]), "=&v"(tok[2]), "=&v"(tok[3]) : "v"(at), "n"(kXRows * 4), "n"(kXRows * 8), "n"(kXRows * 12) : "memory");
+        else
+            asm volatile("ds_read_b32 %0, %2\n ds_read_b32 %1, %2 offset:%3\n s_waitcnt lgkmcnt(0)" : "=&v"(tok[0]), "=&v"(tok[1]) : "v"(at), "n"(kXRows * 4) : "memory");
         const char* q[G::kXLoads + G::kHLoads];
+        const char* const hs = h + (size_t)k0 * 6 * r;
 #pragma unroll
-        for (int i = 0; i < G::kXLoads; ++i) q[i] = xk + i * kXRows < left ? x + (size_t)tok[i] * ldx : zero_chunk();
+        for (int i = 0; i < G::kXLoads; ++i) q[i] = x + (size_t)tok[i] * ldx;
 #pragma unroll
-        for (int i = 0; i < G::kHLoads; ++i) {
-            const int u = G::kHLoads * wave + i, term = u / (4 * NRF), k = (u % (4 * NRF)) * kHRows + ln.l / kHLanes;
-            const int c = (ln.l % kHLanes) ^ ks_swz<G::kHRow>(k);
-            q[G::kXLoads + i] = k < left ? h + ((size_t)(k0 + k) * 3 + term) * r * 2 + min(c * 16, 2 * r - 16) : zero_chunk();
+        for (int i = 0; i < G::kHLoads; ++i) q[G::kXLoads + i] = hs + oh[i];
+        if (left < BK) {
+#pragma unroll
+            for (int i = 0; i < G::kXLoads; ++i) q[i] = xk + i * kXRows < left ? q[i] : zero_chunk();
+#pragma unroll
+            for (int i = 0; i < G::kHLoads; ++i) q[G::kXLoads + i] = hk[i] < left ? q[G::kXLoads + i] : zero_chunk();
         }
 #pragma unroll
         for (int i = 0; i < G::kXLoads + G::kHLoads; ++i) asm volatile("" : "+v"(q[i]));
@@ -988,34 +1034,39 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams 
     for (int base = 0; base < count; base += G::kList) {
         const int here = min(G::kList, count - base), nst = (here + BK - 1) / BK;
         __syncthreads();   // the list before has been read
-        for (int i = tid; i < here; i += kSmallThreads) s_tok[i] = p.plan.order[row0 + base + i];
+        for (int i = tid; i < here; i += kGradThreads) s_tok[i] = p.plan.order[row0 + base + i];
         __syncthreads();
-#pragma unroll
-        for (int t = 0; t < G::kDepth - 1; ++t)
-            if (t < nst) issue(base + t * BK, here - t * BK, smem + t * G::kStage);
-        int at = 0, next = (G::kDepth - 1) * G::kStage;
-        for (int t = 0; t < nst; ++t) {
-            if (t + G::kDepth - 2 < nst) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((G::kDepth - 2) * (G::kXLoads + G::kHLoads)) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            if (t + G::kDepth - 1 < nst) {
-                issue(base + (t + G::kDepth - 1) * BK, here - (t + G::kDepth - 1) * BK, smem + next);
-                next = next == (G::kDepth - 1) * G::kStage ? 0 : next + G::kStage;
+        if (moves) {
+            for (int t = 0; t < min(G::kDepth - 1, nst); ++t) issue(base + t * BK, here - t * BK, smem + t * G::kStage);
+            int next = (G::kDepth - 1) * G::kStage;
+            for (int t = 0; t < nst; ++t) {
+                if (t + G::kDepth - 2 < nst) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((G::kDepth - 2) * (G::kXLoads + G::kHLoads)) : "memory");
+                else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+                __builtin_amdgcn_s_barrier();   // stage t is here, and stage t - 1 has been read
+                if (t + G::kDepth - 1 < nst) {
+                    issue(base + (t + G::kDepth - 1) * BK, here - (t + G::kDepth - 1) * BK, smem + next);
+                    next = next == (G::kDepth - 1) * G::kStage ? 0 : next + G::kStage;
+                }
             }
-            u32x4_t fx[NCF];
-            read_tr<NCF, 4 * G::kXRow>(fx, ax, at);
+        } else {
+            int at = 0;
+            for (int t = 0; t < nst; ++t) {
+                __builtin_amdgcn_s_barrier();
+                u32x4_t fx[NCF];
+                read_tr<NCF, 4 * G::kXRow>(fx, ax, at);
 #pragma unroll
-            for (int term = 0; term < 3; ++term) {
-                u32x4_t fh[NRF];
-                read_tr<NRF, 4 * G::kHRow>(fh, ah, at + term * G::kH);
+                for (int term = 0; term < 3; ++term) {
+                    u32x4_t fh[NRF];
+                    read_tr<NRF, 4 * G::kHRow>(fh, ah, at + term * G::kH);
 #pragma unroll
-                for (int tf = 0; tf < NRF; ++tf)
+                    for (int tf = 0; tf < NRF; ++tf)
 #pragma unroll
-                    for (int af = 0; af < NCF; ++af)
-                        acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[af]), __builtin_bit_cast(bf16x8_t, fh[tf]),
-                                                                              acc[tf][af], 0, 0, 0);
+                        for (int af = 0; af < NCF; ++af)
+                            acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[af]), __builtin_bit_cast(bf16x8_t, fh[tf]),
+                                                                                  acc[tf][af], 0, 0, 0);
+                }
+                at = at == (G::kDepth - 1) * G::kStage ? 0 : at + G::kStage;
             }
-            at = at == (G::kDepth - 1) * G::kStage ? 0 : at + G::kStage;
         }
     }
 #pragma unroll
@@ -1024,7 +1075,7 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_grad_kernel(ProjParams 
         f32x16_t one[1][NCF];
 #pragma unroll
         for (int af = 0; af < NCF; ++af) one[0][af] = acc[tf][af];
-        small_sum<1, NCF>(smem, one, [&](int row, int col, const float (&v)[8]) {
+        small_sum<1, NCF, kGradThreads>(smem, one, [&](int row, int col, const float (&v)[8]) {
             row += 32 * tf;
             col += c0;
             if (row >= r || col >= W) return;
@@ -1174,9 +1225,9 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         const int cols = p.r > 64 ? 64 : 128;
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
         const dim3 grid((unsigned)(8 * g.n * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)));
-        if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kSmallThreads), 0, st, p, g);
-        else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kSmallThreads), 0, st, p, g);
-        else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kSmallThreads), 0, st, p, g);
+        if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kGradThreads), 0, st, p, g);
+        else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kGradThreads), 0, st, p, g);
+        else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kGradThreads), 0, st, p, g);
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

@@ -266,12 +266,12 @@ __device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f
     __syncthreads();
 }
 
-// Adds the four waves' tiles in LDS, wave 0 first, and hands every thread its runs of 8 columns: f(row, column, values).
-template <int NRF, int NCF, class F>
+// Adds the tiles of waves 0..3 in LDS, wave 0 first, and hands every one of THREADS threads its runs of 8 columns: f(row, column, values).
+template <int NRF, int NCF, int THREADS = kSmallThreads, class F>
 __device__ __forceinline__ void small_sum(char* smem, const f32x16_t (&acc)[NRF][NCF], F f) {
-    constexpr int kPitch = NCF * 128, kWave = kPitch * 32 * NRF;
-    {
-        const Lane ln;
+    constexpr int kPitch = NCF * 128, kWave = kPitch * 32 * NRF, kUnits = 128 * NRF * NCF;
+    const Lane ln;
+    if (THREADS == kSmallThreads || ln.w < 4) {
         char* base = smem + ln.w * kWave;
 #pragma unroll
         for (int tf = 0; tf < NRF; ++tf)
@@ -286,9 +286,9 @@ __device__ __forceinline__ void small_sum(char* smem, const f32x16_t (&acc)[NRF]
     }
     __syncthreads();
 #pragma unroll
-    for (int u = 0; u < NRF * NCF / 2 + (NRF * NCF == 1); ++u) {
-        const int unit = u * kSmallThreads + (int)threadIdx.x;
-        if (NRF * NCF == 1 && unit >= 128) break;
+    for (int u = 0; u < (kUnits + THREADS - 1) / THREADS; ++u) {
+        const int unit = u * THREADS + (int)threadIdx.x;
+        if (kUnits % THREADS != 0 && unit >= kUnits) break;
         const int row = unit / (4 * NCF), c8 = unit % (4 * NCF);
         float v[8];
 #pragma unroll
