@@ -65,15 +65,21 @@ struct KcStages : PlainLoader<KcStages<NI, COLUMNS>> {
 #pragma unroll
         for (int i = 0; i < NI; ++i) p[i] = row_of(min(row(ln, i), last)) + chunk(ln, i) * 16;
     }
-    __device__ __forceinline__ void issue(char* dst) {
+    // one of the full stages
+    __device__ __forceinline__ void issue_full(char* dst) {
         char* d = dst + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * (NI * 1024);
-        if (left > 0) {
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                dma16(p[i], d + i * 1024);
-                p[i] += BK * 2;
-            }
+        for (int i = 0; i < NI; ++i) {
+            dma16(p[i], d + i * 1024);
+            p[i] += BK * 2;
+        }
+        --left;
+    }
+    __device__ __forceinline__ void issue(char* dst) {
+        if (left > 0) {
+            issue_full(dst);
         } else {
+            char* d = dst + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * (NI * 1024);
             const Lane ln;
             const char* q[NI];
 #pragma unroll
@@ -89,8 +95,8 @@ struct KcStages : PlainLoader<KcStages<NI, COLUMNS>> {
             for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(q[i]));   // the addresses exist before the first request
 #pragma unroll
             for (int i = 0; i < NI; ++i) dma16(q[i], d + i * 1024);
+            --left;
         }
-        --left;
     }
 };
 
@@ -116,15 +122,20 @@ struct KsStages : PlainLoader<KsStages<NI, TC>> {
 #pragma unroll
         for (int i = 0; i < NI; ++i) p[i] = m + ((size_t)krow(ln, i) * n + col[i & 1]) * 2;
     }
-    __device__ __forceinline__ void issue(char* dst) {
+    __device__ __forceinline__ void issue_full(char* dst) {
         char* d = dst + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * (NI * 1024);
-        if (left > 0) {
 #pragma unroll
-            for (int i = 0; i < NI; ++i) {
-                dma16(p[i], d + i * 1024);
-                p[i] += step;
-            }
+        for (int i = 0; i < NI; ++i) {
+            dma16(p[i], d + i * 1024);
+            p[i] += step;
+        }
+        --left;
+    }
+    __device__ __forceinline__ void issue(char* dst) {
+        if (left > 0) {
+            issue_full(dst);
         } else {
+            char* d = dst + __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)) * (NI * 1024);
             const Lane ln;
             const char* q[NI];
 #pragma unroll
@@ -137,8 +148,8 @@ struct KsStages : PlainLoader<KsStages<NI, TC>> {
             for (int i = 0; i < NI; ++i) asm volatile("" : "+v"(q[i]));
 #pragma unroll
             for (int i = 0; i < NI; ++i) dma16(q[i], d + i * 1024);
+            --left;
         }
-        --left;
     }
 };
 
@@ -242,16 +253,7 @@ __device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f
         la.issue(smem + t * S::kStage + S::kRowsBytes);
     }
     int at = 0, next = (kDepth - 1) * S::kStage;   // buffers of stages t and t + kDepth - 1
-    for (int t = 0; t < nk; ++t) {
-        // stage t is here when at most those behind it are on their way
-        if (t + kDepth - 2 < nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kDepth - 2) * kRequests) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        if (t + kDepth - 1 < nk) {   // into the buffer that every wave has read before the barrier
-            lb.issue(smem + next);
-            la.issue(smem + next + S::kRowsBytes);
-            next = next == (kDepth - 1) * S::kStage ? 0 : next + S::kStage;
-        }
+    auto multiply = [&]() {
         u32x4_t rb[NRF], ra[NCF];
         fr.read(at, rb, ra);
         at = at == (kDepth - 1) * S::kStage ? 0 : at + S::kStage;
@@ -261,6 +263,27 @@ __device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f
             for (int af = 0; af < NCF; ++af)
                 acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ra[af]), __builtin_bit_cast(bf16x8_t, rb[tf]),
                                                                       acc[tf][af], 0, 0, 0);
+    };
+    // while full stages are left to request: no branch but the loop's
+    int t = 0;
+    for (int n = lb.left; n > 0; --n, ++t) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kDepth - 2) * kRequests) : "memory");   // stage t is here when at most those behind it are on their way
+        __builtin_amdgcn_s_barrier();
+        lb.issue_full(smem + next);   // into the buffer that every wave has read before the barrier
+        la.issue_full(smem + next + S::kRowsBytes);
+        next = next == (kDepth - 1) * S::kStage ? 0 : next + S::kStage;
+        multiply();
+    }
+    for (; t < nk; ++t) {
+        if (t + kDepth - 2 < nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kDepth - 2) * kRequests) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if (t + kDepth - 1 < nk) {
+            lb.issue(smem + next);
+            la.issue(smem + next + S::kRowsBytes);
+            next = next == (kDepth - 1) * S::kStage ? 0 : next + S::kStage;
+        }
+        multiply();
     }
     __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
