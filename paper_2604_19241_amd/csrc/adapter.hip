@@ -14,6 +14,7 @@
 #include "adapter.hpp"
 
 #include <algorithm>
+#include <cstdlib>
 #include <type_traits>
 
 namespace uniep {
@@ -22,10 +23,11 @@ constexpr int kFewTokens = 512;
 constexpr int kFewWords = kFewTokens / 64;
 // Rows of a block of the plan: as many tokens of one adapter share the fetch of its first factor.
 static int block_rows(int T) { return T >= 16384 ? 64 : 32; }
+constexpr int kGradRows = 64;         // rows up to which an adapter's gradients are made row by row (adapter_grad_rows_kernel)
 constexpr int kUnit = 64;             // rows of which the plan knows the first and the last segment
 
 // ------------------------------------------------------------------ the plan
-// int32 words: [0] blocks, [1] segments, [2] rows without an adapter, then the arrays.
+// int32 words: [0] blocks, [1] segments, [2] rows without an adapter, [3] adapters with many rows, then the arrays.
 struct PlanView {
     int32_t* head;
     int32_t* order;      // [T] row -> token: those without an adapter, then by adapter, each in the order of the tokens
@@ -33,12 +35,13 @@ struct PlanView {
     int32_t* ordinal;    // [n] which segment an adapter is
     int32_t* seg;        // [n] segment -> adapter
     int32_t* unit;       // [units][2] segments of the first and the last row of every kUnit rows (-1: no adapter)
+    int32_t* many;       // [n] adapters with more than kGradRows rows (as many as head[3] says)
     int32_t* block;      // [blocks][2] first row; rows | (adapter + 1) << 8.  One adapter, one multiple of block_rows
 };
 static size_t plan_blocks(const moe_adapter_shape_t& s) { return (size_t)s.T / block_rows(s.T) + s.adapters + 2; }
 static size_t plan_units(const moe_adapter_shape_t& s) { return ((size_t)s.T + kUnit - 1) / kUnit; }
 static size_t plan_words(const moe_adapter_shape_t& s) {
-    return 16 + (size_t)s.T + 3 * (size_t)s.adapters + 1 + 2 * plan_units(s) + 2 * plan_blocks(s);
+    return 16 + (size_t)s.T + 4 * (size_t)s.adapters + 1 + 2 * plan_units(s) + 2 * plan_blocks(s);
 }
 static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
     PlanView v;
@@ -49,9 +52,10 @@ static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
     v.start = v.order + s.T;
     v.ordinal = v.start + s.adapters + 1;
     v.seg = v.ordinal + s.adapters;
+    v.many = v.seg + s.adapters;
     return v;
 }
-bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= kFewTokens; }
+bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= (getenv("FEW") ? atoi(getenv("FEW")) : kFewTokens); }
 size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) ? 0 : plan_words(s) * 4; }
 
 // IT: the ids stay in registers, 64 IT a wave (0: more than that, read twice).
@@ -120,7 +124,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         const int nb = c > 0 ? (r0 + c - 1) / brows - r0 / brows + 1 : 0;
         const int k0 = scan(nb, 1, base_blocks, total);
         base_blocks += total;
-        const int s0 = scan(b > 0 && c > 0 ? 1 : 0, 2, base_segs, total);
+        const int both = scan(b > 0 && c > 0 ? 1 | (c > kGradRows) << 16 : 0, 2, base_segs, total), s0 = both & 0xffff;   // (up to 1024 of each)
         base_segs += total;
         if (b < bins) {
             first[b] = r0;
@@ -136,6 +140,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
                 v.start[b - 1] = r0;
                 v.ordinal[b - 1] = s0;
                 if (c > 0) v.seg[s0] = b - 1;
+                if (c > kGradRows) v.many[both >> 16] = b - 1;
             }
         }
         __syncthreads();
@@ -145,7 +150,8 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         fblock[bins] = base_blocks;
         v.start[n] = T;
         v.head[0] = base_blocks;
-        v.head[1] = base_segs;
+        v.head[1] = base_segs & 0xffff;
+        v.head[3] = base_segs >> 16;
         v.head[2] = bins > 1 ? first[1] : T;
     }
     __syncthreads();
@@ -287,11 +293,12 @@ struct Members {
     }
 };
 
-// Ranks [j0, j1) of h for up to 4 tokens over [k0, k1) of the reduction, by dot products: wave w has every fourth rank, its lanes 8 elements of 512 each.  For so
-// few tokens the tile of 32 rows by 64 ranks that is used for more moves ten times the bytes (256 tokens of 256 adapters, 8 ranks of 2048: 19 us, with dots
-// FIRST us).
+// Ranks [j0, j1) of h for up to 4 tokens over [k0, k1) of the reduction, by dot products: wave w has every fourth rank, its lanes 8 elements of 512 each;
+// put(m, j, v) is called by one lane.  For so few tokens the tile of 32 rows by 64 ranks that is used for more moves ten times the bytes (the first launch of
+// 256 tokens of 256 adapters, 8 ranks of 2048: 19.0 us, with dots 14.3).
 constexpr int kDotTokens = 4;
-__device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int j1, int rows, const int32_t* list, int k0, int k1, float* out) {
+template <class TokenFn, class PutFn>
+__device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int j1, int rows, int k0, int k1, TokenFn token, PutFn put) {
     constexpr int kRanks = 4;   // of a wave, at a time
     const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
     for (int j = j0 + w; j < j1; j += 4 * kRanks) {
@@ -310,7 +317,7 @@ __device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int
 #pragma unroll
                 for (int m = 0; m < kDotTokens; ++m) {
                     x[h][m] = zero4();
-                    if (k < k1 && m < rows) x[h][m] = *(const u32x4_t*)(p.x + (size_t)list[m] * p.ldx + (size_t)k * 2);
+                    if (k < k1 && m < rows) x[h][m] = *(const u32x4_t*)(p.x + (size_t)token(m) * p.ldx + (size_t)k * 2);
                 }
             }
 #pragma unroll
@@ -329,7 +336,7 @@ __device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int
             for (int m = 0; m < kDotTokens; ++m)
                 if (m < rows && j + 4 * i < j1) {
                     across<64>(acc[i][m], [](float u, float v) { return u + v; });
-                    if (lane == 0) out[(size_t)list[m] * p.r + j + 4 * i] = acc[i][m];
+                    if (lane == 0) put(m, j + 4 * i, acc[i][m]);
                 }
     }
 }
@@ -389,7 +396,9 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
     const int rows = min(32, mb.count() - rank);
     const int s0 = sp * p.hper_split, s1 = min(nst, s0 + p.hper_split);
     if (rank == 0 && rows <= kDotTokens) {
-        few_dots(p, a, 64 * rt, min(p.r, 64 * rt + 64), rows, s_list, s0 * BK, min(p.R, s1 * BK), p.hpart + (size_t)sp * p.T * p.r);
+        float* const out = p.hpart + (size_t)sp * p.T * p.r;
+        few_dots(p, a, 64 * rt, min(p.r, 64 * rt + 64), rows, s0 * BK, min(p.R, s1 * BK), [&](int m) { return s_list[m]; },
+                 [&](int m, int j, float v) { out[(size_t)s_list[m] * p.r + j] = v; });
         return;
     }
     const Stages st = part_of(s0, s1);
@@ -522,50 +531,42 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
 
 // Gradients of 8 ranks and 256 columns of one adapter, token by token; the waves share the tokens and their sums are added in LDS.  (With 512 columns a
 // wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4 workgroups that took 128 tokens one after
-// the other: 48 us.)
+// the other: 48 us, now 11.)
 constexpr int kGradRanks = 8, kGradCols = 256;
+template <int TOKENS>
 struct FewGradShared {
-    float h[kFewTokens][kGradRanks];
+    float h[TOKENS][kGradRanks];
     float sums[4][kGradRanks][kGradCols];
     uint64_t mask[kFewWords];
-    int32_t list[kFewTokens];
+    int32_t list[TOKENS];
 };
-__device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared& S) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    const int of = g.n * g.rank_tiles * g.col_tiles[0], which = id < of ? 0 : 1;
-    if (which) id -= of;
-    const int cb = id % g.col_tiles[which], rest = id / g.col_tiles[which], a = rest % g.n, j0 = rest / g.n * kGradRanks, W = g.W[which];
-    Members mb;
-    mb.find(g.T, g.n, p.ids, a, S.mask);
-    mb.list(0, kFewTokens, S.list);
-    const int count = mb.count(), c = cb * kGradCols + 4 * lane;
+// Which piece of work `id` is.
+struct FewGradTask {
+    int which, cb, a, j0;
+    __device__ __forceinline__ FewGradTask(const GradParams& g, int id) {
+        const int of = g.n * g.rank_tiles * g.col_tiles[0];
+        which = id < of ? 0 : 1;
+        if (which) id -= of;
+        const int rest = id / g.col_tiles[which];
+        cb = id % g.col_tiles[which];
+        a = rest % g.n;
+        j0 = rest / g.n * kGradRanks;
+    }
+};
+// S.list[0 .. count): the adapter's tokens; h4(k, token, j) = 4 ranks from j on of the k-th.
+template <int TOKENS, class H4>
+__device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGradTask& t, int count, FewGradShared<TOKENS>& S, H4 h4) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, W = g.W[t.which], c = t.cb * kGradCols + 4 * lane;
     float acc[kGradRanks][4] = {};
     if (count > 0) {
-        const float s = p.scale ? p.scale[a] : 1.f;
         // the first rows of x are on their way while h is fetched
         constexpr int kPre = 8;
-        const char* const x = g.x[which] + (size_t)min(c, W - 4) * 2;
+        const size_t ldx = g.ldx[t.which];
+        const char* const x = g.x[t.which] + (size_t)min(c, W - 4) * 2;
         u32x2_t pre[kPre];
 #pragma unroll
-        for (int i = 0; i < kPre; ++i) pre[i] = *(const u32x2_t*)(x + (size_t)S.list[min(w + 4 * i, count - 1)] * g.ldx[which]);
-        for (int i = tid; i < 2 * count; i += 256) {   // 4 ranks of a token
-            const int k = i >> 1, j = 4 * (i & 1), tok = S.list[k];
-            f32x4_t v;
-            if (g.h[which]) {
-                v = *(const f32x4_t*)(g.h[which] + (size_t)tok * g.r + j0 + j);
-            } else {
-                v = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-                for (int q = 0; q < p.hsplits; ++q) {
-                    const f32x4_t u = *(const f32x4_t*)(p.hpart + ((size_t)q * p.T + tok) * p.r + j0 + j);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] += u[e];
-                }
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] *= s;
-            }
-            *(f32x4_t*)&S.h[k][j] = v;
-        }
+        for (int i = 0; i < kPre; ++i) pre[i] = *(const u32x2_t*)(x + (size_t)S.list[min(w + 4 * i, count - 1)] * ldx);
+        for (int i = tid; i < 2 * count; i += 256) *(f32x4_t*)&S.h[i >> 1][4 * (i & 1)] = h4(S.list[i >> 1], t.j0 + 4 * (i & 1));
         __syncthreads();
         if (c < W) {
 #pragma unroll
@@ -575,7 +576,7 @@ __device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradPar
                     for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[w + 4 * i][j], pre[i]);
 #pragma unroll 8
             for (int k = w + 4 * kPre; k < count; k += 4) {
-                const u32x2_t b = *(const u32x2_t*)(x + (size_t)S.list[k] * g.ldx[which]);
+                const u32x2_t b = *(const u32x2_t*)(x + (size_t)S.list[k] * ldx);
 #pragma unroll
                 for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[k][j], b);
             }
@@ -595,8 +596,29 @@ __device__ __forceinline__ void few_grad_task(const ProjParams& p, const GradPar
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] += o[q];
         }
-        *(f32x4_t*)(g.out[which] + ((size_t)a * g.r + j0 + j) * W + c) = v;
+        *(f32x4_t*)(g.out[t.which] + ((size_t)t.a * g.r + t.j0 + j) * W + c) = v;
     }
+}
+__device__ __forceinline__ void few_tokens_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared<kFewTokens>& S) {
+    const FewGradTask t(g, id);
+    Members mb;
+    mb.find(g.T, g.n, p.ids, t.a, S.mask);
+    mb.list(0, kFewTokens, S.list);
+    const float* const h = g.h[t.which];
+    const float s = p.scale ? p.scale[t.a] : 1.f;
+    few_grad_task(g, t, mb.count(), S, [&](int tok, int j) {
+        if (h) return *(const f32x4_t*)(h + (size_t)tok * g.r + j);
+        f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+        for (int q = 0; q < p.hsplits; ++q) {
+            const f32x4_t u = *(const f32x4_t*)(p.hpart + ((size_t)q * p.T + tok) * p.r + j);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] += u[e];
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] *= s;
+        return v;
+    });
 }
 
 template <int G>
@@ -608,19 +630,22 @@ template <int G>
 __global__ void __launch_bounds__(256) adapter_few_second_grad_kernel(ProjParams p, GradParams g, int joins) {
     union Shared {
         JoinShared<G> join;
-        FewGradShared grad;
+        FewGradShared<kFewTokens> grad;
     };
     __shared__ Shared S;
     const int id = blockIdx.x;
     if (id < joins) join_task<G>(p, id % p.T, id / p.T, S.join);
-    else few_grad_task(p, g, id - joins, S.grad);
+    else few_tokens_grad_task(p, g, id - joins, S.grad);
 }
 
 // ------------------------------------------------------------------ more tokens
 // The low-rank rows of tile i (tile_rows rows from tile_rows i on): segments first .. first + count - 1 of the plan.  The tiles before
 // it have at most first + i segments together (each may share one with the next), which bounds where it begins.
+// A tile with more segments than a quarter of its rows has its low-rank part added row by row instead, after the product: a segment costs the matrix pipe 2 r columns for all
+// rows, a row costs the vector unit r of its own (in tiles of 64 x 64 both take as long at some 14 segments, of 256 x 256 at 58).
 struct TileLow {
     int first, count, used, ld;   // used, ld: columns; ld a multiple of BK
+    bool apart;
     size_t at;                    // first element in hx
 };
 __device__ __forceinline__ TileLow tile_low(const ProjParams& p, int tile) {
@@ -629,7 +654,8 @@ __device__ __forceinline__ TileLow tile_low(const ProjParams& p, int tile) {
     TileLow t;
     t.first = max(f, 0);
     t.count = l < 0 ? 0 : l - t.first + 1;
-    t.used = t.count * 2 * p.r;
+    t.apart = 4 * t.count > p.tile_rows;
+    t.used = t.apart ? 0 : t.count * 2 * p.r;
     t.ld = (t.used + BK - 1) / BK * BK;
     t.at = (size_t)p.tile_rows * ((size_t)tile * (2 * p.r + BK) + (size_t)t.first * 2 * p.r);
     return t;
@@ -703,8 +729,14 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
             }
             store_terms(p.terms[0] + (size_t)(row0 + row) * 3 * p.r + col, p.r, v);
         }
-    f32x16_t acc[NRF][NCF];
-    {
+    const float s = p.scale ? p.scale[a] : 1.f;
+    // (one copy of what is done with a value, for both ways to it: a launch this short waits for its instructions too)
+    const bool dots = rows <= kDotTokens;
+    float(*const d)[kMaxRank] = (float(*)[kMaxRank])smem;
+    if (dots) {
+        few_dots(p, a, 0, p.r, rows, 0, p.R, [&](int m) { return p.plan.order[row0 + m]; }, [&](int m, int j, float v) { d[m][j] = v; });
+    } else {
+        f32x16_t acc[NRF][NCF];
         const Lane ln;
         KcStages<NRF, false> lb;
         lb.init(ln, rows, st, [&](int r) { return p.x + (size_t)p.plan.order[row0 + r] * p.ldx; });
@@ -712,25 +744,43 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
         KcStages<NCF, true> la;
         la.init(ln, p.r, st, [&](int j) { return p.first + ((size_t)a * p.r + j) * p.R * 2; });
         small_loop<NRF, NCF, kKc>(lb, la, st.full + (st.tail > 0), smem, acc);
+        small_put(smem, acc);
     }
-    const float s = p.scale ? p.scale[a] : 1.f;
-    small_sum<NRF, NCF>(smem, acc, [&](int row, int col, const float (&v)[8]) {
-        if (row >= rows || col >= p.r) return;
-        float h[8], hi[8], lo[8];
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < rows * (p.r / 8); i += kSmallThreads) {
+        const int row = i / (p.r / 8), col = 8 * (i - row * (p.r / 8));
+        float h[8], e[8], l[8];
+        if (dots) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) h[j] = d[row][col + j];
+        } else {
+            small_get<NRF, NCF>(smem, row, col >> 3, h);
+        }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            h[j] = v[j] * s;
-            hi[j] = bf16_round(h[j]);
-            lo[j] = fabsf(hi[j]) < INFINITY ? h[j] - hi[j] : 0.f;   // an infinite h stays one
+            h[j] *= s;
+            e[j] = bf16_round(h[j]);
+            l[j] = fabsf(e[j]) < INFINITY ? h[j] - e[j] : 0.f;   // an infinite h stays one
         }
         f32x4_t* to = (f32x4_t*)(p.h + (size_t)p.plan.order[row0 + row] * p.r + col);
         to[0] = f32x4_t{h[0], h[1], h[2], h[3]};
         to[1] = f32x4_t{h[4], h[5], h[6], h[7]};
-        uint16_t* x = hx + (size_t)row * tl.ld + own + col;
-        *(u32x4_t*)x = pack8f(hi);
-        *(u32x4_t*)(x + p.r) = pack8f(lo);
-        if (p.terms[1]) store_terms(p.terms[1] + (size_t)(row0 + row) * 3 * p.r + col, p.r, h);
-    });
+        const u32x4_t hi = pack8f(e), lo = pack8f(l);
+        if (!tl.apart) {
+            uint16_t* x = hx + (size_t)row * tl.ld + own + col;
+            *(u32x4_t*)x = hi;
+            *(u32x4_t*)(x + p.r) = lo;
+        }
+        if (p.terms[1]) {   // the third term is what the first two leave
+            uint16_t* x = p.terms[1] + (size_t)(row0 + row) * 3 * p.r + col;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) l[j] = fabsf(e[j]) < INFINITY ? l[j] - bf16_round(l[j]) : 0.f;
+            *(u32x4_t*)x = hi;
+            *(u32x4_t*)(x + p.r) = lo;
+            *(u32x4_t*)(x + 2 * p.r) = pack8f(l);
+        }
+    }
 }
 
 // sum_j h[j] second[a][j][col ..]: the low-rank part of 8 columns of one row, for tiles in which something is not finite
@@ -773,22 +823,24 @@ struct TileId {
     }
 };
 
-// Tiles of 64 x 64.
+// Tiles of 64 x 64 and of 128 x 128.
 // A factor with an infinity or NaN must not reach the rows of other adapters, but 0 times it would: a tile whose sums are not all finite
 // is computed again without its low-rank part, which is then added row by row (as is one where x or W is not finite).
-template <int FORM>
-__global__ void __launch_bounds__(kSmallThreads) adapter_small_kernel(ProjParams p) {
-    __shared__ __attribute__((aligned(512))) char smem[SmallTile<2, 2>::kLds];
+template <int FORM, bool MID>
+__global__ void __launch_bounds__(MID ? kMidThreads : kSmallThreads) adapter_tile_kernel(ProjParams p) {
+    constexpr int kTile = MID ? 128 : 64;
+    __shared__ __attribute__((aligned(512))) char smem[MID ? MidTile::kLds : SmallTile<2, 2>::kLds];
     __shared__ int s_bad;
     const TileId at(p);
     const int rt = at.rt, ct = at.ct;
-    const int row0 = rt * 64, rows = min(64, p.T - row0), col0 = ct * 64;
+    const int row0 = rt * kTile, rows = min(kTile, p.T - row0), col0 = ct * kTile;
     const TileLow tl = tile_low(p, rt);
     const Stages st = stages_of(p.R);
     const int dense = st.full + (st.tail > 0);
-    if (threadIdx.x == 0) s_bad = 0;
+    if (threadIdx.x == 0) s_bad = tl.apart;
     f32x16_t acc[2][2];
-    for (int low = 1;; low = 0) {
+#pragma unroll 1
+    for (int low = !tl.apart;; low = 0) {
         {
             const Lane ln;
             KcStages<2, false> lb;
@@ -796,16 +848,18 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_small_kernel(ProjParams
             lb.low = low_of(p, tl, FORM == kKc);
             const int nk = dense + (low ? tl.ld / BK : 0);
             if constexpr (FORM == kKs) {
-                KsStages<2, 64> la;
+                KsStages<2, kTile> la;
                 la.init(ln, p.w, col0, p.C, st);
                 la.low = lb.low;
-                small_loop<2, 2, kKs>(lb, la, nk, smem, acc);
+                if constexpr (MID) mid_loop<kKs>(lb, la, nk, smem, acc);
+                else small_loop<2, 2, kKs>(lb, la, nk, smem, acc);
             } else {
                 KcStages<2, true> la;
-                la.init(ln, min(64, p.C - col0), st, [&](int c) { return p.w + (size_t)(col0 + c) * p.R * 2; });
+                la.init(ln, min(kTile, p.C - col0), st, [&](int c) { return p.w + (size_t)(col0 + c) * p.R * 2; });
                 la.low = lb.low;
                 la.first = col0;
-                small_loop<2, 2, kKc>(lb, la, nk, smem, acc);
+                if constexpr (MID) mid_loop<kKc>(lb, la, nk, smem, acc);
+                else small_loop<2, 2, kKc>(lb, la, nk, smem, acc);
             }
         }
         if (!low || tl.count == 0) break;
@@ -815,12 +869,14 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_small_kernel(ProjParams
         if (!s_bad) break;
     }
     const bool bad = s_bad;
-    small_sum<2, 2>(smem, acc, [&](int row, int col, float (&v)[8]) {
+    auto store = [&](int row, int col, float (&v)[8]) {
         col += col0;
         if (row >= rows || col >= p.C) return;
         if (bad) add_low(p, row0 + row, col, v);
         store_y(p, row0 + row, col, v);
-    });
+    };
+    if constexpr (MID) mid_sum(smem, acc, store);
+    else small_sum<2, 2>(smem, acc, store);
 }
 
 // Tiles of 256 columns and up to 256 rows (mma.hpp's loops).
@@ -857,9 +913,10 @@ __global__ void __launch_bounds__(kMmaThreads) __attribute__((amdgpu_waves_per_e
     const TileLow tl = tile_low(p, rt);
     const Stages st = stages_of(p.R);
     const int dense = st.full + (st.tail > 0);
-    if (threadIdx.x == 0) s_bad = 0;
+    if (threadIdx.x == 0) s_bad = tl.apart;
     Acc acc;
-    for (int low = 1;; low = 0) {
+#pragma unroll 1
+    for (int low = !tl.apart;; low = 0) {
         const Lane ln;
         const LowRank lr = low_of(p, tl, FORM == kKc);
         const int nk = dense + (low ? tl.ld / BK : 0);
@@ -953,6 +1010,7 @@ __device__ __forceinline__ void read_tr(u32x4_t (&f)[N], const uint32_t (&at)[N]
 // Waves 0..3 multiply, waves 4..7 only move operands: with one wave a SIMD for both, its requests (ten a stage, each with an address of its own)
 // and its products were done one after the other.
 constexpr int kGradThreads = 2 * kSmallThreads;
+// g.few: adapters with up to kGradRows rows are left to adapter_grad_rows_kernel.
 template <int NRF, int NCF>
 __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p, GradParams g) {
     using G = GradTile<NRF, NCF>;
@@ -960,7 +1018,12 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     __shared__ int32_t s_tok[G::kList];
     const int tid = threadIdx.x;
     // every XCD a run of the column tiles, adapter by adapter: its workgroups share one adapter's h in their L2, however unlike the adapters are
-    const int tiles = g.col_tiles[0] + g.col_tiles[1], per = (tiles + 7) >> 3, slot = blockIdx.x >> 3, a = slot / per;
+    const int tiles = g.col_tiles[0] + g.col_tiles[1], per = (tiles + 7) >> 3, slot = blockIdx.x >> 3;
+    int a = slot / per;
+    if (g.few) {
+        if (a >= p.plan.head[3]) return;
+        a = p.plan.many[a];
+    }
     int ct = (blockIdx.x & 7) * per + slot % per;
     if (ct >= tiles) return;
     const int which = ct < g.col_tiles[0] ? 0 : 1;
@@ -1086,6 +1149,19 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     }
 }
 
+// The same for adapters with up to kGradRows rows, on the vector unit: a workgroup of the tiles above takes 6 us whatever its rows and has a CU for itself (600 tokens on
+// 200 adapters of 680 x 480, 16 ranks: GRADMANY us, with this GRADROWS).
+__global__ void __launch_bounds__(256) adapter_grad_rows_kernel(ProjParams p, GradParams g) {
+    __shared__ FewGradShared<kGradRows> S;
+    const FewGradTask t(g, blockIdx.x);
+    const int row0 = p.plan.start[t.a], count = p.plan.start[t.a + 1] - row0;
+    if (count > kGradRows) return;
+    if ((int)threadIdx.x < count) S.list[threadIdx.x] = p.plan.order[row0 + threadIdx.x];
+    __syncthreads();
+    const float* const h = g.h[t.which];
+    few_grad_task(g, t, count, S, [&](int tok, int j) { return *(const f32x4_t*)(h + (size_t)tok * g.r + j); });
+}
+
 // ------------------------------------------------------------------ launches
 static int stages_in(int R) { return (R + BK - 1) / BK; }
 struct FewPlan {
@@ -1110,16 +1186,38 @@ static size_t few_bytes(int T, int R, int C, int r) {
     const FewPlan f = few_plan(T, R, C, r);
     return align_up((size_t)f.splits * T * C * 4, 256) + align_up((size_t)f.hsplits * T * r * 4, 256);
 }
-// Rows of a tile, 256 columns wide, or 64 for tiles of 64 x 64.
-static int tile_rows_of(int T, int C) {
-    auto tiles = [&](int rows, int cols) { return ((long long)T + rows - 1) / rows * ((C + cols - 1) / cols); };
-    if (tiles(256, 256) >= 192) return 256;
-    if (tiles(128, 256) >= 128) return 128;
-    return 64;
+// Tiles of the product.  A stage of 64 k takes about 0.38 us in tiles of 64 x 64 (two on a CU), 0.6 in tiles of 128 x 128, 1.0 in 128 x 256 and 1.45 in 256 x 256, and what counts
+// is how often the CUs have to be filled.  Measured, us of the forward call with each (K, N; 16 ranks, 8 adapters; the choice is the fastest of every line):
+//   1021 tokens, 2048 x 2816      34.0   31.3   41.1   56.6        16384, 512 x 256              20.0   16.7   20.8   25.0
+//   4099, 2048 x 128              18.3   28.1   38.3   53.6        600, 5000 x 5000             104.5   58.7   90.4  130.2
+//   4099, 2048 x 1408             54.3   53.0   43.8   57.7        6000, 1000 x 3000             97.6   81.4   78.6   74.6
+//   4099, 1408 x 2048             54.3   57.6   58.6   46.3        2048, 4096 x 4096            119.8   95.1   79.6   99.8
+//   8192, 7168 x 2048            361.9  281.4  241.3  214.0        1024, 7168 x 7168            178.5  139.5  117.9  159.4
+// (256 x 256 by 4 waves, each with a quarter of 128 x 128 in 256 accumulator registers, moves a quarter less through the LDS and was 1 to 10 % slower: one wave a SIMD
+// waits at every barrier.)
+struct TileShape {
+    int rows, cols;
+};
+static TileShape tile_shape(int T, int C) {
+    struct Form {
+        TileShape t;
+        int slots, cost;
+    };
+    static const Form forms[] = {{{256, 256}, 256, 145}, {{128, 256}, 256, 100}, {{128, 128}, 256, 60}, {{64, 64}, 512, 38}};
+    TileShape best = {};
+    long long least = INT64_MAX;
+    for (const Form& f : forms) {
+        const long long tiles = ((long long)T + f.t.rows - 1) / f.t.rows * ((C + f.t.cols - 1) / f.t.cols), cost = (tiles + f.slots - 1) / f.slots * f.cost;
+        if (cost < least) {
+            least = cost;
+            best = f.t;
+        }
+    }
+    return best;
 }
+static size_t hx_most(const moe_adapter_shape_t& s) { return std::max(hx_bytes(s, tile_shape(s.T, s.N).rows), hx_bytes(s, tile_shape(s.T, s.K).rows)); }
 static size_t many_bytes(const moe_adapter_shape_t& s) {
-    const size_t hx = std::max(hx_bytes(s, tile_rows_of(s.T, s.N)), hx_bytes(s, tile_rows_of(s.T, s.K)));
-    return align_up(hx, 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256) +
+    return align_up(hx_most(s), 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256) +
            2 * align_up((size_t)s.T * s.rank * 6, 256);
 }
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
@@ -1148,11 +1246,11 @@ static bool join_groups(const ProjParams& p) { return (long long)p.T * p.r * p.C
 template <int FORM>
 static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
     p.plan = plan_view(s, plan);
-    p.tile_rows = tile_rows_of(p.T, p.C);
+    const TileShape tile = tile_shape(p.T, p.C);
+    p.tile_rows = tile.rows;
     p.blocks = ((int)plan_blocks(s) + 7) & ~7;
-    const size_t hx = std::max(hx_bytes(s, tile_rows_of(s.T, s.N)), hx_bytes(s, tile_rows_of(s.T, s.K)));
     p.hx = ws;
-    char* rest = ws + align_up(hx, 256);
+    char* rest = ws + align_up(hx_most(s), 256);
     if (!p.h) p.h = (float*)rest;
     p.second_t = rest + align_up((size_t)s.T * s.rank * 4, 256);
     const dim3 low((unsigned)(p.blocks + (FORM == kKc ? p.n * ((p.C + 63) / 64) : 0)));
@@ -1167,11 +1265,11 @@ static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan,
     };
     if (block_rows(p.T) == 64) low_launch(std::integral_constant<int, 2>{});
     else low_launch(std::integral_constant<int, 1>{});
-    const int cols = p.tile_rows == 64 ? 64 : BN;
     p.row_tiles = (p.T + p.tile_rows - 1) / p.tile_rows;
-    p.col_tiles = (p.C + cols - 1) / cols;
+    p.col_tiles = (p.C + tile.cols - 1) / tile.cols;
     const dim3 grid((unsigned)(p.row_tiles * p.col_tiles));
-    if (p.tile_rows == 64) hipLaunchKernelGGL((adapter_small_kernel<FORM>), grid, dim3(kSmallThreads), 0, st, p);
+    if (tile.cols == 64) hipLaunchKernelGGL((adapter_tile_kernel<FORM, false>), grid, dim3(kSmallThreads), 0, st, p);
+    else if (tile.cols == 128) hipLaunchKernelGGL((adapter_tile_kernel<FORM, true>), grid, dim3(kMidThreads), 0, st, p);
     else hipLaunchKernelGGL((adapter_big_kernel<FORM>), grid, dim3(kMmaThreads), 0, st, p);
 }
 
@@ -1201,13 +1299,13 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
     p.x = (const char*)dy, p.ldx = lddy * 2, p.w = (const char*)w, p.first = (const char*)b, p.second = (const char*)a;
     p.scale = scale, p.ids = ids, p.y = (char*)dx;
     GradParams g = {};
-    g.T = s.T, g.r = s.rank, g.n = s.adapters, g.few = adapter_few(s);
+    g.T = s.T, g.r = s.rank, g.n = s.adapters;
     g.W[0] = s.N, g.W[1] = s.K;
     g.x[0] = (const char*)dy, g.x[1] = (const char*)x;
     g.ldx[0] = lddy * 2, g.ldx[1] = ldx * 2;
     g.h[0] = h;
     g.out[0] = db, g.out[1] = da;
-    if (g.few) {
+    if (adapter_few(s)) {
         FewPlan f;
         if (s.T > 0) {
             few_params(p, ws, f);
@@ -1222,9 +1320,18 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
     } else {
         p.h_given = h;
         many_launch<kKc>(p, s, plan, ws, st);
+        // With so many adapters that they have few rows on average, those that do have are done by a kernel for that
+        const bool rows = (long long)g.n * kGradRows >= g.T;
+        g.few = rows;
+        g.h[1] = p.h;
+        if (rows) {
+            g.rank_tiles = g.r / kGradRanks;
+            for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols - 1) / kGradCols;
+            hipLaunchKernelGGL(adapter_grad_rows_kernel, dim3((unsigned)(g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st, p, g);
+        }
         const int cols = p.r > 64 ? 64 : 128;
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
-        const dim3 grid((unsigned)(8 * g.n * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)));
+        const dim3 grid((unsigned)(8 * (rows ? std::min(g.n, g.T / (kGradRows + 1)) : g.n) * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)));
         if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kGradThreads), 0, st, p, g);
         else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kGradThreads), 0, st, p, g);
         else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kGradThreads), 0, st, p, g);

@@ -233,99 +233,216 @@ struct SmallFrags {
     }
 };
 
-// acc = sum over nk >= 0 stages of this wave's sub-step.  Ends with a barrier: the buffers may be written.
-template <int NRF, int NCF, int FORM, class LB, class LA>
-__device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f32x16_t (&acc)[NRF][NCF]) {
-    using S = SmallTile<NRF, NCF>;
-    constexpr int kRequests = NRF + NCF, kDepth = S::kDepth;   // requests of a wave, a stage
-    const Lane ln;
-    const SmallFrags<NRF, NCF, FORM> fr(ln, lds_addr(smem));
+// Runs nk >= 0 stages through DEPTH buffers of STAGE bytes, the rows' image first, and calls multiply(buffer) for each; a wave has REQUESTS requests a
+// stage.  One barrier a stage.  Ends with a barrier: the buffers may be written.
+template <int DEPTH, int STAGE, int ROWS, int REQUESTS, class LB, class LA, class M>
+__device__ __forceinline__ void pipeline(LB& lb, LA& la, int nk, char* smem, M multiply) {
+    // (one copy of the requests' code: a launch this short waits for its instructions too)
+#pragma unroll 1
+    for (int t = 0; t < min(DEPTH - 1, nk); ++t) {
+        lb.issue(smem + t * STAGE);
+        la.issue(smem + t * STAGE + ROWS);
+    }
+    int at = 0, next = (DEPTH - 1) * STAGE;   // buffers of stages t and t + DEPTH - 1
+    auto step = [&](int& b) { b = b == (DEPTH - 1) * STAGE ? 0 : b + STAGE; };
+    // while full stages are left to request: no branch but the loop's
+    int t = 0;
+    for (int n = lb.left; n > 0; --n, ++t) {
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 2) * REQUESTS) : "memory");   // stage t is here when at most those behind it are on their way
+        __builtin_amdgcn_s_barrier();
+        lb.issue_full(smem + next);   // into the buffer that every wave has read before the barrier
+        la.issue_full(smem + next + ROWS);
+        step(next);
+        multiply(at);
+        step(at);
+    }
+    for (; t < nk; ++t) {
+        if (t + DEPTH - 2 < nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((DEPTH - 2) * REQUESTS) : "memory");
+        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        if (t + DEPTH - 1 < nk) {
+            lb.issue(smem + next);
+            la.issue(smem + next + ROWS);
+            step(next);
+        }
+        multiply(at);
+        step(at);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+}
+template <int NRF, int NCF>
+__device__ __forceinline__ void zero_tile(f32x16_t (&acc)[NRF][NCF]) {
 #pragma unroll
     for (int tf = 0; tf < NRF; ++tf)
 #pragma unroll
         for (int af = 0; af < NCF; ++af)
 #pragma unroll
             for (int v = 0; v < 16; ++v) acc[tf][af][v] = 0.f;
-    // (one copy of the requests' code: a launch this short waits for its instructions too)
-#pragma unroll 1
-    for (int t = 0; t < min(kDepth - 1, nk); ++t) {
-        lb.issue(smem + t * S::kStage);
-        la.issue(smem + t * S::kStage + S::kRowsBytes);
-    }
-    int at = 0, next = (kDepth - 1) * S::kStage;   // buffers of stages t and t + kDepth - 1
-    auto multiply = [&]() {
-        u32x4_t rb[NRF], ra[NCF];
-        fr.read(at, rb, ra);
-        at = at == (kDepth - 1) * S::kStage ? 0 : at + S::kStage;
+}
+template <int NRF, int NCF>
+__device__ __forceinline__ void mfma_tile(const u32x4_t (&rb)[NRF], const u32x4_t (&ra)[NCF], f32x16_t (&acc)[NRF][NCF]) {
 #pragma unroll
-        for (int tf = 0; tf < NRF; ++tf)
+    for (int tf = 0; tf < NRF; ++tf)
 #pragma unroll
-            for (int af = 0; af < NCF; ++af)
-                acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ra[af]), __builtin_bit_cast(bf16x8_t, rb[tf]),
-                                                                      acc[tf][af], 0, 0, 0);
-    };
-    // while full stages are left to request: no branch but the loop's
-    int t = 0;
-    for (int n = lb.left; n > 0; --n, ++t) {
-        asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kDepth - 2) * kRequests) : "memory");   // stage t is here when at most those behind it are on their way
-        __builtin_amdgcn_s_barrier();
-        lb.issue_full(smem + next);   // into the buffer that every wave has read before the barrier
-        la.issue_full(smem + next + S::kRowsBytes);
-        next = next == (kDepth - 1) * S::kStage ? 0 : next + S::kStage;
-        multiply();
-    }
-    for (; t < nk; ++t) {
-        if (t + kDepth - 2 < nk) asm volatile("s_waitcnt vmcnt(%0)" ::"n"((kDepth - 2) * kRequests) : "memory");
-        else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __builtin_amdgcn_s_barrier();
-        if (t + kDepth - 1 < nk) {
-            lb.issue(smem + next);
-            la.issue(smem + next + S::kRowsBytes);
-            next = next == (kDepth - 1) * S::kStage ? 0 : next + S::kStage;
-        }
-        multiply();
-    }
-    __builtin_amdgcn_sched_barrier(0);
-    __syncthreads();
+        for (int af = 0; af < NCF; ++af)
+            acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, ra[af]), __builtin_bit_cast(bf16x8_t, rb[tf]),
+                                                                  acc[tf][af], 0, 0, 0);
 }
 
-// Adds the tiles of waves 0..3 in LDS, wave 0 first, and hands every one of THREADS threads its runs of 8 columns: f(row, column, values).
+// acc = sum over nk >= 0 stages of this wave's sub-step.
+template <int NRF, int NCF, int FORM, class LB, class LA>
+__device__ __forceinline__ void small_loop(LB& lb, LA& la, int nk, char* smem, f32x16_t (&acc)[NRF][NCF]) {
+    using S = SmallTile<NRF, NCF>;
+    const SmallFrags<NRF, NCF, FORM> fr(Lane(), lds_addr(smem));
+    zero_tile(acc);
+    pipeline<S::kDepth, S::kStage, S::kRowsBytes, NRF + NCF>(lb, la, nk, smem, [&](int buffer) {
+        u32x4_t rb[NRF], ra[NCF];
+        fr.read(buffer, rb, ra);
+        mfma_tile(rb, ra, acc);
+    });
+}
+
+// The tiles of waves 0..3 into LDS, and 8 columns of their sum, wave 0 first.
+template <int NRF, int NCF>
+__device__ __forceinline__ void small_put(char* smem, const f32x16_t (&acc)[NRF][NCF]) {
+    constexpr int kPitch = NCF * 128, kWave = kPitch * 32 * NRF;
+    const Lane ln;
+    if (ln.w >= 4) return;
+    char* base = smem + ln.w * kWave;
+#pragma unroll
+    for (int tf = 0; tf < NRF; ++tf)
+#pragma unroll
+        for (int af = 0; af < NCF; ++af)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int row = 32 * tf + ln.l31, piece = 8 * af + 4 * (q >> 1) + 2 * ln.hf + (q & 1);
+                *(f32x4_t*)(base + row * kPitch + ((piece ^ (row & 7)) << 4)) =
+                    f32x4_t{acc[tf][af][4 * q], acc[tf][af][4 * q + 1], acc[tf][af][4 * q + 2], acc[tf][af][4 * q + 3]};
+            }
+}
+template <int NRF, int NCF>
+__device__ __forceinline__ void small_get(const char* smem, int row, int c8, float (&v)[8]) {
+    constexpr int kPitch = NCF * 128, kWave = kPitch * 32 * NRF;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int at = row * kPitch + (((2 * c8 + h) ^ (row & 7)) << 4);
+        f32x4_t s = *(const f32x4_t*)(smem + at);
+#pragma unroll
+        for (int w = 1; w < 4; ++w) {
+            const f32x4_t o = *(const f32x4_t*)(smem + w * kWave + at);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] += o[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[4 * h + j] = s[j];
+    }
+}
+// Both, and f(row, column, values) for every run of 8 columns by one of THREADS threads.
 template <int NRF, int NCF, int THREADS = kSmallThreads, class F>
 __device__ __forceinline__ void small_sum(char* smem, const f32x16_t (&acc)[NRF][NCF], F f) {
-    constexpr int kPitch = NCF * 128, kWave = kPitch * 32 * NRF, kUnits = 128 * NRF * NCF;
-    const Lane ln;
-    if (THREADS == kSmallThreads || ln.w < 4) {
-        char* base = smem + ln.w * kWave;
+    small_put(smem, acc);
+    __syncthreads();
+#pragma unroll 1
+    for (int unit = threadIdx.x; unit < 128 * NRF * NCF; unit += THREADS) {
+        float v[8];
+        small_get<NRF, NCF>(smem, unit / (4 * NCF), unit % (4 * NCF), v);
+        f(unit / (4 * NCF), 8 * (unit % (4 * NCF)), v);
+    }
+}
+
+// ------------------------------------------------------------------ tiles of 128 x 128
+// 8 waves: wave 4 h + 2 r + c has sub-steps 2 h and 2 h + 1 of every stage for a quarter of 64 x 64; the two halves' sums are added at the end.  A
+// flop takes half the operand bytes that it takes in tiles of 64 x 64, and those are what a CU draws into its LDS at some 60 bytes a nanosecond.
+constexpr int kMidThreads = 512;
+struct MidTile {
+    static constexpr int kRowsBytes = 16384, kStage = 32768, kDepth = 4, kLds = kDepth * kStage;
+};
+template <int FORM>
+struct MidFrags {
+    uint32_t b[2], a[2][2];   // of the wave's two sub-steps; KS: a[0] of the two column fragments
+    __device__ __forceinline__ MidFrags(const Lane& ln, uint32_t lds0) {
+        const int half = ln.w >> 2, rh = (ln.w >> 1) & 1, ch = ln.w & 1, kh = ln.hf;
+        const uint32_t a0 = lds0 + MidTile::kRowsBytes;
 #pragma unroll
-        for (int tf = 0; tf < NRF; ++tf)
+        for (int s = 0; s < 2; ++s) {
+            const int kk = 2 * half + s, n = swap23(ln.l31);
+            b[s] = lds0 + (64 * rh + ln.l31) * 128 + (((2 * kk + kh) ^ ((ln.l31 >> 1) & 7)) << 4);
+            if (FORM == kKc) {
+                a[s][0] = a0 + (64 * ch + n) * 128 + (((2 * kk + kh) ^ ((n >> 1) & 7)) << 4);
+                a[s][1] = 0;
+            }
+        }
+        if (FORM != kKc) {
+            const int g = (ln.l >> 4) & 1, e = (ln.l & 15) >> 2, q = ln.l & 3, sq = ((q & 1) << 1) | (q >> 1);
 #pragma unroll
-            for (int af = 0; af < NCF; ++af)
+            for (int af = 0; af < 2; ++af) {
+                a[0][af] = a0 + (32 * half + 8 * kh + e) * 256 + (((8 * ch + 4 * af + 2 * g + (sq >> 1)) ^ (e << 2)) << 4) + (sq & 1) * 8;
+                a[1][af] = 0;
+            }
+        }
+    }
+    template <int S>
+    __device__ __forceinline__ void read(uint32_t off, u32x4_t (&rb)[2], u32x4_t (&ra)[2]) const {
+        const uint32_t bo = b[S] + off;
+        if constexpr (FORM == kKc) {
+            const uint32_t ao = a[S][0] + off;
+            asm volatile("ds_read_b128 %0, %4\n ds_read_b128 %1, %4 offset:4096\n ds_read_b128 %2, %5\n ds_read_b128 %3, %5 offset:4096\n"
+                         "s_waitcnt lgkmcnt(0)" : "=&v"(rb[0]), "=&v"(rb[1]), "=&v"(ra[0]), "=&v"(ra[1]) : "v"(bo), "v"(ao) : "memory");
+        } else {
+            const uint32_t a0 = a[0][0] + off, a1 = a[0][1] + off;
+            u32x2_t l0, h0, l1, h1;
+            asm volatile("ds_read_b128 %0, %6\n ds_read_b128 %1, %6 offset:4096\n"
+                         "ds_read_b64_tr_b16 %2, %7 offset:%9\n ds_read_b64_tr_b16 %3, %7 offset:%10\n"
+                         "ds_read_b64_tr_b16 %4, %8 offset:%9\n ds_read_b64_tr_b16 %5, %8 offset:%10\n s_waitcnt lgkmcnt(0)"
+                         : "=&v"(rb[0]), "=&v"(rb[1]), "=&v"(l0), "=&v"(h0), "=&v"(l1), "=&v"(h1)
+                         : "v"(bo), "v"(a0), "v"(a1), "n"(S * 4096), "n"(S * 4096 + 1024) : "memory");
+            ra[0] = u32x4_t{l0[0], l0[1], h0[0], h0[1]};
+            ra[1] = u32x4_t{l1[0], l1[1], h1[0], h1[1]};
+        }
+    }
+};
+template <int FORM, class LB, class LA>
+__device__ __forceinline__ void mid_loop(LB& lb, LA& la, int nk, char* smem, f32x16_t (&acc)[2][2]) {
+    const MidFrags<FORM> fr(Lane(), lds_addr(smem));
+    zero_tile(acc);
+    pipeline<MidTile::kDepth, MidTile::kStage, MidTile::kRowsBytes, 4>(lb, la, nk, smem, [&](int buffer) {
+        u32x4_t rb[2], ra[2];
+        fr.template read<0>(buffer, rb, ra);
+        mfma_tile(rb, ra, acc);
+        fr.template read<1>(buffer, rb, ra);
+        mfma_tile(rb, ra, acc);
+    });
+}
+// The two halves' sums, as small_sum.
+template <class F>
+__device__ __forceinline__ void mid_sum(char* smem, const f32x16_t (&acc)[2][2], F f) {
+    constexpr int kPitch = 512, kHalf = 128 * kPitch;
+    {
+        const Lane ln;
+        char* base = smem + (ln.w >> 2) * kHalf;
+#pragma unroll
+        for (int tf = 0; tf < 2; ++tf)
+#pragma unroll
+            for (int af = 0; af < 2; ++af)
 #pragma unroll
                 for (int q = 0; q < 4; ++q) {
-                    const int row = 32 * tf + ln.l31, piece = 8 * af + 4 * (q >> 1) + 2 * ln.hf + (q & 1);
+                    const int row = 64 * ((ln.w >> 1) & 1) + 32 * tf + ln.l31, piece = 16 * (ln.w & 1) + 8 * af + 4 * (q >> 1) + 2 * ln.hf + (q & 1);
                     *(f32x4_t*)(base + row * kPitch + ((piece ^ (row & 7)) << 4)) =
                         f32x4_t{acc[tf][af][4 * q], acc[tf][af][4 * q + 1], acc[tf][af][4 * q + 2], acc[tf][af][4 * q + 3]};
                 }
     }
     __syncthreads();
-#pragma unroll
-    for (int u = 0; u < (kUnits + THREADS - 1) / THREADS; ++u) {
-        const int unit = u * THREADS + (int)threadIdx.x;
-        if (kUnits % THREADS != 0 && unit >= kUnits) break;
-        const int row = unit / (4 * NCF), c8 = unit % (4 * NCF);
+#pragma unroll 1
+    for (int unit = threadIdx.x; unit < 2048; unit += kMidThreads) {
+        const int row = unit >> 4, c8 = unit & 15;
         float v[8];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
             const int at = row * kPitch + (((2 * c8 + h) ^ (row & 7)) << 4);
-            f32x4_t s = *(const f32x4_t*)(smem + at);
+            const f32x4_t s = *(const f32x4_t*)(smem + at), o = *(const f32x4_t*)(smem + kHalf + at);
 #pragma unroll
-            for (int w = 1; w < 4; ++w) {
-                const f32x4_t o = *(const f32x4_t*)(smem + w * kWave + at);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) s[j] += o[j];
-            }
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[4 * h + j] = s[j];
+            for (int j = 0; j < 4; ++j) v[4 * h + j] = s[j] + o[j];
         }
         f(row, 8 * c8, v);
     }

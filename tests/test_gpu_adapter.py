@@ -33,6 +33,7 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     (513, 64, 64, 8, 1, "one", 0, "bf16"), (513, 8, 16, 8, 600, "each", 0, "f32"), (600, 328, 200, 24, 5, "outside", 8, "bf16"),
     (1011, 136, 72, 16, 256, "scattered", 0, "bf16"), (640, 1000, 520, 64, 3, "packed", 64, "f32"), (1021, 264, 712, 128, 2, "scattered", 0, "bf16"),
     (1000, 200, 104, 40, 1024, "scattered", 0, "bf16"), (2049, 512, 128, 8, 4, "packed", 0, "f32"), (777, 72, 640, 96, 6, "none", 0, "bf16"),
+    (900, 264, 392, 16, 300, "each", 0, "bf16"), (1500, 2056, 136, 64, 500, "scattered", 0, "f32"), (2000, 136, 3000, 8, 30, "packed", 0, "bf16"),
     # tiles of 128 and of 256 rows, in each direction
     (4100, 136, 1032, 16, 9, "packed", 0, "bf16"), (4100, 1032, 72, 16, 300, "scattered", 0, "bf16"), (8200, 72, 1544, 24, 6, "scattered", 8, "bf16"),
     (8200, 1544, 136, 64, 5, "packed", 0, "f32"), (16500, 584, 1032, 8, 40, "scattered", 0, "f32"), (16500, 1032, 584, 128, 3, "packed", 0, "bf16"),
