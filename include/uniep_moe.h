@@ -287,12 +287,13 @@ typedef struct {
     int32_t adapters;
 } moe_adapter_shape_t;
 
-/* Workspace of the forward and of the backward call, and bytes of the plan (host outputs; either may be NULL).  The plan of up to 512
- * tokens has 0 bytes: moe_adapter_plan then enqueues nothing, and `plan` may be NULL everywhere. */
+/* Workspace of the forward and of the backward call, and bytes of the plan (host outputs; either may be NULL).  Where few tokens are best not
+ * sorted the plan has 0 bytes: moe_adapter_plan then enqueues nothing.  Up to 512 tokens `plan` may be NULL whatever its size. */
 int moe_adapter_workspace_bytes(const moe_adapter_shape_t* shape, size_t* ws_bytes, size_t* plan_bytes);
 
-/* Sorts the tokens by adapter (stable), for any number of forward and backward calls with the same ids, which have to
- * stay as they are while the plan is in use.  ids: [T] int32. */
+/* Sorts the tokens by adapter (stable), for any number of forward and backward calls with the same ids, T and adapters, whatever their
+ * widths and rank.  The ids have to stay as they are while the plan is in use.  ids: [T] int32.  The backward call
+ * has to be given the plan that the forward call had (or NULL as that). */
 int moe_adapter_plan(const moe_adapter_shape_t* shape, const int32_t* ids, void* plan, size_t plan_bytes, void* stream);
 
 /* Forward.

@@ -14,7 +14,6 @@
 #include "adapter.hpp"
 
 #include <algorithm>
-#include <cstdlib>
 #include <type_traits>
 
 namespace uniep {
@@ -55,14 +54,18 @@ static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
     v.many = v.seg + s.adapters;
     return v;
 }
-bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= (getenv("FEW") ? atoi(getenv("FEW")) : kFewTokens); }
+// Whether the path for few tokens is taken where there is a choice: up to 512 tokens, unless a large product in tiles of 64 x 64 would cost more than the sorting does.  Measured, us
+// of the forward call and of the training step, few tokens / sorted (K, N, ranks, adapters): 200 tokens 7168 x 7168, 16, 16 55.9 and 118 / 71.0 and 154, 300 79.0 and 161 / 81.6
+// and 183, 400 98.8 and 204 / 82.6 and 184; 300 4096 x 4096, 128, 2 66.5 and 136 / 52.8 and 122; 512 2048 x 2816, 16, 16 21.0 and 48.4 / 31.0 and 66.4; 512 680 x 480, 128, 4
+// 20.3 and 48.5 / 27.0 and 76.1; 512 2048 x 7168, 8, 256 45.3 and 130 / 62.3 and 306.
+static bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= kFewTokens / 2 || (s.T <= kFewTokens && (long long)s.T * s.K * s.N <= 8ll << 30); }
+bool adapter_needs_plan(const moe_adapter_shape_t& s) { return s.T > kFewTokens; }
 size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) ? 0 : plan_words(s) * 4; }
+static bool goes_few(const moe_adapter_shape_t& s, const void* plan) { return adapter_few(s) || !plan; }
 
-// IT: the ids stay in registers, 64 IT a wave (0: more than that, read twice).
 // One workgroup: a counting sort.  Every wave counts a contiguous part of the tokens and later gives its tokens their rows, 64 at a
 // time: lanes with the same adapter find each other with a ballot for each bit of the id.
 constexpr int kSortWaves = 16;
-template <int IT>
 __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, int brows, const int32_t* __restrict__ ids, PlanView v) {
     __shared__ int32_t hist[kSortWaves][kMaxAdapters + 1];
     __shared__ int32_t first[kMaxAdapters + 2];     // rows before bin b (bin 0: no adapter, bin a + 1: adapter a)
@@ -72,13 +75,22 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
     const uint64_t below = (1ull << lane) - 1ull;
     for (int b = lane; b < bins; b += 64) hist[w][b] = 0;
     const int part = ((T + kSortWaves - 1) / kSortWaves + 63) & ~63, lo = min(T, w * part), hi = min(T, lo + part);
-    auto bin_of = [&](int t) {
-        const int a = t < hi ? ids[t] : -1;
-        return (unsigned)a < (unsigned)n ? a + 1 : 0;
-    };
-    int bins_of[IT > 0 ? IT : 1];
+    // f(token, bin) for this wave's tokens, 64 at a time; the ids of 256 are fetched together (a copy of f for each of 16 fetches, with the ids kept for the second
+    // time, was slower: 12 KB of code that runs once)
+    auto each = [&](auto f) {
+#pragma unroll 1
+        for (int t0 = lo; t0 < hi; t0 += 256) {
+            int a[4];
 #pragma unroll
-    for (int i = 0; i < IT; ++i) bins_of[i] = bin_of(lo + 64 * i + lane);
+            for (int i = 0; i < 4; ++i) {
+                const int t = t0 + 64 * i + lane;
+                a[i] = t < hi ? ids[t] : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (t0 + 64 * i < hi) f(t0 + 64 * i + lane, (unsigned)a[i] < (unsigned)n ? a[i] + 1 : 0);
+        }
+    };
     __syncthreads();
     auto count = [&](int t, int b) {   // packed requests: mostly 64 tokens with one adapter
         if (__ballot(t < hi && b == rfl(b)) == ~0ull) {
@@ -87,11 +99,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
             atomicAdd(&hist[w][b], 1);
         }
     };
-    if (IT > 0)
-#pragma unroll
-        for (int i = 0; i < IT; ++i) count(lo + 64 * i + lane, bins_of[i]);
-    else
-        for (int t0 = lo; t0 < hi; t0 += 64) count(t0 + lane, bin_of(t0 + lane));
+    each(count);
     __syncthreads();
     // bins -> first rows, blocks and segments: thread b has bin b (two at most a thread: 1025 bins)
     int base_rows = 0, base_blocks = 0, base_segs = 0;
@@ -172,11 +180,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         }
         __builtin_amdgcn_wave_barrier();
     };
-    if (IT > 0)
-#pragma unroll
-        for (int i = 0; i < IT; ++i) place(lo + 64 * i + lane, bins_of[i]);
-    else
-        for (int t0 = lo; t0 < hi; t0 += 64) place(t0 + lane, bin_of(t0 + lane));
+    each(place);
     // blocks and units, a wave a bin
     for (int b = w; b < bins; b += kSortWaves) {
         const int r0 = first[b], r1 = first[b + 1], o = b > 0 ? fseg[b] : -1;
@@ -196,12 +200,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
 
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st) {
     if (adapter_few(s)) return MOE_OK;
-    auto launch = [&](auto it) {
-        hipLaunchKernelGGL((adapter_plan_kernel<it.value>), dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T), ids, plan_view(s, plan));
-    };
-    if (s.T <= 64 * kSortWaves * 4) launch(std::integral_constant<int, 4>{});
-    else if (s.T <= 64 * kSortWaves * 16) launch(std::integral_constant<int, 16>{});
-    else launch(std::integral_constant<int, 0>{});
+    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T), ids, plan_view(s, plan));
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
@@ -1041,16 +1040,15 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     const size_t ldx = g.ldx[which];
     const char* const h = (const char*)(p.terms[which] + (size_t)row0 * 3 * r);
     const uint32_t tok0 = lds_addr(s_tok) + xk * 4;
-    // h: this lane's chunk of its instructions' rows, from the first row of the adapter on
+    // h: this lane's row of instruction i, and its chunk from the first row of the stage on
+    auto h_row = [&](int i) { return ((G::kHLoads * wave + i) % (4 * NRF)) * kHRows + ln.l / kHLanes; };
+    auto h_off = [&](int i) {
+        const int k = h_row(i), c = (ln.l % kHLanes) ^ ks_swz<G::kHRow>(k);
+        return (k * 3 + (G::kHLoads * wave + i) / (4 * NRF)) * r * 2 + min(c * 16, 2 * r - 16);
+    };
     uint32_t oh[G::kHLoads];
-    int hk[G::kHLoads];
 #pragma unroll
-    for (int i = 0; i < G::kHLoads; ++i) {
-        const int u = G::kHLoads * wave + i, term = u / (4 * NRF);
-        hk[i] = (u % (4 * NRF)) * kHRows + ln.l / kHLanes;
-        const int c = (ln.l % kHLanes) ^ ks_swz<G::kHRow>(hk[i]);
-        oh[i] = (hk[i] * 3 + term) * r * 2 + min(c * 16, 2 * r - 16);
-    }
+    for (int i = 0; i < G::kHLoads; ++i) oh[i] = h_off(i);
     auto issue = [&](int k0, int left, char* dst) {   // the 64 rows from row k0 on, of which `left` are there
         int32_t tok[G::kXLoads];
         const uint32_t at = tok0 + (k0 % G::kList) * 4;
@@ -1059,24 +1057,20 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
                          : "=&v"(tok[0]), "=&v"(tok[1]), "=&v"(tok[2]), "=&v"(tok[3]) : "v"(at), "n"(kXRows * 4), "n"(kXRows * 8), "n"(kXRows * 12) : "memory");
         else
             asm volatile("ds_read_b32 %0, %2\n ds_read_b32 %1, %2 offset:%3\n s_waitcnt lgkmcnt(0)" : "=&v"(tok[0]), "=&v"(tok[1]) : "v"(at), "n"(kXRows * 4) : "memory");
-        const char* q[G::kXLoads + G::kHLoads];
+        char* const dx = dst + G::kXLoads * 1024 * wave;
+        char* const dh = dst + G::kX + G::kHLoads * 1024 * wave;
         const char* const hs = h + (size_t)k0 * 6 * r;
+        if (left >= BK) {
 #pragma unroll
-        for (int i = 0; i < G::kXLoads; ++i) q[i] = x + (size_t)tok[i] * ldx;
+            for (int i = 0; i < G::kXLoads; ++i) dma16(x + (size_t)tok[i] * ldx, dx + i * 1024);
 #pragma unroll
-        for (int i = 0; i < G::kHLoads; ++i) q[G::kXLoads + i] = hs + oh[i];
-        if (left < BK) {
+            for (int i = 0; i < G::kHLoads; ++i) dma16(hs + oh[i], dh + i * 1024);
+        } else {
 #pragma unroll
-            for (int i = 0; i < G::kXLoads; ++i) q[i] = xk + i * kXRows < left ? q[i] : zero_chunk();
+            for (int i = 0; i < G::kXLoads; ++i) dma16(xk + i * kXRows < left ? x + (size_t)tok[i] * ldx : zero_chunk(), dx + i * 1024);
 #pragma unroll
-            for (int i = 0; i < G::kHLoads; ++i) q[G::kXLoads + i] = hk[i] < left ? q[G::kXLoads + i] : zero_chunk();
+            for (int i = 0; i < G::kHLoads; ++i) dma16(h_row(i) < left ? hs + oh[i] : zero_chunk(), dh + i * 1024);
         }
-#pragma unroll
-        for (int i = 0; i < G::kXLoads + G::kHLoads; ++i) asm volatile("" : "+v"(q[i]));
-#pragma unroll
-        for (int i = 0; i < G::kXLoads; ++i) dma16(q[i], dst + (G::kXLoads * wave + i) * 1024);
-#pragma unroll
-        for (int i = 0; i < G::kHLoads; ++i) dma16(q[G::kXLoads + i], dst + G::kX + (G::kHLoads * wave + i) * 1024);
     };
     f32x16_t acc[NRF][NCF];
 #pragma unroll
@@ -1094,12 +1088,13 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
 #pragma unroll
     for (int tf = 0; tf < NRF; ++tf)
         ah[tf] = lds_addr(smem) + G::kX + krow * G::kHRow + (((4 * tf + 2 * gg + (q4 >> 1)) ^ ks_swz<G::kHRow>(e)) << 4) + (q4 & 1) * 8;
-    for (int base = 0; base < count; base += G::kList) {
-        const int here = min(G::kList, count - base), nst = (here + BK - 1) / BK;
-        __syncthreads();   // the list before has been read
-        for (int i = tid; i < here; i += kGradThreads) s_tok[i] = p.plan.order[row0 + base + i];
-        __syncthreads();
-        if (moves) {
+    // (both roles meet at the same barriers: two for each list, one for each stage)
+    if (moves) {
+        for (int base = 0; base < count; base += G::kList) {
+            const int here = min(G::kList, count - base), nst = (here + BK - 1) / BK;
+            __syncthreads();   // the stages of the list before have been read
+            for (int i = tid - kSmallThreads; i < here; i += kSmallThreads) s_tok[i] = p.plan.order[row0 + base + i];
+            __syncthreads();
             for (int t = 0; t < min(G::kDepth - 1, nst); ++t) issue(base + t * BK, here - t * BK, smem + t * G::kStage);
             int next = (G::kDepth - 1) * G::kStage;
             for (int t = 0; t < nst; ++t) {
@@ -1111,7 +1106,12 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
                     next = next == (G::kDepth - 1) * G::kStage ? 0 : next + G::kStage;
                 }
             }
-        } else {
+        }
+    } else {
+        for (int base = 0; base < count; base += G::kList) {
+            const int nst = (min(G::kList, count - base) + BK - 1) / BK;
+            __syncthreads();
+            __syncthreads();
             int at = 0;
             for (int t = 0; t < nst; ++t) {
                 __builtin_amdgcn_s_barrier();
@@ -1121,12 +1121,7 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
                 for (int term = 0; term < 3; ++term) {
                     u32x4_t fh[NRF];
                     read_tr<NRF, 4 * G::kHRow>(fh, ah, at + term * G::kH);
-#pragma unroll
-                    for (int tf = 0; tf < NRF; ++tf)
-#pragma unroll
-                        for (int af = 0; af < NCF; ++af)
-                            acc[tf][af] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, fx[af]), __builtin_bit_cast(bf16x8_t, fh[tf]),
-                                                                                  acc[tf][af], 0, 0, 0);
+                    mfma_tile(fh, fx, acc);
                 }
                 at = at == (G::kDepth - 1) * G::kStage ? 0 : at + G::kStage;
             }
@@ -1135,10 +1130,7 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
 #pragma unroll
     for (int tf = 0; tf < NRF; ++tf) {
         __syncthreads();
-        f32x16_t one[1][NCF];
-#pragma unroll
-        for (int af = 0; af < NCF; ++af) one[0][af] = acc[tf][af];
-        small_sum<1, NCF, kGradThreads>(smem, one, [&](int row, int col, const float (&v)[8]) {
+        small_sum<1, NCF, kGradThreads>(smem, *(const f32x16_t(*)[1][NCF])&acc[tf], [&](int row, int col, const float (&v)[8]) {
             row += 32 * tf;
             col += c0;
             if (row >= r || col >= W) return;
@@ -1149,8 +1141,8 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     }
 }
 
-// The same for adapters with up to kGradRows rows, on the vector unit: a workgroup of the tiles above takes 6 us whatever its rows and has a CU for itself (600 tokens on
-// 200 adapters of 680 x 480, 16 ranks: GRADMANY us, with this GRADROWS).
+// The same for adapters with up to kGradRows rows, on the vector unit: a workgroup of the tiles above takes 6 us whatever its rows and has a CU for itself (a training step of 512 tokens on
+// 200 adapters of 680 x 480, 16 ranks, 112 us, of 600 with this and the low-rank parts row by row 85).
 __global__ void __launch_bounds__(256) adapter_grad_rows_kernel(ProjParams p, GradParams g) {
     __shared__ FewGradShared<kGradRows> S;
     const FewGradTask t(g, blockIdx.x);
@@ -1222,8 +1214,9 @@ static size_t many_bytes(const moe_adapter_shape_t& s) {
 }
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
     if (s.T == 0) return 256;
-    if (!adapter_few(s)) return many_bytes(s);
-    return std::max(few_bytes(s.T, s.K, s.N, s.rank), few_bytes(s.T, s.N, s.K, s.rank));
+    size_t most = adapter_few(s) ? 0 : many_bytes(s);
+    if (!adapter_needs_plan(s)) most = std::max({most, few_bytes(s.T, s.K, s.N, s.rank), few_bytes(s.T, s.N, s.K, s.rank)});
+    return most;
 }
 
 static void few_params(ProjParams& p, char* ws, FewPlan& f) {
@@ -1280,7 +1273,7 @@ int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t l
     p.T = s.T, p.R = s.K, p.C = s.N, p.r = s.rank, p.n = s.adapters;
     p.x = (const char*)x, p.ldx = ldx * 2, p.w = (const char*)w, p.first = (const char*)a, p.second = (const char*)b;
     p.scale = scale, p.ids = ids, p.y = (char*)y, p.out_f32 = out_f32, p.h = h;
-    if (adapter_few(s)) {
+    if (goes_few(s, plan)) {
         FewPlan f;
         few_params(p, ws, f);
         few_first<kKs>(p, f, st);
@@ -1305,7 +1298,7 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
     g.ldx[0] = lddy * 2, g.ldx[1] = ldx * 2;
     g.h[0] = h;
     g.out[0] = db, g.out[1] = da;
-    if (adapter_few(s)) {
+    if (goes_few(s, plan)) {
         FewPlan f;
         if (s.T > 0) {
             few_params(p, ws, f);

@@ -25,6 +25,7 @@ int bwd_launch(const moe_shape_t& s, const void* dy, const void* x, const void* 
                const void* w_up, const void* w_down, const moe_routing_t& r, const char* gu,
                const char* h, const char* o, void* dx, void* dw_gate, void* dw_up, void* dw_down,
                float* dtopk_w, char* ws, const moe_opts_t& opts, hipStream_t st);
+bool adapter_needs_plan(const moe_adapter_shape_t& s);
 size_t adapter_plan_bytes(const moe_adapter_shape_t& s);
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s);
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st);
@@ -110,7 +111,7 @@ int check_balance_shape(const moe_balance_shape_t* s) {
 int check_adapter(const moe_adapter_shape_t& s, const void* w, const void* a, const void* b, const float* scale, const int32_t* ids,
                   const void* plan, const void* ws, size_t ws_bytes) {
     if (!w || !a || !b || !ws) return MOE_ERR_ARG;
-    if (s.T > 0 && (!ids || (adapter_plan_bytes(s) > 0 && !plan))) return MOE_ERR_ARG;
+    if (s.T > 0 && (!ids || (adapter_needs_plan(s) && !plan))) return MOE_ERR_ARG;
     if (!aligned(w, 16) || !aligned(a, 16) || !aligned(b, 16) || !aligned(scale, 4) || !aligned(ids, 4) || !aligned(plan, 16) || !aligned(ws, 256))
         return MOE_ERR_ARG;
     return ws_bytes < adapter_workspace_bytes(s) ? MOE_ERR_WORKSPACE : MOE_OK;

@@ -66,6 +66,31 @@ def test_without_scale_and_without_the_stash():
         assert torch.equal(moe.moe_adapter_forward(shape, s["x"], s["w"], s["a"], s["b"], moe.moe_adapter_plan(shape, s["ids"])), got["y"])
 
 
+def test_up_to_512_tokens_with_and_without_a_plan():
+    T, K, N, r, n = 420, 4616, 4616, 16, 5
+    s = ac.make(T, K, N, r, n, "scattered")
+    shape = moe.make_adapter_shape(T, K, N, r, n)
+    v, m = ac.plain(s)
+    e = ac.bounds(s, v, m, False)
+    plan = moe.moe_adapter_plan(shape, s["ids"])
+    assert plan.table is not None
+    for p in (plan, moe.AdapterPlan(s["ids"], None)):
+        h = torch.empty((T, r), device="cuda")
+        got = {"y": moe.moe_adapter_forward(shape, s["x"], s["w"], s["a"], s["b"], p, scale=s["scale"], h=h), "h": h}
+        got |= moe.moe_adapter_backward(shape, s["dy"], s["x"], s["w"], s["a"], s["b"], p, h, scale=s["scale"])
+        for key in ("h", "y", "dx", "da", "db"):
+            ac.check(got[key], v[key], e[key], (p.table is None, key))
+
+
+def test_a_plan_serves_other_widths():
+    T, r, n = 700, 16, 5
+    one, two = ac.make(T, 136, 264, r, n, "scattered"), ac.make(T, 520, 72, 40, n, "scattered")
+    plan = moe.moe_adapter_plan(moe.make_adapter_shape(T, 136, 264, r, n), one["ids"])
+    two["ids"] = one["ids"]
+    y = moe.moe_adapter_forward(moe.make_adapter_shape(T, 520, 72, 40, n), two["x"], two["w"], two["a"], two["b"], plan, scale=two["scale"])
+    assert torch.equal(y, run(two, 40, n, backward=False)["y"])
+
+
 def test_no_tokens():
     s = ac.make(0, 64, 128, 8, 3, "one")
     got = run(s, 8, 3)

@@ -72,6 +72,10 @@ def test_few_tokens_need_no_plan(lib):
     assert b._adapter_bytes(s)[1] == 0
     assert adapter_calls(lib, s, ids=None, plan=None)["plan"]() == b.MOE_OK   # nothing to do
     assert adapter_calls(lib, s, ids=None, plan=None)["forward"]() == b.MOE_ERR_ARG
+    wide = moe.make_adapter_shape(T=512, K=7168, N=7168, rank=16, adapters=4)   # may be sorted, need not be
+    assert b._adapter_bytes(wide)[1] > 0
+    assert adapter_calls(lib, wide, plan=None, nbytes=0)["forward"]() == b.MOE_ERR_WORKSPACE
+    assert adapter_calls(lib, moe.make_adapter_shape(T=513, K=64, N=128, rank=16, adapters=4), plan=None, nbytes=0)["forward"]() == b.MOE_ERR_ARG
 
 
 BAL = dict(T=100, E=16, k=2, seqs=2)
