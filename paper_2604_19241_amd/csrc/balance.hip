@@ -49,16 +49,20 @@ struct BalParams {
 };
 
 __device__ __forceinline__ int seq_begin(const BalParams& p, int s) { return p.offsets ? min(max(p.offsets[s], 0), p.T) : s > 0 ? p.T : 0; }
-// last sequence that begins at or before token t
+// Last sequence that begins at or before token t, the same in the whole wave, whose lanes look at 64 of them at a time: one load for up to 64 sequences, two
+// for 4096 (a search by halves waits for six loads one after the other for 64).
 __device__ __forceinline__ int seq_of(const BalParams& p, int t) {
     if (!p.offsets) return 0;
-    int lo = 0, hi = p.S - 1;
-    while (lo < hi) {
-        const int mid = (lo + hi + 1) >> 1;
-        if (p.offsets[mid] <= t) lo = mid;
-        else hi = mid - 1;
+    const int lane = threadIdx.x & 63;
+    int lo = 0, n = p.S;   // it is one of lo .. lo + n - 1
+    while (n > 1) {
+        const int step = (n + 63) >> 6, i = lo + lane * step;
+        const int before = __popcll(__ballot(lane * step < n && p.offsets[min(i, p.S - 1)] <= t));
+        const int at = max(before - 1, 0) * step;
+        lo += at;
+        n = min(step, n - at);
     }
-    return lo;
+    return rfl(lo);
 }
 
 // G lanes share a token, each with 4 NV of its experts: runs of 4 where rows are 16-byte aligned, else every G-th.
@@ -104,10 +108,20 @@ struct TokenLanes {
 };
 typedef __attribute__((ext_vector_type(4))) int32_t i32x4_t;
 
+__device__ __forceinline__ void write_losses(const BalParams& p, double b, double z, int n) {   // b, z: the sums over all sequences and tokens
+    const double per = 1.0 / (n > 0 ? n : 1), balance = p.E * per * b;
+    z *= per;
+    p.tokens[p.S] = n;
+    p.loss[0] = (float)(p.balance_coef * balance + p.z_coef * z);
+    p.loss[1] = (float)balance;
+    p.loss[2] = (float)z;
+}
+
+// With one workgroup (one_launch) it writes the results itself, else the parts that balance_sum_kernel adds.
 template <int G, int NV, bool VEC>
 __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams p) {
     using L = TokenLanes<G, NV, VEC>;
-    constexpr int kMost = 4 * G * NV, kGroups = 64 / G, kU = NV == 1 ? 4 : 1;
+    constexpr int kMost = 4 * G * NV, kGroups = 64 / G, kU = NV == 1 ? 4 : 1, kSlots = (kMaxTopK + G - 1) / G;
     __shared__ float s_p[kBalWaves][kMost];
     __shared__ int32_t s_c[kMost];
     __shared__ float s_z[kBalWaves];
@@ -123,15 +137,12 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
         if (a >= b) continue;
         for (int e = tid; e < E; e += kBalThreads) s_c[e] = 0;
         __syncthreads();
-        for (int i = tid; i < (b - a) * p.k; i += kBalThreads) {
-            const int t = a + i / p.k, e = p.idx[(size_t)a * p.k + i];
-            if ((unsigned)e < (unsigned)E && (!p.mask || p.mask[t])) atomicAdd(&s_c[e], 1);
-        }
         float sums[L::kValues] = {}, z = 0.f;
         int n = 0;
         // U tokens a turn: their loads are on their way together
         for (int t0 = a + w * kGroups + lane / G; t0 < b; t0 += kU * kBalWaves * kGroups) {
             float x[kU][L::kValues];
+            int slot[kU][kSlots];
             bool keep[kU];
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
@@ -140,7 +151,12 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
             }
 #pragma unroll
             for (int u = 0; u < kU; ++u)
-                if (keep[u]) ln.template load<f32x4_t>(p.logits + (size_t)(t0 + u * kBalWaves * kGroups) * E, E, -INFINITY, x[u]);
+                if (keep[u]) {
+                    const size_t t = t0 + u * kBalWaves * kGroups;
+                    ln.template load<f32x4_t>(p.logits + t * E, E, -INFINITY, x[u]);
+#pragma unroll
+                    for (int i = 0; i < kSlots; ++i) slot[u][i] = i * G + ln.g < p.k ? p.idx[t * p.k + i * G + ln.g] : -1;
+                }
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
                 const int t = t0 + u * kBalWaves * kGroups;
@@ -156,6 +172,9 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
                         x[u][v] = ln.expert(v) < E ? __expf(x[u][v] - m) : 0.f;
                         q += x[u][v];
                     }
+#pragma unroll
+                    for (int i = 0; i < kSlots; ++i)
+                        if ((unsigned)slot[u][i] < (unsigned)E) atomicAdd(&s_c[slot[u][i]], 1);
                     const float total = L::sum(q), inv = 1.f / total;
 #pragma unroll
                     for (int v = 0; v < L::kValues; ++v) sums[v] += x[u][v] * inv;
@@ -185,6 +204,26 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
             }
         }
         __syncthreads();
+        if (gridDim.x == 1 && p.S == 1) {
+            __shared__ double s_b[kBalWaves];
+            n = s_n[0] + s_n[1] + s_n[2] + s_n[3];
+            double bal = 0.0;
+            for (int e = tid; e < E; e += kBalThreads) {
+                const float sum = ((s_p[0][e] + s_p[1][e]) + s_p[2][e]) + s_p[3][e];
+                p.prob_sums[e] = sum;
+                p.counts[e] = s_c[e];
+                bal += (double)s_c[e] * sum;
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) bal += __shfl_xor(bal, o);
+            if (lane == 0) s_b[w] = bal;
+            __syncthreads();
+            if (tid == 0) {
+                p.tokens[0] = n;
+                write_losses(p, n > 0 ? (((s_b[0] + s_b[1]) + s_b[2]) + s_b[3]) / ((double)p.k * n) : 0.0, ((double)s_z[0] + s_z[1]) + s_z[2] + s_z[3], n);
+            }
+            return;
+        }
         const size_t slot = (size_t)c + s;
         for (int e = tid; e < E; e += kBalThreads) {
             p.part_p[slot * E + e] = ((s_p[0][e] + s_p[1][e]) + s_p[2][e]) + s_p[3][e];
@@ -295,14 +334,7 @@ __global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p, i
             n += s_i[1][i];
         }
     }
-    if (tid == 0) {
-        const double per = 1.0 / (n > 0 ? n : 1), balance = p.E * per * b;
-        z *= per;
-        p.tokens[p.S] = n;
-        p.loss[0] = (float)(p.balance_coef * balance + p.z_coef * z);
-        p.loss[1] = (float)balance;
-        p.loss[2] = (float)z;
-    }
+    if (tid == 0) write_losses(p, b, z, n);
 }
 
 // The gates' part goes to its experts through a row of LDS that is all zeros between tokens: the lanes of the slots add to it and clear their
@@ -322,7 +354,7 @@ __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams
     if (p.w)
 #pragma unroll
         for (int v = 0; v < L::kValues; ++v) row[ln.expert(v)] = 0.f;
-    int s = -1, end = 0;
+    int s = seq_of(p, min(c0 + w * kGroups, p.T - 1)), end = -1;   // (of the wave's first token; then every group goes on by itself)
     float f[L::kValues];   // cb f[s]
     for (int t0 = c0 + w * kGroups + lane / G; t0 < c1; t0 += kU * kBalWaves * kGroups) {
         float d[kU][L::kValues], lse[kU], g[kU][kSlots], dw[kU][kSlots];
@@ -350,9 +382,8 @@ __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams
             const int t = t0 + u * kBalWaves * kGroups;
             if (t >= c1) break;
             if (lse[u] != -INFINITY) {
-                if (s < 0 || t >= end) {
-                    s = seq_of(p, t);
-                    end = seq_begin(p, s + 1);
+                if (t >= end) {
+                    while ((end = seq_begin(p, s + 1)) <= t && s + 1 < p.S) ++s;
                     const float scale = cb / ((float)p.k * (float)max(p.tokens[s], 1));
                     int32_t cnt[L::kValues];
                     ln.template load<i32x4_t>(p.counts + (size_t)s * E, E, 0, cnt);
@@ -423,14 +454,21 @@ __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams
 }
 
 // ------------------------------------------------------------------ launches
+// Whether one workgroup is the faster way: one sequence, and up to four turns of its four waves (with G lanes a token a wave takes 64 / G tokens, four times, a
+// turn).  256 tokens, 8 experts: 4.3 us, 8.4 in two launches.
+static bool one_launch(const moe_balance_shape_t& s) {
+    const int lanes = s.E <= 8 ? 2 : s.E <= 32 ? 8 : s.E <= 64 ? 16 : s.E <= 128 ? 32 : 64;
+    return s.seqs == 1 && s.T > 0 && s.E <= 256 && s.T <= 4 * (64 / lanes) * 4 * kBalWaves;
+}
 // Tokens of a chunk (one workgroup).
 static int chunk_of(const moe_balance_shape_t& s) {
+    if (one_launch(s)) return s.T;
     int chunk = 32;
-    while (chunk < 128 && (s.T + chunk - 1) / chunk > 1024) chunk *= 2;
+    while (chunk < 64 && (s.T + chunk - 1) / chunk > 1024) chunk *= 2;
     while (chunk > 4 && (long long)chunk * s.seqs > 4ll * s.T) chunk /= 2;   // a part is a turn of the workgroup: few sequences a chunk
     return chunk;
 }
-// Experts of a workgroup of the sum: as many as leave a thread up to 16 parts.
+// Experts of a workgroup of the sum: as many as leave a thread up to 16 parts.  (One workgroup for 8192 tokens, 128 experts and 257 parts needs no other's sums, and was slower.)
 static int sum_wide(const moe_balance_shape_t& s) {
     const long long parts = (s.T + chunk_of(s) - 1) / chunk_of(s) / s.seqs + 1;
     int wide = 32;
@@ -498,6 +536,7 @@ int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, co
             hipLaunchKernelGGL((balance_forward_kernel<g.value, nv.value, vec.value>), dim3((unsigned)p.chunks), dim3(kBalThreads), 0, st, p);
         });
     else hipLaunchKernelGGL(balance_ticket_kernel, dim3(1), dim3(1), 0, st, p.ticket);
+    if (p.chunks == 1 && s.seqs == 1) return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
     hipLaunchKernelGGL(balance_sum_kernel, dim3((unsigned)(s.seqs * sum_blocks(s))), dim3(kSumThreads), 0, st, p, sum_wide(s), sum_blocks(s));
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

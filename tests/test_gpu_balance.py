@@ -104,7 +104,8 @@ def test_every_number_of_experts(T, E, k):
 
 
 @pytest.mark.parametrize("T,E,k,S,masked", [(64, 8, 2, 64, 0.0), (300, 129, 4, 400, 0.2), (5000, 64, 8, 7, 0.5), (70000, 20, 4, 300, 0.1),
-                                            (140000, 8, 2, 1, 0.0), (40001, 256, 8, 61, 0.1), (4, 128, 8, 1, 0.0), (2, 8, 2, 1, 0.0)])
+                                            (140000, 8, 2, 1, 0.0), (40001, 256, 8, 61, 0.1), (4, 128, 8, 1, 0.0), (2, 8, 2, 1, 0.0),
+                                            (2048, 8, 2, 1, 0.3), (2049, 8, 2, 1, 0.3), (256, 60, 4, 1, 0.2), (257, 60, 4, 1, 0.0), (64, 256, 8, 1, 0.1), (65, 256, 8, 1, 0.0)])
 def test_sequences_of_any_length(T, E, k, S, masked):
     say(f"[balance] {T} {E} {k} {S} {masked}")
     s = make(T, E, k, S, masked)
