@@ -275,7 +275,7 @@ int moe_global_map(const moe_shape_t* shape, int32_t W, int32_t rank, const moe_
  * Beside the routed experts a layer has dense projections (of a shared expert, of the router) that many
  * requests share, each with a low-rank adapter of its own or none:
  *   y[t] = x[t] W + s_a (x[t] A_a^T) B_a,   a = ids[t];   y[t] = x[t] W where ids[t] is outside [0, adapters)
- * bf16 in, fp32 accumulate; h = s_a x A_a^T is kept to at least 16 bits of its fp32 value, and y is rounded once.  An
+ * bf16 in, fp32 accumulate; h = s_a x A_a^T is kept to 2^-17 of its fp32 value (whole for an fp32 y), and y is rounded once.  An
  * adapter that holds infinities or NaN reaches the rows of its own tokens only.  Results are the same bits on every run.
  * Limits (MOE_ERR_SHAPE otherwise): 0 <= T <= 2^26, K and N multiples of 8 from 8 to 2^16, T * max(K, N) <= 2^38, rank a
  * multiple of 8 from 8 to 128, 1 <= adapters <= 1024. */

@@ -229,6 +229,7 @@ struct ProjParams {
     uint16_t* terms[2];     // backward: [T rows][3][r], h (of the forward call) and this h as three bf16 terms, by row
     const float* h_given;   // the forward call's h
     int tile_rows;
+    int span;               // columns of a segment's low-rank part: 2 r, for an fp32 result 3 r
     int blocks;             // at most, of the plan
 };
 struct GradParams {
@@ -654,14 +655,14 @@ __device__ __forceinline__ TileLow tile_low(const ProjParams& p, int tile) {
     t.first = max(f, 0);
     t.count = l < 0 ? 0 : l - t.first + 1;
     t.apart = 4 * t.count > p.tile_rows;
-    t.used = t.apart ? 0 : t.count * 2 * p.r;
+    t.used = t.apart ? 0 : t.count * p.span;
     t.ld = (t.used + BK - 1) / BK * BK;
-    t.at = (size_t)p.tile_rows * ((size_t)tile * (2 * p.r + BK) + (size_t)t.first * 2 * p.r);
+    t.at = (size_t)p.tile_rows * ((size_t)tile * (p.span + BK) + (size_t)t.first * p.span);
     return t;
 }
 static size_t hx_bytes(const moe_adapter_shape_t& s, int tile_rows) {
     const size_t tiles = ((size_t)s.T + tile_rows - 1) / tile_rows, segs = (size_t)(s.adapters < s.T ? s.adapters : s.T);
-    return 2 * (size_t)tile_rows * (tiles * (2 * (size_t)s.rank + BK) + segs * 2 * (size_t)s.rank);
+    return 2 * (size_t)tile_rows * (tiles * (3 * (size_t)s.rank + BK) + segs * 3 * (size_t)s.rank);   // (three terms, for an fp32 result)
 }
 
 // h of one block of the plan, as fp32 and as the rows of its tile's low-rank part; behind the blocks, where the factors are wanted
@@ -706,10 +707,10 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
     const int tile = row0 / p.tile_rows;
     const TileLow tl = tile_low(p, tile);
     uint16_t* const hx = (uint16_t*)p.hx + tl.at + (size_t)(row0 - tile * p.tile_rows) * tl.ld;
-    const int own = a < 0 ? -1 : (p.plan.ordinal[a] - tl.first) * 2 * p.r;   // first column of its segment
+    const int own = a < 0 ? -1 : (p.plan.ordinal[a] - tl.first) * p.span;   // first column of its segment
     for (int i = tid; i < rows * (tl.ld / 8); i += kSmallThreads) {
         const int row = i / (tl.ld / 8), col = 8 * (i - row * (tl.ld / 8));
-        if (a < 0 || col < own || col >= own + 2 * p.r) *(u32x4_t*)(hx + (size_t)row * tl.ld + col) = zero4();
+        if (a < 0 || col < own || col >= own + p.span) *(u32x4_t*)(hx + (size_t)row * tl.ld + col) = zero4();
     }
     if (a < 0) {
         for (int i = tid; i < rows * p.r; i += kSmallThreads) p.h[(size_t)p.plan.order[row0 + i / p.r] * p.r + i % p.r] = 0.f;
@@ -766,18 +767,20 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
         to[0] = f32x4_t{h[0], h[1], h[2], h[3]};
         to[1] = f32x4_t{h[4], h[5], h[6], h[7]};
         const u32x4_t hi = pack8f(e), lo = pack8f(l);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) l[j] = fabsf(e[j]) < INFINITY ? l[j] - bf16_round(l[j]) : 0.f;
+        const u32x4_t rest = pack8f(l);   // the third term: what the first two leave
         if (!tl.apart) {
             uint16_t* x = hx + (size_t)row * tl.ld + own + col;
             *(u32x4_t*)x = hi;
             *(u32x4_t*)(x + p.r) = lo;
+            if (p.span > 2 * p.r) *(u32x4_t*)(x + 2 * p.r) = rest;
         }
-        if (p.terms[1]) {   // the third term is what the first two leave
+        if (p.terms[1]) {
             uint16_t* x = p.terms[1] + (size_t)(row0 + row) * 3 * p.r + col;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) l[j] = fabsf(e[j]) < INFINITY ? l[j] - bf16_round(l[j]) : 0.f;
             *(u32x4_t*)x = hi;
             *(u32x4_t*)(x + p.r) = lo;
-            *(u32x4_t*)(x + 2 * p.r) = pack8f(l);
+            *(u32x4_t*)(x + 2 * p.r) = rest;
         }
     }
 }
@@ -806,7 +809,7 @@ __device__ __forceinline__ bool all_finite(const f32x16_t& a) {
     return s == 0.f;
 }
 __device__ __forceinline__ LowRank low_of(const ProjParams& p, const TileLow& t, bool transposed) {
-    return LowRank{p.hx + t.at * 2, (uint32_t)t.ld * 2, transposed ? p.second_t : p.second, p.plan.seg + t.first, t.used, p.r, p.C};
+    return LowRank{p.hx + t.at * 2, (uint32_t)t.ld * 2, transposed ? p.second_t : p.second, p.plan.seg + t.first, t.used, p.span, p.r, p.C};
 }
 
 // Which tile a workgroup has.  Workgroups go to the eight XCDs in turn; each XCD gets a run of the tiles in an order that has 8 row tiles
@@ -1241,6 +1244,7 @@ static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan,
     p.plan = plan_view(s, plan);
     const TileShape tile = tile_shape(p.T, p.C);
     p.tile_rows = tile.rows;
+    p.span = (p.out_f32 ? 3 : 2) * p.r;
     p.blocks = ((int)plan_blocks(s) + 7) & ~7;
     p.hx = ws;
     char* rest = ws + align_up(hx_most(s), 256);

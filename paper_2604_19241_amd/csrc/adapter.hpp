@@ -4,9 +4,9 @@
 //   y[t] = x[t] W + s_a (x[t] A_a^T) B_a,   a = ids[t]            [T, K] x [K, N], A_a [r, K], B_a [r, N]
 //
 // With the rows sorted by adapter a tile of rows holds a few runs ("segments"), and its low-rank part is a
-// product over 2 r more columns a segment: the tile's row of h = s x A^T stands, as the bf16 pair hi + lo (16 bits of
-// the fp32 value, an error of 2^-17: small beside the rounding of y), at the columns of its own segment, zeros at the
-// others', and B_a stands twice behind W.  So the matrix pipeline runs on without a second loop: stages of 64
+// product over 2 r more columns a segment: the tile's row of h = s x A^T stands, as the bf16 pair hi + lo (an error of
+// 2^-17 of the fp32 value: small beside the rounding of a bf16 y), at the columns of its own segment, zeros at the
+// others', and B_a stands twice behind W.  For an fp32 y it is three terms, the whole 24 bits, and 3 r columns.  So the matrix pipeline runs on without a second loop: stages of 64
 // k are the dense ones, one that holds the rest of K, and then those of the low-rank part.  Every chunk of 16 bytes that
 // lies past either is fetched from a page of zeros.
 #pragma once
@@ -20,22 +20,22 @@ __device__ __forceinline__ const char* zero_chunk() { return (const char*)g_zero
 
 // The low-rank part of a tile's reduction.
 struct LowRank {
-    const char* h;        // [rows of the tile][ld bytes] bf16: hi (r columns) and lo (r) of every segment, zeros elsewhere
+    const char* h;        // [rows of the tile][ld bytes] bf16: the terms (r columns each) of every segment, zeros elsewhere
     uint32_t ld;
     const char* f;        // KS: factors [adapters][r][C]; KC: [adapters][C][r]
     const int32_t* seg;   // adapters of the tile's segments
-    int used;             // columns that hold something: 2 r a segment
-    int r, C;
+    int used;             // columns that hold something: `span` a segment
+    int span, r, C;
     __device__ __forceinline__ const char* row(int row, int j) const { return h + (size_t)row * ld + (size_t)j * 2; }
     __device__ __forceinline__ const char* ks(int j, int col) const {
         if (j >= used) return zero_chunk();
-        const int s = j / (2 * r), q = j - s * 2 * r;
-        return f + (((size_t)seg[s] * r + (q < r ? q : q - r)) * C + col) * 2;
+        const int s = j / span, q = j - s * span;
+        return f + (((size_t)seg[s] * r + (q < r ? q : q < 2 * r ? q - r : q - 2 * r)) * C + col) * 2;
     }
     __device__ __forceinline__ const char* kc(int j, int col) const {   // j a multiple of 8, as r is
         if (j >= used) return zero_chunk();
-        const int s = j / (2 * r), q = j - s * 2 * r;
-        return f + (((size_t)seg[s] * C + col) * r + (q < r ? q : q - r)) * 2;
+        const int s = j / span, q = j - s * span;
+        return f + (((size_t)seg[s] * C + col) * r + (q < r ? q : q < 2 * r ? q - r : q - 2 * r)) * 2;
     }
 };
 

@@ -90,8 +90,8 @@ def bounds(s, v, m, out_f32):
     r = s["a"].shape[1]
     half = 2.0 ** -8   # of a bf16 value
     e = {"h": sums(m["h"], K)}
-    # h as hi + lo: 2^-17 of its value, beside the error that h has
-    e["y"] = sums(m["y"] + m["ylow"], K + 2 * r) + 2.0 ** -16 * m["ylow"] + low_error(s, m, "h", K, s["b"])
+    # h as hi + lo: 2^-17 of its value, beside the error that h has; for an fp32 y it is kept whole
+    e["y"] = sums(m["y"] + m["ylow"], K + 3 * r) + (0.0 if out_f32 else 2.0 ** -16) * m["ylow"] + low_error(s, m, "h", K, s["b"])
     e["dx"] = sums(m["dx"] + m["dxlow"], N + 2 * r) + 2.0 ** -16 * m["dxlow"] + low_error(s, m, "g", N, s["a"])
     if not out_f32:
         e["y"] = e["y"] + half * v["y"].abs()
