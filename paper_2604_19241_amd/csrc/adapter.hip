@@ -221,7 +221,7 @@ struct ProjParams {
     float* part;            // [splits][T][C]
     float* hpart;           // [hsplits][T][r]
     int splits, per_split, hsplits, hper_split;
-    int col_tiles, row_tiles, rank_tiles;
+    int col_tiles, row_tiles, rank_tiles, hgroups;
     // more
     PlanView plan;
     char* hx;               // the low-rank rows of every tile (hx_base)
@@ -239,6 +239,8 @@ struct GradParams {
     size_t ldx[2];
     const float* h[2];      // [T][r]; NULL: hpart (few tokens)
     float* out[2];          // [n][r][W]
+    int parts;              // more tokens: into how many parts an adapter's rows are cut, and the parts' sums, [parts][n][r][W] each
+    float* part[2];
     int col_tiles[2], rank_tiles;
 };
 
@@ -341,8 +343,8 @@ __device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int
     }
 }
 
-// Parts of x W and of h.  Tasks: (column tile, split, row tile), then (token, rank tile, split): a workgroup whose token is not every
-// 32nd of its adapter's has nothing to do.
+// Parts of x W and of h.  Tasks: (column tile, split, row tile), then of h (token, rank tile, split), where a workgroup whose token is not every
+// 32nd of its adapter's has nothing to do, or (adapter, 32 of its tokens, rank tile, split) where that is fewer.
 template <int NRF, int FORM>
 __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjParams p) {
     constexpr int kLds = SmallTile<NRF, 2>::kLds > SmallTile<1, 2>::kLds ? SmallTile<NRF, 2>::kLds : SmallTile<1, 2>::kLds;   // (h: 32 rows)
@@ -385,13 +387,13 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
         return;
     }
     id -= gemm;
-    const int t = id % p.T, rest = id / p.T, rt = rest % p.rank_tiles, sp = rest / p.rank_tiles;
-    const int a = adapter_of(p.ids, t, p.n);
+    const int t = id % p.hgroups, rest = id / p.hgroups, rt = rest % p.rank_tiles, sp = rest / p.rank_tiles;
+    const int blocks = (p.T + 31) / 32, a = p.hgroups == p.T ? rfl(adapter_of(p.ids, t, p.n)) : t / blocks;
     if (a < 0) return;
     Members mb;
     mb.find(p.T, p.n, p.ids, a, s_mask);
-    const int rank = mb.before(t);
-    if (rank % 32 != 0) return;
+    const int rank = p.hgroups == p.T ? mb.before(t) : t % blocks * 32;
+    if (rank % 32 != 0 || rank >= mb.count()) return;
     mb.list(rank, 32, s_list);
     const int rows = min(32, mb.count() - rank);
     const int s0 = sp * p.hper_split, s1 = min(nst, s0 + p.hper_split);
@@ -441,7 +443,7 @@ __device__ __forceinline__ void fma8(float (&acc)[8], float h, u32x4_t b) {
 constexpr int kJoinCols = 1024;
 template <int G>
 struct JoinShared {
-    float h[G][kMaxRank];
+    __attribute__((aligned(16))) float h[kMaxRank][G];
     uint64_t mask[kFewWords];
     int32_t list[G];
 };
@@ -470,7 +472,7 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
     const char* const f = p.second + ((size_t)max(a, 0) * p.r * p.C + c) * 2;
     const float* const part = p.part + c;
     // the first loads of everything are on their way together: this kernel is what its dependent loads take
-    constexpr int kPreB = 8, kPreP = 4;
+    constexpr int kPreB = 8, kPreP = 8;
     u32x2_t b[kPreB];
     f32x4_t q[kPreP];
 #pragma unroll
@@ -488,7 +490,7 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
         for (int i = tid; i < rows * p.r; i += 256) {
             const int m = G == 1 ? 0 : i / p.r, j = i - m * p.r, tok = token(m);
             const float v = a < 0 ? 0.f : whole_h(p, tok, j, s);
-            S.h[m][j] = v;
+            S.h[j][m] = v;
             if (p.h && cb == 0) p.h[(size_t)tok * p.r + j] = v;
         }
         __syncthreads();
@@ -512,12 +514,12 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
 #pragma unroll
         for (int i = 0; i < kPreB; ++i)
 #pragma unroll
-            for (int m = 0; m < G; ++m) fma4(acc[m], S.h[m][i], b[i]);   // (rows that are not there: never stored)
+            for (int m = 0; m < G; ++m) fma4(acc[m], S.h[i][m], b[i]);   // (rows that are not there: never stored)
 #pragma unroll 8
         for (int j = kPreB; j < p.r; ++j) {
             const u32x2_t x = *(const u32x2_t*)(f + (size_t)j * p.C * 2);
 #pragma unroll
-            for (int m = 0; m < G; ++m) fma4(acc[m], S.h[m][j], x);
+            for (int m = 0; m < G; ++m) fma4(acc[m], S.h[j][m], x);
         }
     }
 #pragma unroll
@@ -529,14 +531,17 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
         }
 }
 
-// Gradients of 8 ranks and 256 columns of one adapter, token by token; the waves share the tokens and their sums are added in LDS.  (With 512 columns a
-// wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4 workgroups that took 128 tokens one after
-// the other: 48 us, now 11.)
-constexpr int kGradRanks = 8, kGradCols = 256;
-template <int TOKENS>
+// Gradients of 8 ranks of one adapter, token by token.  SHARE: 256 columns, the waves share the tokens and their sums are added in LDS; else
+// 1024 columns, 256 a wave, which keeps the LDS small and the workgroups few where the adapters have few tokens or none (11 tokens, 27 adapters of 64 ranks, 6552 x 464: the
+// training step 66 us with SHARE, NOSHARE without).  (With 512 columns a wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4
+// workgroups that took 128 tokens one after the other: 48 us, now 11.)
+constexpr int kGradRanks = 8;
+template <bool SHARE>
+constexpr int kGradCols = SHARE ? 256 : 1024;
+template <int TOKENS, bool SHARE>
 struct FewGradShared {
     float h[TOKENS][kGradRanks];
-    float sums[4][kGradRanks][kGradCols];
+    float sums[SHARE ? 4 : 1][kGradRanks][SHARE ? 256 : 1];
     uint64_t mask[kFewWords];
     int32_t list[TOKENS];
 };
@@ -553,34 +558,43 @@ struct FewGradTask {
         j0 = rest / g.n * kGradRanks;
     }
 };
-// S.list[0 .. count): the adapter's tokens; h4(k, token, j) = 4 ranks from j on of the k-th.
-template <int TOKENS, class H4>
-__device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGradTask& t, int count, FewGradShared<TOKENS>& S, H4 h4) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, W = g.W[t.which], c = t.cb * kGradCols + 4 * lane;
+// S.list[0 .. count): the adapter's tokens; h4(token, j) = 4 ranks of it from j on.
+template <int TOKENS, bool SHARE, class H4>
+__device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGradTask& t, int count, FewGradShared<TOKENS, SHARE>& S, H4 h4) {
+    constexpr int kStep = SHARE ? 4 : 1, kPre = SHARE ? 8 : 4;
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, W = g.W[t.which], c = t.cb * kGradCols<SHARE> + (SHARE ? 4 * lane : 4 * tid);
+    float* const out = g.out[t.which] + ((size_t)t.a * g.r + t.j0) * W + c;
     float acc[kGradRanks][4] = {};
     if (count > 0) {
         // the first rows of x are on their way while h is fetched
-        constexpr int kPre = 8;
+        const int k0 = SHARE ? w : 0;
         const size_t ldx = g.ldx[t.which];
         const char* const x = g.x[t.which] + (size_t)min(c, W - 4) * 2;
         u32x2_t pre[kPre];
 #pragma unroll
-        for (int i = 0; i < kPre; ++i) pre[i] = *(const u32x2_t*)(x + (size_t)S.list[min(w + 4 * i, count - 1)] * ldx);
+        for (int i = 0; i < kPre; ++i) pre[i] = *(const u32x2_t*)(x + (size_t)S.list[min(k0 + kStep * i, count - 1)] * ldx);
         for (int i = tid; i < 2 * count; i += 256) *(f32x4_t*)&S.h[i >> 1][4 * (i & 1)] = h4(S.list[i >> 1], t.j0 + 4 * (i & 1));
         __syncthreads();
         if (c < W) {
 #pragma unroll
             for (int i = 0; i < kPre; ++i)
-                if (w + 4 * i < count)
+                if (k0 + kStep * i < count)
 #pragma unroll
-                    for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[w + 4 * i][j], pre[i]);
+                    for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[k0 + kStep * i][j], pre[i]);
 #pragma unroll 8
-            for (int k = w + 4 * kPre; k < count; k += 4) {
+            for (int k = k0 + kStep * kPre; k < count; k += kStep) {
                 const u32x2_t b = *(const u32x2_t*)(x + (size_t)S.list[k] * ldx);
 #pragma unroll
                 for (int j = 0; j < kGradRanks; ++j) fma4(acc[j], S.h[k][j], b);
             }
         }
+    }
+    if (!SHARE || count == 0) {
+        if (c < W)
+#pragma unroll
+            for (int j = 0; j < kGradRanks; ++j)
+                if (!SHARE || (j & 3) == w) *(f32x4_t*)(out + (size_t)j * W) = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+        return;
     }
 #pragma unroll
     for (int j = 0; j < kGradRanks; ++j) *(f32x4_t*)&S.sums[w][j][4 * lane] = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
@@ -596,14 +610,15 @@ __device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGrad
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] += o[q];
         }
-        *(f32x4_t*)(g.out[t.which] + ((size_t)t.a * g.r + t.j0 + j) * W + c) = v;
+        *(f32x4_t*)(out + (size_t)j * W) = v;
     }
 }
-__device__ __forceinline__ void few_tokens_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared<kFewTokens>& S) {
+template <int TOKENS, bool SHARE>
+__device__ __forceinline__ void few_tokens_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared<TOKENS, SHARE>& S) {
     const FewGradTask t(g, id);
     Members mb;
     mb.find(g.T, g.n, p.ids, t.a, S.mask);
-    mb.list(0, kFewTokens, S.list);
+    mb.list(0, TOKENS, S.list);
     const float* const h = g.h[t.which];
     const float s = p.scale ? p.scale[t.a] : 1.f;
     few_grad_task(g, t, mb.count(), S, [&](int tok, int j) {
@@ -626,11 +641,12 @@ __global__ void __launch_bounds__(256) adapter_few_second_kernel(ProjParams p) {
     __shared__ JoinShared<G> S;
     join_task<G>(p, blockIdx.x % p.T, blockIdx.x / p.T, S);
 }
-template <int G>
+// FEW: up to kGradRows tokens
+template <int G, bool FEW>
 __global__ void __launch_bounds__(256) adapter_few_second_grad_kernel(ProjParams p, GradParams g, int joins) {
     union Shared {
         JoinShared<G> join;
-        FewGradShared<kFewTokens> grad;
+        FewGradShared<FEW ? kGradRows : kFewTokens, !FEW> grad;
     };
     __shared__ Shared S;
     const int id = blockIdx.x;
@@ -1031,7 +1047,14 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     const int which = ct < g.col_tiles[0] ? 0 : 1;
     if (which) ct -= g.col_tiles[0];
     const int W = g.W[which], c0 = ct * 32 * NCF, r = g.r;
-    const int row0 = p.plan.start[a], count = p.plan.start[a + 1] - row0;
+    int row0 = p.plan.start[a], count = p.plan.start[a + 1] - row0;
+    float* out = g.out[which];
+    if (g.parts > 1) {
+        const int rows = ((count + g.parts - 1) / g.parts + BK - 1) / BK * BK, first = min(count, (int)blockIdx.y * rows);
+        row0 += first;
+        count = min(rows, count - first);
+        out = g.part[which] + (size_t)blockIdx.y * g.n * r * W;
+    }
     const Lane ln;
     const int wave = ln.wave_uniform() & 3;
     const bool moves = ln.wave_uniform() >= 4;
@@ -1137,17 +1160,35 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
             row += 32 * tf;
             col += c0;
             if (row >= r || col >= W) return;
-            f32x4_t* to = (f32x4_t*)(g.out[which] + ((size_t)a * r + row) * W + col);
+            f32x4_t* to = (f32x4_t*)(out + ((size_t)a * r + row) * W + col);
             to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
             to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
         });
     }
 }
+// The parts' sums, first part first.
+__global__ void __launch_bounds__(256) adapter_grad_sum_kernel(GradParams g) {
+    const size_t n0 = (size_t)g.n * g.r * g.W[0] / 4, n1 = (size_t)g.n * g.r * g.W[1] / 4;
+    size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const int which = i < n0 ? 0 : 1;
+    if (which) i -= n0;
+    const size_t n = which ? n1 : n0;
+    if (i >= n) return;
+    const f32x4_t* const q = (const f32x4_t*)g.part[which];
+    f32x4_t v = q[i];
+#pragma unroll 8
+    for (int k = 1; k < g.parts; ++k) {
+        const f32x4_t u = q[(size_t)k * n + i];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] += u[e];
+    }
+    ((f32x4_t*)g.out[which])[i] = v;
+}
 
 // The same for adapters with up to kGradRows rows, on the vector unit: a workgroup of the tiles above takes 6 us whatever its rows and has a CU for itself (a training step of 512 tokens on
 // 200 adapters of 680 x 480, 16 ranks, 112 us, of 600 with this and the low-rank parts row by row 85).
 __global__ void __launch_bounds__(256) adapter_grad_rows_kernel(ProjParams p, GradParams g) {
-    __shared__ FewGradShared<kGradRows> S;
+    __shared__ FewGradShared<kGradRows, false> S;
     const FewGradTask t(g, blockIdx.x);
     const int row0 = p.plan.start[t.a], count = p.plan.start[t.a + 1] - row0;
     if (count > kGradRows) return;
@@ -1158,12 +1199,13 @@ __global__ void __launch_bounds__(256) adapter_grad_rows_kernel(ProjParams p, Gr
 }
 
 // ------------------------------------------------------------------ launches
+constexpr int kMostSplits = 16;
 static int stages_in(int R) { return (R + BK - 1) / BK; }
 struct FewPlan {
-    int row_frags, col_tiles, row_tiles, rank_tiles, splits, per_split, hsplits, hper_split;
+    int row_frags, col_tiles, row_tiles, rank_tiles, hgroups, splits, per_split, hsplits, hper_split;
 };
-// Parts of at least 4 stages, as many as give every CU a workgroup; h is cut alike, or into fewer parts where every token may be a group of its own.
-static FewPlan few_plan(int T, int R, int C, int r) {
+// Parts of at least 4 stages, as many as give every CU a workgroup but no more than the second launch fetches in two goes; h is cut alike, or into fewer parts where every token may be a group of its own.
+static FewPlan few_plan(int T, int R, int C, int r, int n) {
     FewPlan f;
     f.row_frags = T <= 32 ? 1 : 2;
     f.col_tiles = (C + 63) / 64;
@@ -1171,14 +1213,15 @@ static FewPlan few_plan(int T, int R, int C, int r) {
     f.rank_tiles = (r + 63) / 64;
     const int nst = stages_in(R), tiles = f.col_tiles * f.row_tiles;
     const int want = std::max(1, 256 / tiles);
-    f.per_split = std::max(4, (nst + want - 1) / want);
+    f.per_split = std::max({4, (nst + want - 1) / want, (nst + kMostSplits - 1) / kMostSplits});
     f.splits = (nst + f.per_split - 1) / f.per_split;
-    f.hper_split = std::max(std::min(f.per_split, 16), (int)(((long long)nst * T * f.rank_tiles + 511) / 512));
+    f.hgroups = (int)std::min((long long)T, (long long)n * ((T + 31) / 32));
+    f.hper_split = std::max(std::min(f.per_split, 16), (int)(((long long)nst * f.hgroups * f.rank_tiles + 511) / 512));
     f.hsplits = (nst + f.hper_split - 1) / f.hper_split;
     return f;
 }
-static size_t few_bytes(int T, int R, int C, int r) {
-    const FewPlan f = few_plan(T, R, C, r);
+static size_t few_bytes(int T, int R, int C, int r, int n) {
+    const FewPlan f = few_plan(T, R, C, r, n);
     return align_up((size_t)f.splits * T * C * 4, 256) + align_up((size_t)f.hsplits * T * r * 4, 256);
 }
 // Tiles of the product.  A stage of 64 k takes about 0.38 us in tiles of 64 x 64 (two on a CU), 0.6 in tiles of 128 x 128, 1.0 in 128 x 256 and 1.45 in 256 x 256, and what counts
@@ -1211,33 +1254,48 @@ static TileShape tile_shape(int T, int C) {
     return best;
 }
 static size_t hx_most(const moe_adapter_shape_t& s) { return std::max(hx_bytes(s, tile_shape(s.T, s.N).rows), hx_bytes(s, tile_shape(s.T, s.K).rows)); }
+// The factors' gradients: columns of a tile; whether adapters with few rows have a kernel of their own (where they have few on average); and into how many parts
+// an adapter's rows are cut where the tiles would leave more than half of the CUs idle (3594 tokens on one adapter, 2528 x 264: GPARTS1 us in one part, GPARTS2 in
+// 7 with the sum of the parts).
+static int grad_cols(int r) { return r > 64 ? 64 : 128; }
+static bool grad_rows(const moe_adapter_shape_t& s) { return (long long)s.adapters * kGradRows >= s.T; }
+static int grad_parts(const moe_adapter_shape_t& s) {
+    const int cols = grad_cols(s.rank), tiles = s.adapters * ((s.K + cols - 1) / cols + (s.N + cols - 1) / cols);
+    return grad_rows(s) ? 1 : std::max(1, std::min(256 / tiles, s.T / (s.adapters * 512)));
+}
+static size_t grad_part_at(const moe_adapter_shape_t& s);
 static size_t many_bytes(const moe_adapter_shape_t& s) {
+    const int parts = grad_parts(s);
+    return grad_part_at(s) + (parts > 1 ? (size_t)parts * s.adapters * s.rank * ((size_t)s.K + s.N) * 4 : 0);
+}
+static size_t grad_part_at(const moe_adapter_shape_t& s) {
     return align_up(hx_most(s), 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256) +
            2 * align_up((size_t)s.T * s.rank * 6, 256);
 }
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
     if (s.T == 0) return 256;
     size_t most = adapter_few(s) ? 0 : many_bytes(s);
-    if (!adapter_needs_plan(s)) most = std::max({most, few_bytes(s.T, s.K, s.N, s.rank), few_bytes(s.T, s.N, s.K, s.rank)});
+    if (!adapter_needs_plan(s)) most = std::max({most, few_bytes(s.T, s.K, s.N, s.rank, s.adapters), few_bytes(s.T, s.N, s.K, s.rank, s.adapters)});
     return most;
 }
 
 static void few_params(ProjParams& p, char* ws, FewPlan& f) {
-    f = few_plan(p.T, p.R, p.C, p.r);
+    f = few_plan(p.T, p.R, p.C, p.r, p.n);
     p.part = (float*)ws;
     p.hpart = (float*)(ws + align_up((size_t)f.splits * p.T * p.C * 4, 256));
     p.splits = f.splits, p.per_split = f.per_split, p.hsplits = f.hsplits, p.hper_split = f.hper_split;
-    p.col_tiles = f.col_tiles, p.row_tiles = f.row_tiles, p.rank_tiles = f.rank_tiles;
+    p.col_tiles = f.col_tiles, p.row_tiles = f.row_tiles, p.rank_tiles = f.rank_tiles, p.hgroups = f.hgroups;
 }
 template <int FORM>
 static void few_first(const ProjParams& p, const FewPlan& f, hipStream_t st) {
-    const dim3 grid((unsigned)(f.col_tiles * f.splits * f.row_tiles + p.T * f.rank_tiles * f.hsplits));
+    const dim3 grid((unsigned)(f.col_tiles * f.splits * f.row_tiles + f.hgroups * f.rank_tiles * f.hsplits));
     if (f.row_frags == 1) hipLaunchKernelGGL((adapter_few_first_kernel<1, FORM>), grid, dim3(kSmallThreads), 0, st, p);
     else hipLaunchKernelGGL((adapter_few_first_kernel<2, FORM>), grid, dim3(kSmallThreads), 0, st, p);
 }
 static int few_joins(const ProjParams& p) { return p.T * ((p.C + kJoinCols - 1) / kJoinCols); }
-// Whether tokens of one adapter share the fetch of its second factor in the second launch.
-static bool join_groups(const ProjParams& p) { return (long long)p.T * p.r * p.C > 32 << 20; }
+// Whether tokens of one adapter share the fetch of its second factor in the second launch.  Measured, us by themselves / in fours (tokens, ranks, columns): 254, 128, 1728
+// 11.7 / 17.4; 500, 16, 7168 12.0 / 20.8; 400, 128, 2048 18.3 / 18.9; 250, 64, 7168 17.4 / 16.8; 250, 128, 14336 59.8 / 40.3.
+static bool join_groups(const ProjParams& p) { return (long long)p.T * p.r * p.C > 1 << 27; }
 
 template <int FORM>
 static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
@@ -1310,28 +1368,39 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         }
         const int joins = s.T > 0 ? few_joins(p) : 0;
         g.rank_tiles = g.r / kGradRanks;
-        for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols - 1) / kGradCols;
+        const bool few = s.T <= kGradRows;
+        const int cols = few ? kGradCols<false> : kGradCols<true>;
+        for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
         const dim3 grid((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1])));
-        if (join_groups(p)) hipLaunchKernelGGL((adapter_few_second_grad_kernel<4>), grid, dim3(256), 0, st, p, g, joins);
-        else hipLaunchKernelGGL((adapter_few_second_grad_kernel<1>), grid, dim3(256), 0, st, p, g, joins);
+        auto launch = [&](auto group, auto small) {
+            hipLaunchKernelGGL((adapter_few_second_grad_kernel<group.value, small.value>), grid, dim3(256), 0, st, p, g, joins);
+        };
+        std::integral_constant<int, 4> groups;
+        std::integral_constant<int, 1> single;
+        if (few) join_groups(p) ? launch(groups, std::true_type{}) : launch(single, std::true_type{});
+        else join_groups(p) ? launch(groups, std::false_type{}) : launch(single, std::false_type{});
     } else {
         p.h_given = h;
         many_launch<kKc>(p, s, plan, ws, st);
         // With so many adapters that they have few rows on average, those that do have are done by a kernel for that
-        const bool rows = (long long)g.n * kGradRows >= g.T;
+        const bool rows = grad_rows(s);
         g.few = rows;
         g.h[1] = p.h;
         if (rows) {
             g.rank_tiles = g.r / kGradRanks;
-            for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols - 1) / kGradCols;
+            for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols<false> - 1) / kGradCols<false>;
             hipLaunchKernelGGL(adapter_grad_rows_kernel, dim3((unsigned)(g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st, p, g);
         }
-        const int cols = p.r > 64 ? 64 : 128;
+        const int cols = grad_cols(p.r);
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
-        const dim3 grid((unsigned)(8 * (rows ? std::min(g.n, g.T / (kGradRows + 1)) : g.n) * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)));
+        g.parts = grad_parts(s);
+        g.part[0] = (float*)(ws + grad_part_at(s));
+        g.part[1] = g.part[0] + (size_t)g.parts * g.n * g.r * g.W[0];
+        const dim3 grid((unsigned)(8 * (rows ? std::min(g.n, g.T / (kGradRows + 1)) : g.n) * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)), (unsigned)g.parts);
         if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kGradThreads), 0, st, p, g);
         else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kGradThreads), 0, st, p, g);
         else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kGradThreads), 0, st, p, g);
+        if (g.parts > 1) hipLaunchKernelGGL(adapter_grad_sum_kernel, dim3((unsigned)(((size_t)g.n * g.r * (g.W[0] + g.W[1]) / 4 + 255) / 256)), dim3(256), 0, st, g);
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

@@ -28,7 +28,8 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     (33, 1000, 88, 16, 64, "each", 64, "bf16"), (64, 4096, 40, 128, 2, "scattered", 0, "bf16"), (65, 328, 640, 72, 7, "outside", 0, "bf16"),
     (200, 136, 2056, 8, 256, "each", 0, "bf16"), (256, 448, 264, 128, 1, "one", 0, "f32"), (256, 512, 1024, 8, 2, "packed", 0, "bf16"),
     (257, 64, 64, 8, 1, "one", 0, "bf16"), (257, 8, 16, 8, 300, "each", 0, "f32"), (300, 328, 200, 24, 5, "outside", 8, "bf16"),
-    (512, 1160, 264, 96, 2, "one", 0, "bf16"), (500, 72, 2056, 16, 9, "scattered", 0, "bf16"),
+    (512, 1160, 264, 96, 2, "one", 0, "bf16"), (500, 72, 2056, 128, 9, "scattered", 0, "bf16"), (301, 2056, 136, 128, 2, "each", 0, "bf16"),
+    (500, 72, 3000, 128, 20, "scattered", 0, "f32"), (500, 72, 2056, 16, 9, "scattered", 0, "bf16"),
     # more tokens: sorted by adapter
     (513, 64, 64, 8, 1, "one", 0, "bf16"), (513, 8, 16, 8, 600, "each", 0, "f32"), (600, 328, 200, 24, 5, "outside", 8, "bf16"),
     (1011, 136, 72, 16, 256, "scattered", 0, "bf16"), (640, 1000, 520, 64, 3, "packed", 64, "f32"), (1021, 264, 712, 128, 2, "scattered", 0, "bf16"),
@@ -38,6 +39,10 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     (4100, 136, 1032, 16, 9, "packed", 0, "bf16"), (4100, 1032, 72, 16, 300, "scattered", 0, "bf16"), (8200, 72, 1544, 24, 6, "scattered", 8, "bf16"),
     (8200, 1544, 136, 64, 5, "packed", 0, "f32"), (16500, 584, 1032, 8, 40, "scattered", 0, "f32"), (16500, 1032, 584, 128, 3, "packed", 0, "bf16"),
     (16500, 136, 72, 48, 7, "scattered", 0, "bf16"),
+    # an adapter's rows in several parts
+    (4099, 264, 136, 16, 1, "one", 0, "bf16"), (3000, 72, 200, 72, 2, "scattered", 0, "bf16"), (5000, 392, 72, 8, 3, "none", 0, "f32"),
+    # parts of a long reduction in both directions
+    (40, 7000, 4104, 16, 3, "scattered", 0, "bf16"), (400, 5000, 264, 24, 2, "packed", 8, "f32"),
 ]
 
 
