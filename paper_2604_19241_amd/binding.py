@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
+from functools import lru_cache
 from pathlib import Path
 from typing import Optional
 
@@ -359,12 +360,22 @@ def saved_views(shape: MoEShape, saved: torch.Tensor) -> dict:
 class MoEAdapterShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "K", "N", "rank", "adapters")]
 
+    def __init__(self, T, K, N, rank, adapters):
+        super().__init__(T, K, N, rank, adapters)
+        self.sizes = (T, K, N, rank, adapters)   # (a field of the structure takes as long to read as a tensor's property)
+
 
 def make_adapter_shape(T, K, N, rank, adapters) -> MoEAdapterShape:
     return MoEAdapterShape(T, K, N, rank, adapters)
 
 
 def _adapter_bytes(shape: MoEAdapterShape) -> tuple:
+    return _adapter_sizes_bytes(*shape.sizes)
+
+
+@lru_cache(maxsize=1024)
+def _adapter_sizes_bytes(*sizes) -> tuple:
+    shape = MoEAdapterShape(*sizes)
     ws, plan = ctypes.c_size_t(0), ctypes.c_size_t(0)
     _check(load_library().moe_adapter_workspace_bytes(ctypes.byref(shape), ctypes.byref(ws), ctypes.byref(plan)),
            "moe_adapter_workspace_bytes")
@@ -384,7 +395,7 @@ class AdapterPlan:
 
 def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
     """Sorts the tokens by adapter, once for all projections of the batch with as many adapters."""
-    assert ids.is_cuda and ids.dtype == torch.int32 and ids.is_contiguous() and ids.shape == (shape.T,)
+    assert ids.is_cuda and ids.dtype is _I32 and ids.is_contiguous() and ids.shape == shape.sizes[:1]
     nbytes = _adapter_bytes(shape)[1]
     if nbytes == 0:
         return AdapterPlan(ids, None)
@@ -405,13 +416,13 @@ def _adapter_rows(t: torch.Tensor, T: int, width: int) -> int:
 
 
 def _adapter_operands(shape: MoEAdapterShape, w, a, b, scale, plan: AdapterPlan):
-    K, N, r, n = shape.K, shape.N, shape.rank, shape.adapters
+    T, K, N, r, n = shape.sizes
     # (written out: a generator over the operands took as long as half a launch)
     assert w.is_cuda and w.dtype is _BF16 and w.is_contiguous() and w.shape == (K, N)
     assert a.is_cuda and a.dtype is _BF16 and a.is_contiguous() and a.shape == (n, r, K)
     assert b.is_cuda and b.dtype is _BF16 and b.is_contiguous() and b.shape == (n, r, N)
     assert scale is None or (scale.is_cuda and scale.dtype is _F32 and scale.is_contiguous() and scale.shape == (n,))
-    assert plan.ids.shape == (shape.T,)
+    assert plan.ids.shape == (T,)
 
 
 def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, scale=None, out_dtype=torch.bfloat16,
@@ -419,15 +430,16 @@ def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, s
     """y[t] = x[t] w + scale[i] (x[t] a[i]^T) b[i] with i = ids[t]: x [T,K] (rows may be parts of wider ones), w [K,N],
     a [adapters,rank,K], b [adapters,rank,N], all bf16; scale [adapters] fp32.  h [T,rank] fp32, if given, receives what
     moe_adapter_backward reads."""
-    ldx = _adapter_rows(x, shape.T, shape.K)
+    T, K, N, rank, _ = shape.sizes
+    ldx = _adapter_rows(x, T, K)
     _adapter_operands(shape, w, a, b, scale, plan)
     assert out_dtype is _BF16 or out_dtype is _F32
     if y is None:   # (new_empty with a type takes a microsecond more)
-        y = x.new_empty((shape.T, shape.N)) if out_dtype is _BF16 else torch.empty((shape.T, shape.N), dtype=_F32, device=x.device)
+        y = x.new_empty((T, N)) if out_dtype is _BF16 else torch.empty((T, N), dtype=_F32, device=x.device)
     else:
-        assert y.is_cuda and y.dtype is out_dtype and y.is_contiguous() and y.shape == (shape.T, shape.N)
+        assert y.is_cuda and y.dtype is out_dtype and y.is_contiguous() and y.shape == (T, N)
     if h is not None:
-        assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
+        assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (T, rank)
     if ws is None:
         ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
     _check(load_library().moe_adapter_forward(
@@ -439,11 +451,12 @@ def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, s
 def moe_adapter_backward(shape: MoEAdapterShape, dy, x, w, a, b, plan: AdapterPlan, h, scale=None, out: dict | None = None,
                          ws: torch.Tensor | None = None) -> dict:
     """Gradients of x (bf16) and of every adapter's two factors (fp32); w is frozen.  h as moe_adapter_forward wrote it."""
-    lddy, ldx = _adapter_rows(dy, shape.T, shape.N), _adapter_rows(x, shape.T, shape.K)
+    T, K, N, rank, _ = shape.sizes
+    lddy, ldx = _adapter_rows(dy, T, N), _adapter_rows(x, T, K)
     _adapter_operands(shape, w, a, b, scale, plan)
-    assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (shape.T, shape.rank)
+    assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (T, rank)
     if out is None:
-        out = {"dx": x.new_empty((shape.T, shape.K)), "da": h.new_empty(a.shape), "db": h.new_empty(b.shape)}
+        out = {"dx": torch.empty_like(x) if ldx == K else x.new_empty((T, K)), "da": h.new_empty(a.shape), "db": h.new_empty(b.shape)}
     else:
         for key, dtype, size in (("dx", _BF16, x.shape), ("da", _F32, a.shape), ("db", _F32, b.shape)):
             t = out[key]
@@ -460,6 +473,10 @@ def moe_adapter_backward(shape: MoEAdapterShape, dy, x, w, a, b, plan: AdapterPl
 
 class MoEBalanceShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "E", "k", "seqs")] + [(n, ctypes.c_float) for n in ("balance_coef", "z_coef")]
+
+    def __init__(self, T, E, k, seqs, balance_coef, z_coef):
+        super().__init__(T, E, k, seqs, balance_coef, z_coef)
+        self.sizes = (T, E, k, seqs)
 
 
 class MoEBalanceStatsC(ctypes.Structure):
@@ -490,22 +507,22 @@ def moe_balance_workspace_bytes(shape: MoEBalanceShape) -> int:
 
 
 def _balance_inputs(shape: MoEBalanceShape, logits, topk_idx, seq_offsets, mask):
-    assert logits.is_cuda and logits.dtype is _F32 and logits.is_contiguous() and logits.shape == (shape.T, shape.E)
-    assert topk_idx.is_cuda and topk_idx.dtype is _I32 and topk_idx.is_contiguous() and topk_idx.shape == (shape.T, shape.k)
+    T, E, k, S = shape.sizes
+    assert logits.is_cuda and logits.dtype is _F32 and logits.is_contiguous() and logits.shape == (T, E)
+    assert topk_idx.is_cuda and topk_idx.dtype is _I32 and topk_idx.is_contiguous() and topk_idx.shape == (T, k)
     if seq_offsets is not None:
         assert seq_offsets.is_cuda and seq_offsets.dtype == torch.int32 and seq_offsets.is_contiguous()
-        assert seq_offsets.shape == (shape.seqs + 1,)
+        assert seq_offsets.shape == (S + 1,)
     if mask is not None:
-        assert mask.is_cuda and mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.shape == (shape.T,)
+        assert mask.is_cuda and mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.shape == (T,)
 
 
 def moe_balance_forward(shape: MoEBalanceShape, logits, topk_idx, seq_offsets=None, mask=None, ws: torch.Tensor | None = None) -> BalanceStats:
     """Balance loss and z loss of a router's logits [T,E] fp32 and its selection [T,k] int32, over the packed sequences that
     seq_offsets [seqs+1] int32 cuts (one without) and the tokens that mask [T] keeps."""
     _balance_inputs(shape, logits, topk_idx, seq_offsets, mask)
-    S = shape.seqs
-    counts = topk_idx.new_empty((S, shape.E))
-    st = BalanceStats(logits.new_empty(3), counts, counts.new_empty(S + 1), logits.new_empty((S, shape.E)), logits.new_empty(shape.T))
+    T, E, _, S = shape.sizes
+    st = BalanceStats(logits.new_empty(3), topk_idx.new_empty((S, E)), topk_idx.new_empty(S + 1), logits.new_empty((S, E)), logits.new_empty(T))
     if ws is None:
         ws = _ws(moe_balance_workspace_bytes(shape), logits.device)
     cs = st.c_struct()
@@ -519,15 +536,16 @@ def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: Balanc
     """Gradient [T,E] of the logits for the gradient dloss [1] of stats.loss[0]; with topk_w and dtopk_w also what
     moe_route_backward would give, added before the one rounding.  seq_offsets as in the forward call; tokens that it did not keep have stats.lse = -inf."""
     _balance_inputs(shape, logits, topk_idx, seq_offsets, None)
+    T, E, k, _ = shape.sizes
     for t in (topk_w, dtopk_w):
         if t is not None:
-            assert t.is_cuda and t.dtype == torch.float32 and t.is_contiguous() and t.shape == (shape.T, shape.k)
-    assert dloss.is_cuda and dloss.dtype == torch.float32 and dloss.numel() == 1
+            assert t.is_cuda and t.dtype is _F32 and t.is_contiguous() and t.shape == (T, k)
+    assert dloss.is_cuda and dloss.dtype is _F32 and dloss.numel() == 1
     assert out_dtype is _F32 or out_dtype is _BF16
     if out is None:
-        out = torch.empty_like(logits) if out_dtype is _F32 else torch.empty((shape.T, shape.E), dtype=_BF16, device=logits.device)
+        out = torch.empty_like(logits) if out_dtype is _F32 else torch.empty((T, E), dtype=_BF16, device=logits.device)
     else:
-        assert out.is_cuda and out.dtype is out_dtype and out.is_contiguous() and out.shape == (shape.T, shape.E)
+        assert out.is_cuda and out.dtype is out_dtype and out.is_contiguous() and out.shape == (T, E)
     cs = stats.c_struct()
     _check(load_library().moe_balance_backward(
         ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), ctypes.byref(cs), _ptr(topk_w), _ptr(dtopk_w),

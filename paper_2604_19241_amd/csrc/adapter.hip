@@ -230,7 +230,8 @@ struct ProjParams {
     const float* h_given;   // the forward call's h
     int tile_rows;
     int span;               // columns of a segment's low-rank part: 2 r, for an fp32 result 3 r
-    int blocks;             // at most, of the plan
+    int blocks;             // at most, of the plan (0: there is none)
+    int join_rows;          // adapter_parts_join_kernel: rows of a workgroup
 };
 struct GradParams {
     int T, r, n, few;
@@ -388,14 +389,26 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
     }
     id -= gemm;
     const int t = id % p.hgroups, rest = id / p.hgroups, rt = rest % p.rank_tiles, sp = rest / p.rank_tiles;
-    const int blocks = (p.T + 31) / 32, a = p.hgroups == p.T ? rfl(adapter_of(p.ids, t, p.n)) : t / blocks;
-    if (a < 0) return;
-    Members mb;
-    mb.find(p.T, p.n, p.ids, a, s_mask);
-    const int rank = p.hgroups == p.T ? mb.before(t) : t % blocks * 32;
-    if (rank % 32 != 0 || rank >= mb.count()) return;
-    mb.list(rank, 32, s_list);
-    const int rows = min(32, mb.count() - rank);
+    int a, rows, rank = 0;
+    if (p.blocks > 0) {   // sorted: a block of the plan
+        if (t >= p.plan.head[0]) return;
+        const int row0 = p.plan.block[2 * t], code = p.plan.block[2 * t + 1];
+        a = (code >> 8) - 1;
+        rows = code & 255;
+        if (a < 0) return;
+        if ((int)threadIdx.x < rows) s_list[threadIdx.x] = p.plan.order[row0 + threadIdx.x];
+        __syncthreads();
+    } else {
+        const int blocks = (p.T + 31) / 32;
+        a = p.hgroups == p.T ? rfl(adapter_of(p.ids, t, p.n)) : t / blocks;
+        if (a < 0) return;
+        Members mb;
+        mb.find(p.T, p.n, p.ids, a, s_mask);
+        rank = p.hgroups == p.T ? mb.before(t) : t % blocks * 32;
+        if (rank % 32 != 0 || rank >= mb.count()) return;
+        mb.list(rank, 32, s_list);
+        rows = min(32, mb.count() - rank);
+    }
     const int s0 = sp * p.hper_split, s1 = min(nst, s0 + p.hper_split);
     if (rank == 0 && rows <= kDotTokens) {
         float* const out = p.hpart + (size_t)sp * p.T * p.r;
@@ -533,7 +546,7 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
 
 // Gradients of 8 ranks of one adapter, token by token.  SHARE: 256 columns, the waves share the tokens and their sums are added in LDS; else
 // 1024 columns, 256 a wave, which keeps the LDS small and the workgroups few where the adapters have few tokens or none (11 tokens, 27 adapters of 64 ranks, 6552 x 464: the
-// training step 66 us with SHARE, NOSHARE without).  (With 512 columns a wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4
+// training step 66 us with SHARE, 51 without).  (With 512 columns a wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4
 // workgroups that took 128 tokens one after the other: 48 us, now 11.)
 constexpr int kGradRanks = 8;
 template <bool SHARE>
@@ -799,6 +812,81 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p
             *(u32x4_t*)(x + 2 * p.r) = rest;
         }
     }
+}
+
+// The second launch where the product is cut into parts (parts_pay): y of up to 16 rows of the plan and 1024 columns, 4 a thread, and with the first
+// columns h and the gradients' terms, as adapter_low_kernel writes them.
+constexpr int kPartsRows = 16;
+__global__ void __launch_bounds__(256) adapter_parts_join_kernel(ProjParams p) {
+    __shared__ float s_h[kPartsRows][kMaxRank];
+    __shared__ int32_t s_tok[kPartsRows], s_a[kPartsRows];
+    const int tid = threadIdx.x, groups = (p.T + p.join_rows - 1) / p.join_rows, row0 = (int)blockIdx.x % groups * p.join_rows, cb = (int)blockIdx.x / groups;
+    const int rows = min(p.join_rows, p.T - row0);
+    if (tid < rows) {
+        const int t = p.plan.order[row0 + tid];
+        s_tok[tid] = t;
+        s_a[tid] = adapter_of(p.ids, t, p.n);
+    }
+    __syncthreads();
+#pragma unroll 1
+    for (int i = tid; i < rows * (p.r / 8); i += 256) {
+        const int m = i / (p.r / 8), col = 8 * (i - m * (p.r / 8)), t = s_tok[m], a = s_a[m];
+        float v[8] = {};
+        if (a >= 0) {
+            const float* const q = p.hpart + (size_t)t * p.r + col;
+#pragma unroll 4
+            for (int k = 0; k < p.hsplits; ++k) {
+                const f32x4_t* const u = (const f32x4_t*)(q + (size_t)k * p.T * p.r);
+                const f32x4_t x = u[0], y = u[1];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[j] += x[j];
+                    v[4 + j] += y[j];
+                }
+            }
+            const float s = p.scale ? p.scale[a] : 1.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] *= s;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s_h[m][col + j] = v[j];
+        if (cb == 0) {
+            f32x4_t* const to = (f32x4_t*)(p.h + (size_t)t * p.r + col);
+            to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
+            to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
+            if (p.terms[0]) {
+                const size_t at = (size_t)(row0 + m) * 3 * p.r + col;
+                store_terms(p.terms[1] + at, p.r, v);
+                const f32x4_t* const g = (const f32x4_t*)(p.h_given + (size_t)t * p.r + col);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[j] = g[0][j];
+                    v[4 + j] = g[1][j];
+                }
+                store_terms(p.terms[0] + at, p.r, v);
+            }
+        }
+    }
+    __syncthreads();
+    const int wide = min(256, (p.C + 3) / 4), m = tid / wide, c = (cb * 256 + tid % wide) * 4;
+    if (m >= rows || c >= p.C) return;
+    const int t = s_tok[m], a = s_a[m];
+    float acc[4] = {};
+    const float* const part = p.part + (size_t)t * p.C + c;
+#pragma unroll 8
+    for (int k = 0; k < p.splits; ++k) {
+        const f32x4_t u = *(const f32x4_t*)(part + (size_t)k * p.T * p.C);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] += u[j];
+    }
+    if (a >= 0) {
+        const char* const f = p.second + ((size_t)a * p.r * p.C + c) * 2;
+#pragma unroll 8
+        for (int j = 0; j < p.r; ++j) fma4(acc, s_h[m][j], *(const u32x2_t*)(f + (size_t)j * p.C * 2));
+    }
+    const size_t at = (size_t)t * p.C + c;
+    if (p.out_f32) *(f32x4_t*)(p.y + at * 4) = f32x4_t{acc[0], acc[1], acc[2], acc[3]};
+    else *(u32x2_t*)(p.y + at * 2) = u32x2_t{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
 }
 
 // sum_j h[j] second[a][j][col ..]: the low-rank part of 8 columns of one row, for tiles in which something is not finite
@@ -1205,7 +1293,7 @@ struct FewPlan {
     int row_frags, col_tiles, row_tiles, rank_tiles, hgroups, splits, per_split, hsplits, hper_split;
 };
 // Parts of at least 4 stages, as many as give every CU a workgroup but no more than the second launch fetches in two goes; h is cut alike, or into fewer parts where every token may be a group of its own.
-static FewPlan few_plan(int T, int R, int C, int r, int n) {
+static FewPlan few_plan(int T, int R, int C, int r, int n, int blocks = 0) {
     FewPlan f;
     f.row_frags = T <= 32 ? 1 : 2;
     f.col_tiles = (C + 63) / 64;
@@ -1215,13 +1303,13 @@ static FewPlan few_plan(int T, int R, int C, int r, int n) {
     const int want = std::max(1, 256 / tiles);
     f.per_split = std::max({4, (nst + want - 1) / want, (nst + kMostSplits - 1) / kMostSplits});
     f.splits = (nst + f.per_split - 1) / f.per_split;
-    f.hgroups = (int)std::min((long long)T, (long long)n * ((T + 31) / 32));
+    f.hgroups = blocks > 0 ? blocks : (int)std::min((long long)T, (long long)n * ((T + 31) / 32));
     f.hper_split = std::max(std::min(f.per_split, 16), (int)(((long long)nst * f.hgroups * f.rank_tiles + 511) / 512));
     f.hsplits = (nst + f.hper_split - 1) / f.hper_split;
     return f;
 }
-static size_t few_bytes(int T, int R, int C, int r, int n) {
-    const FewPlan f = few_plan(T, R, C, r, n);
+static size_t few_bytes(int T, int R, int C, int r, int n, int blocks = 0) {
+    const FewPlan f = few_plan(T, R, C, r, n, blocks);
     return align_up((size_t)f.splits * T * C * 4, 256) + align_up((size_t)f.hsplits * T * r * 4, 256);
 }
 // Tiles of the product.  A stage of 64 k takes about 0.38 us in tiles of 64 x 64 (two on a CU), 0.6 in tiles of 128 x 128, 1.0 in 128 x 256 and 1.45 in 256 x 256, and what counts
@@ -1255,7 +1343,7 @@ static TileShape tile_shape(int T, int C) {
 }
 static size_t hx_most(const moe_adapter_shape_t& s) { return std::max(hx_bytes(s, tile_shape(s.T, s.N).rows), hx_bytes(s, tile_shape(s.T, s.K).rows)); }
 // The factors' gradients: columns of a tile; whether adapters with few rows have a kernel of their own (where they have few on average); and into how many parts
-// an adapter's rows are cut where the tiles would leave more than half of the CUs idle (3594 tokens on one adapter, 2528 x 264: GPARTS1 us in one part, GPARTS2 in
+// an adapter's rows are cut where the tiles would leave more than half of the CUs idle (3594 tokens on one adapter, 2528 x 264: 30.5 us in one part, 13.5 in
 // 7 with the sum of the parts).
 static int grad_cols(int r) { return r > 64 ? 64 : 128; }
 static bool grad_rows(const moe_adapter_shape_t& s) { return (long long)s.adapters * kGradRows >= s.T; }
@@ -1263,11 +1351,20 @@ static int grad_parts(const moe_adapter_shape_t& s) {
     const int cols = grad_cols(s.rank), tiles = s.adapters * ((s.K + cols - 1) / cols + (s.N + cols - 1) / cols);
     return grad_rows(s) ? 1 : std::max(1, std::min(256 / tiles, s.T / (s.adapters * 512)));
 }
-static size_t grad_part_at(const moe_adapter_shape_t& s);
-static size_t many_bytes(const moe_adapter_shape_t& s) {
-    const int parts = grad_parts(s);
-    return grad_part_at(s) + (parts > 1 ? (size_t)parts * s.adapters * s.rank * ((size_t)s.K + s.N) * 4 : 0);
+// Whether a product of sorted tokens is cut along its reduction into fp32 parts, with h beside it, as that of few tokens: long reductions of small results, which
+// tiles in one piece leave to a few CUs, behind an equally long h.  Measured, us of the forward call in one piece / in parts (tokens, K,
+// N): 2608, 6952, 24 58.8 / 30.2; 4099, 2048, 128 27.6 / 24.8; 6793, 5800, 64 50.1 / 45.3; 1214, 5720, 1640 79.4 / 93.6.
+static bool parts_pay(int T, int R, int C) { return T < 16384 && stages_in(R) >= 24 && (long long)T * C <= 640 << 10; }
+static int parts_blocks(const moe_adapter_shape_t& s) { return ((int)plan_blocks(s) + 7) & ~7; }
+static size_t parts_bytes(const moe_adapter_shape_t& s, int R, int C) {
+    return parts_pay(s.T, R, C) ? few_bytes(s.T, R, C, s.rank, s.adapters, parts_blocks(s)) : 0;
 }
+static size_t grad_part_at(const moe_adapter_shape_t& s);
+static size_t parts_at(const moe_adapter_shape_t& s) {
+    const int parts = grad_parts(s);
+    return grad_part_at(s) + (parts > 1 ? align_up((size_t)parts * s.adapters * s.rank * ((size_t)s.K + s.N) * 4, 256) : 0);
+}
+static size_t many_bytes(const moe_adapter_shape_t& s) { return parts_at(s) + std::max(parts_bytes(s, s.K, s.N), parts_bytes(s, s.N, s.K)); }
 static size_t grad_part_at(const moe_adapter_shape_t& s) {
     return align_up(hx_most(s), 256) + align_up((size_t)s.T * s.rank * 4, 256) + align_up((size_t)s.adapters * s.K * s.rank * 2, 256) +
            2 * align_up((size_t)s.T * s.rank * 6, 256);
@@ -1280,7 +1377,7 @@ size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
 }
 
 static void few_params(ProjParams& p, char* ws, FewPlan& f) {
-    f = few_plan(p.T, p.R, p.C, p.r, p.n);
+    f = few_plan(p.T, p.R, p.C, p.r, p.n, p.blocks);
     p.part = (float*)ws;
     p.hpart = (float*)(ws + align_up((size_t)f.splits * p.T * p.C * 4, 256));
     p.splits = f.splits, p.per_split = f.per_split, p.hsplits = f.hsplits, p.hper_split = f.hper_split;
@@ -1303,16 +1400,26 @@ static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan,
     const TileShape tile = tile_shape(p.T, p.C);
     p.tile_rows = tile.rows;
     p.span = (p.out_f32 ? 3 : 2) * p.r;
-    p.blocks = ((int)plan_blocks(s) + 7) & ~7;
+    p.blocks = parts_blocks(s);
     p.hx = ws;
     char* rest = ws + align_up(hx_most(s), 256);
     if (!p.h) p.h = (float*)rest;
     p.second_t = rest + align_up((size_t)s.T * s.rank * 4, 256);
-    const dim3 low((unsigned)(p.blocks + (FORM == kKc ? p.n * ((p.C + 63) / 64) : 0)));
     if (FORM == kKc) {
         p.terms[0] = (uint16_t*)(p.second_t + align_up((size_t)s.adapters * s.K * s.rank * 2, 256));
         p.terms[1] = (uint16_t*)((char*)p.terms[0] + align_up((size_t)s.T * s.rank * 6, 256));
     }
+    if (parts_pay(p.T, p.R, p.C)) {
+        FewPlan f;
+        few_params(p, ws + parts_at(s), f);
+        few_first<FORM>(p, f, st);
+        const int wide = (p.C + 3) / 4;
+        p.join_rows = std::max(1, std::min(kPartsRows, 256 / wide));
+        const unsigned groups = (unsigned)((p.T + p.join_rows - 1) / p.join_rows * ((wide + 255) / 256));
+        hipLaunchKernelGGL(adapter_parts_join_kernel, dim3(groups), dim3(256), 0, st, p);
+        return;
+    }
+    const dim3 low((unsigned)(p.blocks + (FORM == kKc ? p.n * ((p.C + 63) / 64) : 0)));
     auto low_launch = [&](auto nrf) {
         if (p.r <= 32) hipLaunchKernelGGL((adapter_low_kernel<nrf.value, 1>), low, dim3(kSmallThreads), 0, st, p);
         else if (p.r <= 64) hipLaunchKernelGGL((adapter_low_kernel<nrf.value, 2>), low, dim3(kSmallThreads), 0, st, p);

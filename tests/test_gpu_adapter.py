@@ -41,7 +41,9 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     (16500, 136, 72, 48, 7, "scattered", 0, "bf16"),
     # an adapter's rows in several parts
     (4099, 264, 136, 16, 1, "one", 0, "bf16"), (3000, 72, 200, 72, 2, "scattered", 0, "bf16"), (5000, 392, 72, 8, 3, "none", 0, "f32"),
-    # parts of a long reduction in both directions
+    # parts of a long reduction in both directions, few tokens and sorted ones
+    (600, 1544, 1600, 16, 7, "scattered", 0, "bf16"), (2600, 3000, 24, 8, 12, "packed", 8, "bf16"), (1100, 24, 2056, 128, 3, "scattered", 0, "f32"),
+    (900, 1552, 1608, 24, 300, "each", 0, "f32"), (3000, 1600, 520, 40, 2, "one", 0, "bf16"),
     (40, 7000, 4104, 16, 3, "scattered", 0, "bf16"), (400, 5000, 264, 24, 2, "packed", 8, "f32"),
 ]
 
