@@ -121,7 +121,7 @@ __device__ __forceinline__ void write_losses(const BalParams& p, double b, doubl
 template <int G, int NV, bool VEC>
 __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams p) {
     using L = TokenLanes<G, NV, VEC>;
-    constexpr int kMost = 4 * G * NV, kGroups = 64 / G, kU = NV == 1 ? 4 : 1, kSlots = (kMaxTopK + G - 1) / G;
+    constexpr int kMost = 4 * G * NV, kGroups = 64 / G, kU = NV == 1 ? (G == 64 ? 8 : 4) : 1, kSlots = (kMaxTopK + G - 1) / G;
     __shared__ float s_p[kBalWaves][kMost];
     __shared__ int32_t s_c[kMost];
     __shared__ float s_z[kBalWaves];
@@ -149,9 +149,10 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
                 const int t = t0 + u * kBalWaves * kGroups;
                 keep[u] = t < b && (!p.mask || p.mask[t]);
             }
+            // (fetched whether they are kept or not: behind the mask they would wait for it)
 #pragma unroll
             for (int u = 0; u < kU; ++u)
-                if (keep[u]) {
+                if (t0 + u * kBalWaves * kGroups < b) {
                     const size_t t = t0 + u * kBalWaves * kGroups;
                     ln.template load<f32x4_t>(p.logits + t * E, E, -INFINITY, x[u]);
 #pragma unroll
