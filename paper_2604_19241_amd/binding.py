@@ -391,6 +391,7 @@ class AdapterPlan:
     """The tokens of one batch by adapter.  `ids` has to stay as it is while the plan is in use."""
     ids: torch.Tensor                 # [T] i32, outside [0, adapters): no adapter
     table: Optional[torch.Tensor]     # None for few tokens: nothing is sorted
+    adapters: int = 0                 # that the table was made for
 
 
 def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
@@ -402,7 +403,7 @@ def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
     table = ids.new_empty(nbytes // 4)
     _check(load_library().moe_adapter_plan(ctypes.byref(shape), _ptr(ids), _ptr(table), nbytes, _stream(ids.device)),
            "moe_adapter_plan")
-    return AdapterPlan(ids, table)
+    return AdapterPlan(ids, table, shape.sizes[4])
 
 
 _BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
@@ -422,7 +423,7 @@ def _adapter_operands(shape: MoEAdapterShape, w, a, b, scale, plan: AdapterPlan)
     assert a.is_cuda and a.dtype is _BF16 and a.is_contiguous() and a.shape == (n, r, K)
     assert b.is_cuda and b.dtype is _BF16 and b.is_contiguous() and b.shape == (n, r, N)
     assert scale is None or (scale.is_cuda and scale.dtype is _F32 and scale.is_contiguous() and scale.shape == (n,))
-    assert plan.ids.shape == (T,)
+    assert plan.ids.shape == (T,) and (plan.table is None or plan.adapters == n)
 
 
 def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, scale=None, out_dtype=torch.bfloat16,

@@ -26,7 +26,7 @@ constexpr int kGradRows = 64;         // rows up to which an adapter's gradients
 constexpr int kUnit = 64;             // rows of which the plan knows the first and the last segment
 
 // ------------------------------------------------------------------ the plan
-// int32 words: [0] blocks, [1] segments, [2] rows without an adapter, [3] adapters with many rows, then the arrays.
+// int32 words: [0] blocks, [1] adapters with many rows, then the arrays.
 struct PlanView {
     int32_t* head;
     int32_t* order;      // [T] row -> token: those without an adapter, then by adapter, each in the order of the tokens
@@ -34,7 +34,7 @@ struct PlanView {
     int32_t* ordinal;    // [n] which segment an adapter is
     int32_t* seg;        // [n] segment -> adapter
     int32_t* unit;       // [units][2] segments of the first and the last row of every kUnit rows (-1: no adapter)
-    int32_t* many;       // [n] adapters with more than kGradRows rows (as many as head[3] says)
+    int32_t* many;       // [n] adapters with more than kGradRows rows (as many as head[1] says)
     int32_t* block;      // [blocks][2] first row; rows | (adapter + 1) << 8.  One adapter, one multiple of block_rows
 };
 static size_t plan_blocks(const moe_adapter_shape_t& s) { return (size_t)s.T / block_rows(s.T) + s.adapters + 2; }
@@ -158,9 +158,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         fblock[bins] = base_blocks;
         v.start[n] = T;
         v.head[0] = base_blocks;
-        v.head[1] = base_segs & 0xffff;
-        v.head[3] = base_segs >> 16;
-        v.head[2] = bins > 1 ? first[1] : T;
+        v.head[1] = base_segs >> 16;
     }
     __syncthreads();
     // rows
@@ -1127,7 +1125,7 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     const int tiles = g.col_tiles[0] + g.col_tiles[1], per = (tiles + 7) >> 3, slot = blockIdx.x >> 3;
     int a = slot / per;
     if (g.few) {
-        if (a >= p.plan.head[3]) return;
+        if (a >= p.plan.head[1]) return;
         a = p.plan.many[a];
     }
     int ct = (blockIdx.x & 7) * per + slot % per;

@@ -29,7 +29,7 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     (200, 136, 2056, 8, 256, "each", 0, "bf16"), (256, 448, 264, 128, 1, "one", 0, "f32"), (256, 512, 1024, 8, 2, "packed", 0, "bf16"),
     (257, 64, 64, 8, 1, "one", 0, "bf16"), (257, 8, 16, 8, 300, "each", 0, "f32"), (300, 328, 200, 24, 5, "outside", 8, "bf16"),
     (512, 1160, 264, 96, 2, "one", 0, "bf16"), (500, 72, 2056, 128, 9, "scattered", 0, "bf16"), (301, 2056, 136, 128, 2, "each", 0, "bf16"),
-    (500, 72, 3000, 128, 20, "scattered", 0, "f32"), (500, 72, 2056, 16, 9, "scattered", 0, "bf16"),
+    (500, 72, 3000, 128, 20, "scattered", 0, "f32"), (500, 2200, 72, 128, 3, "scattered", 0, "bf16"), (64, 16400, 40, 128, 2, "scattered", 0, "bf16"), (500, 72, 2056, 16, 9, "scattered", 0, "bf16"),
     # more tokens: sorted by adapter
     (513, 64, 64, 8, 1, "one", 0, "bf16"), (513, 8, 16, 8, 600, "each", 0, "f32"), (600, 328, 200, 24, 5, "outside", 8, "bf16"),
     (1011, 136, 72, 16, 256, "scattered", 0, "bf16"), (640, 1000, 520, 64, 3, "packed", 64, "f32"), (1021, 264, 712, 128, 2, "scattered", 0, "bf16"),
@@ -94,6 +94,9 @@ def test_a_plan_serves_other_widths():
     one, two = ac.make(T, 136, 264, r, n, "scattered"), ac.make(T, 520, 72, 40, n, "scattered")
     plan = moe.moe_adapter_plan(moe.make_adapter_shape(T, 136, 264, r, n), one["ids"])
     two["ids"] = one["ids"]
+    with pytest.raises(AssertionError):   # but no other number of adapters
+        six = ac.make(T, 520, 72, 40, 6, "scattered")
+        moe.moe_adapter_forward(moe.make_adapter_shape(T, 520, 72, 40, 6), six["x"], six["w"], six["a"], six["b"], plan)
     y = moe.moe_adapter_forward(moe.make_adapter_shape(T, 520, 72, 40, n), two["x"], two["w"], two["a"], two["b"], plan, scale=two["scale"])
     assert torch.equal(y, run(two, 40, n, backward=False)["y"])
 
