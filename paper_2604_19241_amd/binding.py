@@ -3,12 +3,14 @@
 Argument marshalling only: torch supplies device memory and the current HIP
 stream; every step of the hot path runs in the library's kernels.  There is
 no CPU fallback: a missing library or a failed call raises.
+
+The calls that take longer on the host than on the GPU in Python (the projection with adapters and the balance loss) check their tensors and
+allocate their outputs in an extension module (csrc/call.cpp), which calls the same library.
 """
 from __future__ import annotations
 
 import ctypes
 from dataclasses import dataclass
-from functools import lru_cache
 from pathlib import Path
 from typing import Optional
 
@@ -16,6 +18,7 @@ import torch
 
 _PKG = Path(__file__).resolve().parent
 LIB_PATH = _PKG / "libuniep_moe.so"
+CALL_PATH = _PKG / "_call.so"
 
 MOE_OK = 0
 MOE_ERR_ARG, MOE_ERR_SHAPE, MOE_ERR_WORKSPACE, MOE_ERR_HIP, MOE_ERR_DEVICE = -1, -2, -3, -4, -5
@@ -126,6 +129,31 @@ def _stream(device):
         raise ValueError(f"expected a cuda device, but got: {device}")
     # (the handle itself: a Stream object around it takes 1.8 us, as long as a launch)
     return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device() if device.index is None else device.index)
+
+
+_call = None
+_BF16, _F32 = torch.bfloat16, torch.float32
+_addressof = ctypes.addressof
+
+
+def _load_call():
+    """The extension module behind the short calls; raises if it was not built."""
+    global _call
+    if _call is None:
+        lib = load_library()
+        if not CALL_PATH.exists():
+            raise FileNotFoundError(f"{CALL_PATH} is missing: build it with `python -m paper_2604_19241_amd.build`.")
+        from . import _call as module
+        names = ("moe_adapter_plan", "moe_adapter_forward", "moe_adapter_backward", "moe_balance_forward", "moe_balance_backward",
+                 "moe_adapter_workspace_bytes", "moe_balance_workspace_bytes")
+        module.bind(*[ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names])
+        _call = module
+    return _call
+
+
+def _raw_stream(t: torch.Tensor) -> int:
+    """Handle of the stream that is current on t's device (0 on the CPU: the call itself refuses the tensor)."""
+    return torch._C._cuda_getCurrentRawStream(t.get_device()) if t.is_cuda else 0
 
 
 def moe_workspace_bytes(shape: MoEShape) -> dict:
@@ -360,22 +388,12 @@ def saved_views(shape: MoEShape, saved: torch.Tensor) -> dict:
 class MoEAdapterShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "K", "N", "rank", "adapters")]
 
-    def __init__(self, T, K, N, rank, adapters):
-        super().__init__(T, K, N, rank, adapters)
-        self.sizes = (T, K, N, rank, adapters)   # (a field of the structure takes as long to read as a tensor's property)
-
 
 def make_adapter_shape(T, K, N, rank, adapters) -> MoEAdapterShape:
     return MoEAdapterShape(T, K, N, rank, adapters)
 
 
 def _adapter_bytes(shape: MoEAdapterShape) -> tuple:
-    return _adapter_sizes_bytes(*shape.sizes)
-
-
-@lru_cache(maxsize=1024)
-def _adapter_sizes_bytes(*sizes) -> tuple:
-    shape = MoEAdapterShape(*sizes)
     ws, plan = ctypes.c_size_t(0), ctypes.c_size_t(0)
     _check(load_library().moe_adapter_workspace_bytes(ctypes.byref(shape), ctypes.byref(ws), ctypes.byref(plan)),
            "moe_adapter_workspace_bytes")
@@ -396,34 +414,11 @@ class AdapterPlan:
 
 def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
     """Sorts the tokens by adapter, once for all projections of the batch with as many adapters."""
-    assert ids.is_cuda and ids.dtype is _I32 and ids.is_contiguous() and ids.shape == shape.sizes[:1]
-    nbytes = _adapter_bytes(shape)[1]
-    if nbytes == 0:
-        return AdapterPlan(ids, None)
-    table = ids.new_empty(nbytes // 4)
-    _check(load_library().moe_adapter_plan(ctypes.byref(shape), _ptr(ids), _ptr(table), nbytes, _stream(ids.device)),
-           "moe_adapter_plan")
-    return AdapterPlan(ids, table, shape.sizes[4])
-
-
-_BF16, _F32, _I32 = torch.bfloat16, torch.float32, torch.int32
-
-
-def _adapter_rows(t: torch.Tensor, T: int, width: int) -> int:
-    """Elements from one row of t to the next."""
-    ld, one = t.stride()
-    assert t.is_cuda and t.dtype is _BF16 and t.shape == (T, width) and one == 1
-    return ld if T > 1 else width
-
-
-def _adapter_operands(shape: MoEAdapterShape, w, a, b, scale, plan: AdapterPlan):
-    T, K, N, r, n = shape.sizes
-    # (written out: a generator over the operands took as long as half a launch)
-    assert w.is_cuda and w.dtype is _BF16 and w.is_contiguous() and w.shape == (K, N)
-    assert a.is_cuda and a.dtype is _BF16 and a.is_contiguous() and a.shape == (n, r, K)
-    assert b.is_cuda and b.dtype is _BF16 and b.is_contiguous() and b.shape == (n, r, N)
-    assert scale is None or (scale.is_cuda and scale.dtype is _F32 and scale.is_contiguous() and scale.shape == (n,))
-    assert plan.ids.shape == (T,) and (plan.table is None or plan.adapters == n)
+    call = _call or _load_call()
+    out = call.adapter_plan(_addressof(shape), ids, _raw_stream(ids))
+    if type(out) is int:
+        _check(out, "moe_adapter_plan")
+    return AdapterPlan(ids, out, shape.adapters)
 
 
 def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, scale=None, out_dtype=torch.bfloat16,
@@ -431,42 +426,24 @@ def moe_adapter_forward(shape: MoEAdapterShape, x, w, a, b, plan: AdapterPlan, s
     """y[t] = x[t] w + scale[i] (x[t] a[i]^T) b[i] with i = ids[t]: x [T,K] (rows may be parts of wider ones), w [K,N],
     a [adapters,rank,K], b [adapters,rank,N], all bf16; scale [adapters] fp32.  h [T,rank] fp32, if given, receives what
     moe_adapter_backward reads."""
-    T, K, N, rank, _ = shape.sizes
-    ldx = _adapter_rows(x, T, K)
-    _adapter_operands(shape, w, a, b, scale, plan)
     assert out_dtype is _BF16 or out_dtype is _F32
-    if y is None:   # (new_empty with a type takes a microsecond more)
-        y = x.new_empty((T, N)) if out_dtype is _BF16 else torch.empty((T, N), dtype=_F32, device=x.device)
-    else:
-        assert y.is_cuda and y.dtype is out_dtype and y.is_contiguous() and y.shape == (T, N)
-    if h is not None:
-        assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (T, rank)
-    if ws is None:
-        ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
-    _check(load_library().moe_adapter_forward(
-        ctypes.byref(shape), _ptr(x), ldx, _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.ids), _ptr(plan.table), _ptr(y),
-        1 if out_dtype is _F32 else 0, _ptr(h), _ptr(ws), ws.numel(), _stream(x.device)), "moe_adapter_forward")
-    return y
+    call = _call or _load_call()
+    out = call.adapter_forward(_addressof(shape), x, w, a, b, scale, plan.ids, plan.table, plan.adapters, out_dtype is _F32, h, y, ws, _raw_stream(x))
+    if type(out) is int:
+        _check(out, "moe_adapter_forward")
+    return out
 
 
 def moe_adapter_backward(shape: MoEAdapterShape, dy, x, w, a, b, plan: AdapterPlan, h, scale=None, out: dict | None = None,
                          ws: torch.Tensor | None = None) -> dict:
     """Gradients of x (bf16) and of every adapter's two factors (fp32); w is frozen.  h as moe_adapter_forward wrote it."""
-    T, K, N, rank, _ = shape.sizes
-    lddy, ldx = _adapter_rows(dy, T, N), _adapter_rows(x, T, K)
-    _adapter_operands(shape, w, a, b, scale, plan)
-    assert h.is_cuda and h.dtype is _F32 and h.is_contiguous() and h.shape == (T, rank)
+    call = _call or _load_call()
+    dx, da, db = (None, None, None) if out is None else (out["dx"], out["da"], out["db"])
+    got = call.adapter_backward(_addressof(shape), dy, x, w, a, b, scale, plan.ids, plan.table, plan.adapters, h, dx, da, db, ws, _raw_stream(x))
+    if type(got) is int:
+        _check(got, "moe_adapter_backward")
     if out is None:
-        out = {"dx": torch.empty_like(x) if ldx == K else x.new_empty((T, K)), "da": h.new_empty(a.shape), "db": h.new_empty(b.shape)}
-    else:
-        for key, dtype, size in (("dx", _BF16, x.shape), ("da", _F32, a.shape), ("db", _F32, b.shape)):
-            t = out[key]
-            assert t.is_cuda and t.dtype is dtype and t.is_contiguous() and t.shape == size
-    if ws is None:
-        ws = _ws(moe_adapter_workspace_bytes(shape), x.device)
-    _check(load_library().moe_adapter_backward(
-        ctypes.byref(shape), _ptr(dy), lddy, _ptr(x), ldx, _ptr(w), _ptr(a), _ptr(b), _ptr(scale), _ptr(plan.ids), _ptr(plan.table),
-        _ptr(h), _ptr(out["dx"]), _ptr(out["da"]), _ptr(out["db"]), _ptr(ws), ws.numel(), _stream(x.device)), "moe_adapter_backward")
+        out = {"dx": got[0], "da": got[1], "db": got[2]}
     return out
 
 
@@ -474,10 +451,6 @@ def moe_adapter_backward(shape: MoEAdapterShape, dy, x, w, a, b, plan: AdapterPl
 
 class MoEBalanceShape(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("T", "E", "k", "seqs")] + [(n, ctypes.c_float) for n in ("balance_coef", "z_coef")]
-
-    def __init__(self, T, E, k, seqs, balance_coef, z_coef):
-        super().__init__(T, E, k, seqs, balance_coef, z_coef)
-        self.sizes = (T, E, k, seqs)
 
 
 class MoEBalanceStatsC(ctypes.Structure):
@@ -492,10 +465,6 @@ class BalanceStats:
     prob_sums: torch.Tensor   # [seqs,E] f32
     lse: torch.Tensor         # [T] f32, -inf where a token is not kept
 
-    def c_struct(self) -> MoEBalanceStatsC:
-        return MoEBalanceStatsC(self.loss.data_ptr(), self.counts.data_ptr(), self.tokens.data_ptr(), self.prob_sums.data_ptr(),
-                                self.lse.data_ptr())
-
 
 def make_balance_shape(T, E, k, seqs=1, balance_coef=0.01, z_coef=0.001) -> MoEBalanceShape:
     return MoEBalanceShape(T, E, k, seqs, balance_coef, z_coef)
@@ -507,51 +476,27 @@ def moe_balance_workspace_bytes(shape: MoEBalanceShape) -> int:
     return ws.value
 
 
-def _balance_inputs(shape: MoEBalanceShape, logits, topk_idx, seq_offsets, mask):
-    T, E, k, S = shape.sizes
-    assert logits.is_cuda and logits.dtype is _F32 and logits.is_contiguous() and logits.shape == (T, E)
-    assert topk_idx.is_cuda and topk_idx.dtype is _I32 and topk_idx.is_contiguous() and topk_idx.shape == (T, k)
-    if seq_offsets is not None:
-        assert seq_offsets.is_cuda and seq_offsets.dtype == torch.int32 and seq_offsets.is_contiguous()
-        assert seq_offsets.shape == (S + 1,)
-    if mask is not None:
-        assert mask.is_cuda and mask.dtype in (torch.bool, torch.uint8) and mask.is_contiguous() and mask.shape == (T,)
-
-
 def moe_balance_forward(shape: MoEBalanceShape, logits, topk_idx, seq_offsets=None, mask=None, ws: torch.Tensor | None = None) -> BalanceStats:
     """Balance loss and z loss of a router's logits [T,E] fp32 and its selection [T,k] int32, over the packed sequences that
-    seq_offsets [seqs+1] int32 cuts (one without) and the tokens that mask [T] keeps."""
-    _balance_inputs(shape, logits, topk_idx, seq_offsets, mask)
-    T, E, _, S = shape.sizes
-    st = BalanceStats(logits.new_empty(3), topk_idx.new_empty((S, E)), topk_idx.new_empty(S + 1), logits.new_empty((S, E)), logits.new_empty(T))
-    if ws is None:
-        ws = _ws(moe_balance_workspace_bytes(shape), logits.device)
-    cs = st.c_struct()
-    _check(load_library().moe_balance_forward(ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), _ptr(mask),
-                                              ctypes.byref(cs), _ptr(ws), ws.numel(), _stream(logits.device)), "moe_balance_forward")
-    return st
+    seq_offsets [seqs+1] int32 cuts (one without) and the tokens that mask [T] (bool or uint8) keeps."""
+    call = _call or _load_call()
+    out = call.balance_forward(_addressof(shape), logits, topk_idx, seq_offsets, mask, ws, _raw_stream(logits))
+    if type(out) is int:
+        _check(out, "moe_balance_forward")
+    return BalanceStats(*out)
 
 
 def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: BalanceStats, dloss, seq_offsets=None, topk_w=None,
                          dtopk_w=None, out_dtype=torch.float32, out: torch.Tensor | None = None) -> torch.Tensor:
     """Gradient [T,E] of the logits for the gradient dloss [1] of stats.loss[0]; with topk_w and dtopk_w also what
     moe_route_backward would give, added before the one rounding.  seq_offsets as in the forward call; tokens that it did not keep have stats.lse = -inf."""
-    _balance_inputs(shape, logits, topk_idx, seq_offsets, None)
-    T, E, k, _ = shape.sizes
-    for t in (topk_w, dtopk_w):
-        if t is not None:
-            assert t.is_cuda and t.dtype is _F32 and t.is_contiguous() and t.shape == (T, k)
-    assert dloss.is_cuda and dloss.dtype is _F32 and dloss.numel() == 1
     assert out_dtype is _F32 or out_dtype is _BF16
-    if out is None:
-        out = torch.empty_like(logits) if out_dtype is _F32 else torch.empty((T, E), dtype=_BF16, device=logits.device)
-    else:
-        assert out.is_cuda and out.dtype is out_dtype and out.is_contiguous() and out.shape == (T, E)
-    cs = stats.c_struct()
-    _check(load_library().moe_balance_backward(
-        ctypes.byref(shape), _ptr(logits), _ptr(topk_idx), _ptr(seq_offsets), ctypes.byref(cs), _ptr(topk_w), _ptr(dtopk_w),
-        _ptr(dloss), _ptr(out), 1 if out_dtype == torch.bfloat16 else 0, _stream(logits.device)), "moe_balance_backward")
-    return out
+    call = _call or _load_call()
+    got = call.balance_backward(_addressof(shape), logits, topk_idx, seq_offsets, stats.counts, stats.tokens, stats.lse, topk_w, dtopk_w, dloss,
+                                out_dtype is _BF16, out, _raw_stream(logits))
+    if type(got) is int:
+        _check(got, "moe_balance_backward")
+    return got
 
 
 # ---- analytical performance model and configuration search (host only) -------

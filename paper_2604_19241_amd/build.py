@@ -1,4 +1,4 @@
-"""Builds libuniep_moe.so (HIP, gfx950 only) in-tree with hipcc.
+"""Builds libuniep_moe.so (HIP, gfx950 only) in-tree with hipcc, and the binding's extension module with g++.
 
 Objects and compiler temporaries go to <repo>/_build/; the shared library is
 written next to this file so that it travels with the source tree.
@@ -14,6 +14,7 @@ from pathlib import Path
 PKG = Path(__file__).resolve().parent
 CSRC = PKG / "csrc"
 LIB = PKG / "libuniep_moe.so"
+CALL = PKG / "_call.so"                  # host side of the short calls (csrc/call.cpp)
 BUILD = PKG.parent / "_build"
 SOURCES = ["route.hip", "forward.hip", "backward.hip", "adapter.hip", "balance.hip", "api.hip", "perf_model.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
@@ -39,10 +40,24 @@ def _compile(src: str, save_temps: bool) -> Path:
     return obj
 
 
+def _build_call() -> None:
+    """The extension module that checks, allocates and calls for binding.py (host code: g++)."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    inc = [f"-I{d}" for d in (*cpp_extension.include_paths(), sysconfig.get_paths()["include"])]
+    lib = [f"-L{d}" for d in cpp_extension.library_paths()]
+    subprocess.run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                    *inc, str(CSRC / "call.cpp"), "-o", str(CALL), *lib, "-lc10", "-ltorch_cpu", "-ltorch", "-ltorch_python"], check=True)
+
+
 def build(save_temps: bool = False, jobs: int = 6) -> Path:
     BUILD.mkdir(exist_ok=True)
     with ThreadPoolExecutor(max_workers=jobs) as ex:
+        call = ex.submit(_build_call)
         objs = list(ex.map(lambda s: _compile(s, save_temps), SOURCES))
+        call.result()
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", *map(str, objs), "-o", str(LIB)]
     subprocess.run(cmd, check=True)
     return LIB

@@ -201,3 +201,39 @@ def test_in_a_graph_and_behind_other_work_of_the_stream():
             torch.cuda.synchronize()
             assert all(torch.equal(out[k], want[k]) for k in out), (T, turn)
             assert all(torch.equal(v, want[k]) for k, v in step().items()), (T, turn)
+
+
+def test_other_tensors_are_refused():
+    T, K, N, r, n = 40, 64, 72, 8, 3
+    s = ac.make(T, K, N, r, n, "scattered", 8)
+    shape = moe.make_adapter_shape(T, K, N, r, n)
+    plan = moe.moe_adapter_plan(shape, s["ids"])
+    h = torch.zeros((T, r), device="cuda")
+    forward = {"x": s["x"], "w": s["w"], "a": s["a"], "b": s["b"], "scale": s["scale"], "h": h}
+    backward = forward | {"dy": s["dy"]}
+
+    def call(back, kw):
+        kw, args = dict(kw), [shape]
+        for name in ("dy", "x", "w", "a", "b") if back else ("x", "w", "a", "b"):
+            args.append(kw.pop(name))
+        (moe.moe_adapter_backward if back else moe.moe_adapter_forward)(*args, plan, **kw)
+
+    call(False, forward)
+    call(True, backward)
+    for back, good in ((False, forward), (True, backward)):
+        for name, t in good.items():
+            wrong = [t.cpu(), t.double(), t[..., :-1], t[None]]
+            if t.dim() > 1:
+                wrong.append(t.transpose(-1, -2).contiguous().transpose(-1, -2))   # right sizes, the other order
+            for bad in wrong:
+                with pytest.raises(AssertionError):
+                    call(back, good | {name: bad})
+    with pytest.raises(AssertionError):
+        call(False, forward | {"y": torch.empty((T, N), device="cuda")})           # fp32 where bf16 is asked for
+    with pytest.raises(AssertionError):
+        call(False, forward | {"ws": torch.empty(1 << 20, device="cuda")})
+    with pytest.raises(RuntimeError):
+        call(False, forward | {"ws": torch.empty(0, dtype=torch.uint8, device="cuda")})   # too small
+    for bad in (s["ids"].long(), s["ids"][:-1], s["ids"].cpu()):
+        with pytest.raises(AssertionError):
+            moe.moe_adapter_plan(shape, bad)

@@ -215,3 +215,30 @@ def test_in_a_graph():
         assert torch.equal(st.loss, want.loss) and torch.equal(st.counts, want.counts) and torch.equal(d, dwant)
         again, dagain = run(t)
         assert torch.equal(again.loss, want.loss) and torch.equal(dagain, dwant)
+
+
+def test_other_tensors_are_refused():
+    T, E, k = 40, 24, 4
+    shape = moe.make_balance_shape(T, E, k, seqs=2, balance_coef=0.01, z_coef=0.001)
+    logits = torch.randn((T, E), device="cuda")
+    good = {"logits": logits, "topk_idx": logits.topk(k).indices.int(), "seq_offsets": torch.tensor([0, 7, T], dtype=torch.int32, device="cuda"),
+            "mask": torch.ones(T, dtype=torch.bool, device="cuda")}
+    stats = moe.moe_balance_forward(shape, **good)
+    back = {"logits": logits, "topk_idx": good["topk_idx"], "seq_offsets": good["seq_offsets"], "stats": stats, "dloss": torch.ones(1, device="cuda"),
+            "topk_w": torch.rand((T, k), device="cuda"), "dtopk_w": torch.rand((T, k), device="cuda")}
+    moe.moe_balance_backward(shape, **back)
+    for call, kw in ((moe.moe_balance_forward, good), (moe.moe_balance_backward, back)):
+        for name, t in kw.items():
+            if name == "stats":
+                continue
+            wrong = [t.cpu(), t.double(), t[..., :-1]]
+            if t.dim() > 1:
+                wrong.append(t.t().contiguous().t())
+            for bad in wrong:
+                with pytest.raises(AssertionError):
+                    call(shape, **kw | {name: bad})
+    for field in ("counts", "tokens", "lse"):
+        bad = moe.BalanceStats(stats.loss, stats.counts, stats.tokens, stats.prob_sums, stats.lse)
+        setattr(bad, field, getattr(stats, field)[..., :-1])
+        with pytest.raises(AssertionError):
+            moe.moe_balance_backward(shape, **back | {"stats": bad})

@@ -120,3 +120,22 @@ def test_the_binding_refuses_other_tensors():
         moe.moe_adapter_plan(s, torch.zeros(600, dtype=torch.int32))   # not on the GPU
     with pytest.raises(AssertionError):
         moe.moe_balance_forward(moe.make_balance_shape(4, 8, 2), torch.zeros((4, 8)), torch.zeros((4, 2), dtype=torch.int32))
+
+
+def test_the_binding_fails_loudly_without_its_extension_module(monkeypatch, tmp_path):
+    monkeypatch.setattr(b, "_call", None)
+    monkeypatch.setattr(b, "CALL_PATH", tmp_path / "nope.so")
+    with pytest.raises(FileNotFoundError):
+        moe.moe_adapter_plan(moe.make_adapter_shape(**GOOD), torch.zeros(600, dtype=torch.int32))
+
+
+def test_the_extension_module_refuses_what_is_no_argument():
+    call, s = b._load_call(), moe.make_adapter_shape(**GOOD)
+    with pytest.raises(TypeError):
+        call.adapter_plan(0)
+    with pytest.raises(ValueError):
+        call.adapter_plan(0, torch.zeros(600, dtype=torch.int32), 0)
+    with pytest.raises(AssertionError):
+        call.adapter_plan(b.ctypes.addressof(s), None, 0)
+    with pytest.raises(TypeError):
+        call.adapter_plan("shape", torch.zeros(600, dtype=torch.int32), 0)
