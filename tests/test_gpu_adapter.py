@@ -237,3 +237,27 @@ def test_other_tensors_are_refused():
     for bad in (s["ids"].long(), s["ids"][:-1], s["ids"].cpu()):
         with pytest.raises(AssertionError):
             moe.moe_adapter_plan(shape, bad)
+
+
+@pytest.mark.parametrize("T,K,N,r,n", [(5, 64, 72, 8, 4), (48, 264, 392, 16, 4), (300, 136, 264, 16, 100), (512, 64, 512, 16, 4), (700, 264, 392, 16, 4), (900, 1552, 1608, 24, 300), (1011, 136, 72, 16, 256),
+                                       (4200, 72, 1032, 16, 4), (4200, 1032, 72, 64, 5), (8300, 1544, 136, 16, 4), (3000, 72, 200, 72, 2), (16500, 584, 264, 128, 3)])
+def test_tokens_that_are_not_finite_stay_by_themselves(T, K, N, r, n):
+    """Other tokens' rows, and the gradients of adapters that have none of these tokens."""
+    s = ac.make(T, K, N, r, n, "scattered")
+    clean = run(s, r, n)
+    v, m = ac.plain(s)
+    e = ac.bounds(s, v, m, False)
+    ids = s["ids"]
+    for where in (ids == 1, (ids == -1)):
+        for name, value in (("x", float("nan")), ("x", float("inf")), ("dy", float("-inf")), ("dy", float("nan"))):
+            say(f"[adapter] {T} {K} {N}: {name} holds {value}")
+            bad = dict(s)
+            bad[name] = s[name].clone()
+            bad[name][where, 3:9] = value
+            got = run(bad, r, n)
+            for key in ("y", "dx"):
+                ac.check(got[key][~where], v[key][~where], e[key][~where], (T, name, value, key))
+            assert torch.equal(got["h"][~where], clean["h"][~where])
+            for i in range(n):
+                if not (where & (ids == i)).any():
+                    assert torch.equal(got["da"][i], clean["da"][i]) and torch.equal(got["db"][i], clean["db"][i]), (name, value, i)
