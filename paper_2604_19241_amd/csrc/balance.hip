@@ -391,15 +391,17 @@ __global__ void __launch_bounds__(kBalThreads) balance_backward_kernel(BalParams
 #pragma unroll
                     for (int v = 0; v < L::kValues; ++v) f[v] = scale * (float)cnt[v];
                 }
-                float inner = 0.f;
+                // (divided by their sum: lse has been rounded, which for logits of thousands is a factor of 1e-4 to all of them)
+                float inner = 0.f, q = 0.f;
 #pragma unroll
                 for (int v = 0; v < L::kValues; ++v) {
                     d[u][v] = ln.expert(v) < E ? __expf(d[u][v] - lse[u]) : 0.f;
                     inner += f[v] * d[u][v];
+                    q += d[u][v];
                 }
-                const float add = cz * lse[u] - L::sum(inner);
+                const float inv = 1.f / L::sum(q), add = cz * lse[u] - L::sum(inner) * inv;
 #pragma unroll
-                for (int v = 0; v < L::kValues; ++v) d[u][v] *= f[v] + add;
+                for (int v = 0; v < L::kValues; ++v) d[u][v] *= (f[v] + add) * inv;
             } else {
 #pragma unroll
                 for (int v = 0; v < L::kValues; ++v) d[u][v] = 0.f;

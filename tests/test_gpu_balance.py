@@ -242,3 +242,18 @@ def test_other_tensors_are_refused():
         setattr(bad, field, getattr(stats, field)[..., :-1])
         with pytest.raises(AssertionError):
             moe.moe_balance_backward(shape, **back | {"stats": bad})
+
+
+@pytest.mark.parametrize("E,k", [(8, 2), (20, 4), (60, 6), (128, 8), (257, 8)])
+def test_logits_far_from_zero(E, k):
+    """lse is rounded to fp32, by 1e-3 at 3e4; the probabilities know only their differences."""
+    s = make(300, E, k, S=3, gates=False)
+    s["logits"] = s["logits"] + torch.linspace(-3e4, 3e4, 300, device="cuda")[:, None]
+    st, d = run(s)
+    v = plain(s)
+    rel = 64 * 2.0 ** -23   # of a probability, as in check()
+    scale = v["p"] * 0.75 * (BC * E * 2 + ZC * 2 * v["lse"].abs()[:, None]) / 300
+    err = rel * scale + 16 * 2.0 ** -23 * v["dlogits"].abs()
+    assert ((st.lse.double() - v["lse"]).abs() <= 8 * 2.0 ** -23 * (v["lse"].abs() + 2)).all()
+    assert ((st.prob_sums.double() - v["prob_sums"]).abs() <= rel * v["prob_sums"] + 1e-30).all()
+    assert ((d.double() - v["dlogits"]).abs() <= err + 1e-30).all()
