@@ -261,3 +261,34 @@ def test_tokens_that_are_not_finite_stay_by_themselves(T, K, N, r, n):
             for i in range(n):
                 if not (where & (ids == i)).any():
                     assert torch.equal(got["da"][i], clean["da"][i]) and torch.equal(got["db"][i], clean["db"][i]), (name, value, i)
+
+
+def test_offsets_beyond_32_bits():
+    """Rows that lie far apart, and results of more than 2^32 bytes."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    for T, K, N, apart in ((600, 64, 72, 1 << 22), (40, 64, 72, 1 << 26), (34000, 64, 65536, 0)):
+        say(f"[adapter] {T} {K} {N}, rows {apart} apart")
+        r, n = 16, 3
+        s = ac.make(min(T, 2), K, 8, r, n, "one")   # (w and b below)
+        wide = torch.empty((T, max(apart, K)), dtype=torch.bfloat16, device="cuda")
+        wide[:, :K] = torch.randn((T, K), generator=g, device="cuda").to(torch.bfloat16)
+        s |= {"x": wide[:, :K], "ids": ac.ids_of("scattered", T, n), "w": (torch.randn((K, N), generator=g, device="cuda") * K ** -0.5).to(torch.bfloat16),
+              "b": (torch.randn((n, r, N), generator=g, device="cuda") * 0.3).to(torch.bfloat16)}
+        dy = torch.empty((T, max(apart, N)), dtype=torch.bfloat16, device="cuda")
+        for i in range(0, T, 2000):
+            dy[i:i + 2000, :N] = torch.randn((min(2000, T - i), N), generator=g, device="cuda").to(torch.bfloat16)
+        s["dy"] = dy[:, :N]
+        got = run(s, r, n)
+        # rows of the results by themselves, and a few columns of the gradient that every row of dy is part of
+        at = torch.tensor(sorted({0, 1, T // 2, T - 2, T - 1} | set(range(0, T, max(1, T // 40)))), device="cuda")
+        few = {k: v[at].contiguous() if k in ("x", "dy", "ids") else v for k, v in s.items()}
+        v, m = ac.plain(few)
+        e = ac.bounds(few, v, m, False)
+        for key in ("h", "y", "dx"):
+            ac.check(got[key][at], v[key], e[key], (T, apart, key))
+        cols = torch.tensor([0, 1, N // 2, N - 1], device="cuda")
+        part = {"x": s["x"], "ids": s["ids"], "scale": s["scale"], "a": s["a"], "w": s["w"][:, cols], "b": s["b"][:, :, cols], "dy": s["dy"][:, cols]}
+        v, m = ac.plain(part)
+        e = ac.bounds(part, v, m, False)
+        ac.check(got["db"][:, :, cols], v["db"], e["db"], (T, apart, "db"))
+        del got, s, wide, dy
