@@ -66,7 +66,7 @@ static bool goes_few(const moe_adapter_shape_t& s, const void* plan) { return ad
 // One workgroup: a counting sort.  Every wave counts a contiguous part of the tokens and later gives its tokens their rows, 64 at a
 // time: lanes with the same adapter find each other with a ballot for each bit of the id.
 constexpr int kSortWaves = 16;
-__global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, int brows, const int32_t* __restrict__ ids, PlanView v) {
+__global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, int n, int brows_log2, const int32_t* __restrict__ ids, PlanView v) {
     __shared__ int32_t hist[kSortWaves][kMaxAdapters + 1];
     __shared__ int32_t first[kMaxAdapters + 2];     // rows before bin b (bin 0: no adapter, bin a + 1: adapter a)
     __shared__ int32_t fblock[kMaxAdapters + 2], fseg[kMaxAdapters + 2];
@@ -75,17 +75,23 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
     const uint64_t below = (1ull << lane) - 1ull;
     for (int b = lane; b < bins; b += 64) hist[w][b] = 0;
     const int part = ((T + kSortWaves - 1) / kSortWaves + 63) & ~63, lo = min(T, w * part), hi = min(T, lo + part);
-    // f(token, bin) for this wave's tokens, 64 at a time; the ids of 256 are fetched together (a copy of f for each of 16 fetches, with the ids kept for the second
-    // time, was slower: 12 KB of code that runs once)
+    // f(token, bin) for this wave's tokens, 64 at a time; the ids of 256 are fetched together while those before them are worked on, and the first are kept
+    // (a copy of f for each of 16 fetches, with all ids kept for the second time, was slower: 12 KB of code that runs once)
+    auto fetch = [&](int (&a)[4], int t0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = t0 + 64 * i + lane;
+            a[i] = t < hi ? ids[t] : -1;
+        }
+    };
+    int start[4];
+    fetch(start, lo);
     auto each = [&](auto f) {
+        int next[4] = {start[0], start[1], start[2], start[3]};
 #pragma unroll 1
         for (int t0 = lo; t0 < hi; t0 += 256) {
-            int a[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int t = t0 + 64 * i + lane;
-                a[i] = t < hi ? ids[t] : -1;
-            }
+            const int a[4] = {next[0], next[1], next[2], next[3]};
+            if (t0 + 256 < hi) fetch(next, t0 + 256);
 #pragma unroll
             for (int i = 0; i < 4; ++i)
                 if (t0 + 64 * i < hi) f(t0 + 64 * i + lane, (unsigned)a[i] < (unsigned)n ? a[i] + 1 : 0);
@@ -105,44 +111,45 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
     int base_rows = 0, base_blocks = 0, base_segs = 0;
     for (int b0 = 0; b0 < bins; b0 += 64 * kSortWaves) {
         const int b = b0 + tid;
-        int c = 0;
-        if (b < bins)
-            for (int k = 0; k < kSortWaves; ++k) c += hist[k][b];
-        auto scan = [&](int x, int which, int base, int& total) {
-            int p = x;
+        int h[kSortWaves], c = 0;
 #pragma unroll
-            for (int o = 1; o < 64; o <<= 1) {
-                const int u = __shfl_up(p, o);
-                if (lane >= o) p += u;
-            }
+        for (int k = 0; k < kSortWaves; ++k) {
+            h[k] = b < bins ? hist[k][b] : 0;
+            c += h[k];
+        }
+        // x's sum over the threads before this one; the waves' totals are exchanged between the two
+        auto within = [&](int x, int which) {
+            const int p = wave_scan(x);
             if (lane == 63) carry[which][w] = p;
-            __syncthreads();
-            int before = base;
-            total = 0;
+            return p - x;
+        };
+        auto before = [&](int p, int which, int& base) {
+            p += base;
 #pragma unroll
             for (int k = 0; k < kSortWaves; ++k) {
-                if (k < w) before += carry[which][k];
-                total += carry[which][k];
+                const int u = carry[which][k];
+                if (k < w) p += u;
+                base += u;
             }
-            return before + p - x;
+            return p;
         };
-        int total;
-        const int r0 = scan(c, 0, base_rows, total);
-        base_rows += total;
-        const int nb = c > 0 ? (r0 + c - 1) / brows - r0 / brows + 1 : 0;
-        const int k0 = scan(nb, 1, base_blocks, total);
-        base_blocks += total;
-        const int both = scan(b > 0 && c > 0 ? 1 | (c > kGradRows) << 16 : 0, 2, base_segs, total), s0 = both & 0xffff;   // (up to 1024 of each)
-        base_segs += total;
+        int r0 = within(c, 0), both = within(b > 0 && c > 0 ? 1 | (c > kGradRows) << 16 : 0, 2);   // (up to 1024 of each)
+        __syncthreads();
+        r0 = before(r0, 0, base_rows);
+        both = before(both, 2, base_segs);
+        const int s0 = both & 0xffff;
+        int k0 = within(c > 0 ? ((r0 + c - 1) >> brows_log2) - (r0 >> brows_log2) + 1 : 0, 1);
+        __syncthreads();
+        k0 = before(k0, 1, base_blocks);
         if (b < bins) {
             first[b] = r0;
             fblock[b] = k0;
             fseg[b] = s0;
             int at = r0;
+#pragma unroll
             for (int k = 0; k < kSortWaves; ++k) {
-                const int h = hist[k][b];
                 hist[k][b] = at;
-                at += h;
+                at += h[k];
             }
             if (b > 0) {
                 v.start[b - 1] = r0;
@@ -183,9 +190,9 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
     for (int b = w; b < bins; b += kSortWaves) {
         const int r0 = first[b], r1 = first[b + 1], o = b > 0 ? fseg[b] : -1;
         if (r1 <= r0) continue;
-        const int q0 = r0 / brows, q1 = (r1 - 1) / brows;
+        const int q0 = r0 >> brows_log2, q1 = (r1 - 1) >> brows_log2;
         for (int q = q0 + lane; q <= q1; q += 64) {
-            const int a = max(r0, q * brows), e = min(r1, (q + 1) * brows);
+            const int a = max(r0, q << brows_log2), e = min(r1, (q + 1) << brows_log2);
             v.block[2 * (fblock[b] + q - q0)] = a;
             v.block[2 * (fblock[b] + q - q0) + 1] = (e - a) | b << 8;
         }
@@ -198,7 +205,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
 
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st) {
     if (adapter_few(s)) return MOE_OK;
-    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T), ids, plan_view(s, plan));
+    hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T) == 64 ? 6 : 5, ids, plan_view(s, plan));
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 

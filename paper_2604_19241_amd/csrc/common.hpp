@@ -1,5 +1,6 @@
 // Shared device/host definitions of the gfx950 fused-MoE library.
 #pragma once
+#include <type_traits>
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -102,6 +103,48 @@ __device__ __forceinline__ void across(float& v, F f) {
         const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
         v = f(__uint_as_float(r[0]), __uint_as_float(r[1]));
     }
+}
+
+// Sum over the wave, in each of its lanes, of a type of 4 or 8 bytes (with the exchanges of across).
+template <class T>
+__device__ __forceinline__ T wave_sum(T v) {
+    constexpr int kWords = sizeof(T) / 4;
+    struct Words {
+        uint32_t w[kWords];
+    };
+    auto dpp = [&](auto ctrl) {
+        Words u = __builtin_bit_cast(Words, v);
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) u.w[i] = __builtin_amdgcn_update_dpp(0, u.w[i], decltype(ctrl)::value, 0xf, 0xf, true);
+        v += __builtin_bit_cast(T, u);
+    };
+    dpp(std::integral_constant<int, 0xb1>{});
+    dpp(std::integral_constant<int, 0x4e>{});
+    dpp(std::integral_constant<int, 0x141>{});
+    dpp(std::integral_constant<int, 0x140>{});
+    auto swap = [&](auto exchange) {
+        const Words u = __builtin_bit_cast(Words, v);
+        Words a, b;
+#pragma unroll
+        for (int i = 0; i < kWords; ++i) {
+            const auto r = exchange(u.w[i]);
+            a.w[i] = r[0], b.w[i] = r[1];
+        }
+        v = __builtin_bit_cast(T, a) + __builtin_bit_cast(T, b);
+    };
+    swap([](uint32_t x) { return __builtin_amdgcn_permlane16_swap(x, x, false, false); });
+    swap([](uint32_t x) { return __builtin_amdgcn_permlane32_swap(x, x, false, false); });
+    return v;
+}
+// Sum over this lane and those before it.
+__device__ __forceinline__ int wave_scan(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);    // row_shr:1 (rows of 16 lanes)
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);   // row_bcast:15, to rows 1 and 3
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);   // row_bcast:31, to rows 2 and 3
+    return v;
 }
 
 __device__ __forceinline__ int rfl(int v) { return __builtin_amdgcn_readfirstlane(v); }
