@@ -549,17 +549,17 @@ __device__ __forceinline__ void join_task(const ProjParams& p, int t, int cb, Jo
         }
 }
 
-// Gradients of 8 ranks of one adapter, token by token.  SHARE: 256 columns, the waves share the tokens and their sums are added in LDS; else
-// 1024 columns, 256 a wave, which keeps the LDS small and the workgroups few where the adapters have few tokens or none (11 tokens, 27 adapters of 64 ranks, 6552 x 464: the
-// training step 66 us with SHARE, 51 without).  (With 512 columns a wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4
-// workgroups that took 128 tokens one after the other: 48 us, now 11.)
+// Gradients of 8 ranks of one adapter, token by token.  With COLS = 64 or 256 columns a workgroup groups of 16 or 64 lanes share the tokens, and their sums are added in LDS; with 1024
+// every lane has its own columns, which keeps the LDS small and the workgroups few where the adapters have few tokens or none (11 tokens, 27 adapters of 64 ranks, 6552 x 464:
+// the training step 66 us with 256, 51 with 1024).  (With 512 columns a wave and each wave its own columns or ranks, 256 tokens on 2 adapters of 512 x 1024 were 4
+// workgroups that took 128 tokens one after the other: 48 us; with 256 columns 12 workgroups, 11; with 64, where a group's tokens are all fetched at once, 8.)
 constexpr int kGradRanks = 8;
-template <bool SHARE>
-constexpr int kGradCols = SHARE ? 256 : 1024;
-template <int TOKENS, bool SHARE>
+// LPR lanes have a token's row.
+template <int TOKENS, int COLS>
 struct FewGradShared {
+    static constexpr int LPR = COLS < 1024 ? COLS / 4 : 256, kGroups = 256 / LPR;
     float h[TOKENS][kGradRanks];
-    float sums[SHARE ? 4 : 1][kGradRanks][SHARE ? 256 : 1];
+    __attribute__((aligned(16))) float sums[kGroups > 1 ? kGroups : 1][kGroups > 1 ? kGradRanks : 1][kGroups > 1 ? COLS : 4];
     uint64_t mask[kFewWords];
     int32_t list[TOKENS];
 };
@@ -577,15 +577,14 @@ struct FewGradTask {
     }
 };
 // S.list[0 .. count): the adapter's tokens; h4(token, j) = 4 ranks of it from j on.
-template <int TOKENS, bool SHARE, class H4>
-__device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGradTask& t, int count, FewGradShared<TOKENS, SHARE>& S, H4 h4) {
-    constexpr int kStep = SHARE ? 4 : 1, kPre = SHARE ? 8 : 4;
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, W = g.W[t.which], c = t.cb * kGradCols<SHARE> + (SHARE ? 4 * lane : 4 * tid);
-    float* const out = g.out[t.which] + ((size_t)t.a * g.r + t.j0) * W + c;
+template <int TOKENS, int COLS, class H4>
+__device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGradTask& t, int count, FewGradShared<TOKENS, COLS>& S, H4 h4) {
+    constexpr int LPR = FewGradShared<TOKENS, COLS>::LPR, kStep = FewGradShared<TOKENS, COLS>::kGroups, kPre = kStep > 1 ? 8 : 4;
+    const int tid = threadIdx.x, k0 = tid / LPR, W = g.W[t.which], c = t.cb * COLS + 4 * (tid % LPR);
+    float* const out = g.out[t.which] + ((size_t)t.a * g.r + t.j0) * W;
     float acc[kGradRanks][4] = {};
     if (count > 0) {
         // the first rows of x are on their way while h is fetched
-        const int k0 = SHARE ? w : 0;
         const size_t ldx = g.ldx[t.which];
         const char* const x = g.x[t.which] + (size_t)min(c, W - 4) * 2;
         u32x2_t pre[kPre];
@@ -607,32 +606,31 @@ __device__ __forceinline__ void few_grad_task(const GradParams& g, const FewGrad
             }
         }
     }
-    if (!SHARE || count == 0) {
+    if (kStep == 1) {
         if (c < W)
 #pragma unroll
-            for (int j = 0; j < kGradRanks; ++j)
-                if (!SHARE || (j & 3) == w) *(f32x4_t*)(out + (size_t)j * W) = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+            for (int j = 0; j < kGradRanks; ++j) *(f32x4_t*)(out + (size_t)j * W + c) = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
         return;
     }
 #pragma unroll
-    for (int j = 0; j < kGradRanks; ++j) *(f32x4_t*)&S.sums[w][j][4 * lane] = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
+    for (int j = 0; j < kGradRanks; ++j) *(f32x4_t*)&S.sums[k0][j][4 * (tid % LPR)] = f32x4_t{acc[j][0], acc[j][1], acc[j][2], acc[j][3]};
     __syncthreads();
     if (c >= W) return;
+    // the groups' sums: k0 adds up ranks k0, k0 + kStep ..
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {   // wave w adds up ranks w and w + 4
-        const int j = w + 4 * i;
-        f32x4_t v = *(const f32x4_t*)&S.sums[0][j][4 * lane];
+    for (int j = k0; j < kGradRanks; j += kStep) {
+        f32x4_t v = *(const f32x4_t*)&S.sums[0][j][4 * (tid % LPR)];
 #pragma unroll
-        for (int k = 1; k < 4; ++k) {
-            const f32x4_t o = *(const f32x4_t*)&S.sums[k][j][4 * lane];
+        for (int k = 1; k < kStep; ++k) {
+            const f32x4_t o = *(const f32x4_t*)&S.sums[k][j][4 * (tid % LPR)];
 #pragma unroll
             for (int q = 0; q < 4; ++q) v[q] += o[q];
         }
-        *(f32x4_t*)(out + (size_t)j * W) = v;
+        *(f32x4_t*)(out + (size_t)j * W + c) = v;
     }
 }
-template <int TOKENS, bool SHARE>
-__device__ __forceinline__ void few_tokens_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared<TOKENS, SHARE>& S) {
+template <int TOKENS, int COLS>
+__device__ __forceinline__ void few_tokens_grad_task(const ProjParams& p, const GradParams& g, int id, FewGradShared<TOKENS, COLS>& S) {
     const FewGradTask t(g, id);
     Members mb;
     mb.find(g.T, g.n, p.ids, t.a, S.mask);
@@ -659,12 +657,12 @@ __global__ void __launch_bounds__(256) adapter_few_second_kernel(ProjParams p) {
     __shared__ JoinShared<G> S;
     join_task<G>(p, blockIdx.x % p.T, blockIdx.x / p.T, S);
 }
-// FEW: up to kGradRows tokens
-template <int G, bool FEW>
+// COLS = 1024: up to kGradRows tokens
+template <int G, int COLS>
 __global__ void __launch_bounds__(256) adapter_few_second_grad_kernel(ProjParams p, GradParams g, int joins) {
     union Shared {
         JoinShared<G> join;
-        FewGradShared<FEW ? kGradRows : kFewTokens, !FEW> grad;
+        FewGradShared<COLS == 1024 ? kGradRows : kFewTokens, COLS> grad;
     };
     __shared__ Shared S;
     const int id = blockIdx.x;
@@ -1281,7 +1279,7 @@ __global__ void __launch_bounds__(256) adapter_grad_sum_kernel(GradParams g) {
 // The same for adapters with up to kGradRows rows, on the vector unit: a workgroup of the tiles above takes 6 us whatever its rows and has a CU for itself (a training step of 512 tokens on
 // 200 adapters of 680 x 480, 16 ranks, 112 us, of 600 with this and the low-rank parts row by row 85).
 __global__ void __launch_bounds__(256) adapter_grad_rows_kernel(ProjParams p, GradParams g) {
-    __shared__ FewGradShared<kGradRows, false> S;
+    __shared__ FewGradShared<kGradRows, 1024> S;
     const FewGradTask t(g, blockIdx.x);
     const int row0 = p.plan.start[t.a], count = p.plan.start[t.a + 1] - row0;
     if (count > kGradRows) return;
@@ -1459,6 +1457,15 @@ int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t l
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 
+// Columns of a workgroup of the factors' gradients of few tokens: 64 where that leaves the CUs a workgroup each.  Backward call with 256 / with 64, us (workgroups of
+// 256 columns; tokens, K, N, ranks, adapters): 4 (128, 512 x 512, 8, 1) 12.4 / 10.2, 12 (256, 512 x 1024, 8, 2) 16.7 / 14.0, 56 (512, 2048 x 1408, 16, 2) 31.4 / 22.7, 64 (200,
+// 1024 x 1024, 64, 1) 18.7 / 15.9, 96 (80, 1024 x 2048, 8, 8) 11.2 / 11.3, 448 (256, 2048 x 1408, 16, 16) 18.1 / 19.6, 1920 (200, 4096 x 4096, 16, 30) 36.0 / 58.4.
+static int few_grad_cols(const moe_adapter_shape_t& s) {
+    if (s.T <= kGradRows) return 1024;
+    const size_t wide = (size_t)s.adapters * (s.rank / kGradRanks) * ((s.K + 255) / 256 + (s.N + 255) / 256);
+    return 4 * wide <= 256 ? 64 : 256;
+}
+
 int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t lddy, const void* x, size_t ldx, const void* w, const void* a, const void* b,
                             const float* scale, const int32_t* ids, void* plan, const float* h, void* dx, float* da, float* db, char* ws, hipStream_t st) {
     ProjParams p = {};
@@ -1480,17 +1487,16 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         }
         const int joins = s.T > 0 ? few_joins(p) : 0;
         g.rank_tiles = g.r / kGradRanks;
-        const bool few = s.T <= kGradRows;
-        const int cols = few ? kGradCols<false> : kGradCols<true>;
+        const int cols = few_grad_cols(s);
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
         const dim3 grid((unsigned)(joins + g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1])));
-        auto launch = [&](auto group, auto small) {
-            hipLaunchKernelGGL((adapter_few_second_grad_kernel<group.value, small.value>), grid, dim3(256), 0, st, p, g, joins);
+        auto launch = [&](auto width) {
+            if (join_groups(p)) hipLaunchKernelGGL((adapter_few_second_grad_kernel<4, width.value>), grid, dim3(256), 0, st, p, g, joins);
+            else hipLaunchKernelGGL((adapter_few_second_grad_kernel<1, width.value>), grid, dim3(256), 0, st, p, g, joins);
         };
-        std::integral_constant<int, 4> groups;
-        std::integral_constant<int, 1> single;
-        if (few) join_groups(p) ? launch(groups, std::true_type{}) : launch(single, std::true_type{});
-        else join_groups(p) ? launch(groups, std::false_type{}) : launch(single, std::false_type{});
+        if (cols == 1024) launch(std::integral_constant<int, 1024>{});
+        else if (cols == 256) launch(std::integral_constant<int, 256>{});
+        else launch(std::integral_constant<int, 64>{});
     } else {
         p.h_given = h;
         many_launch<kKc>(p, s, plan, ws, st);
@@ -1500,7 +1506,7 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         g.h[1] = p.h;
         if (rows) {
             g.rank_tiles = g.r / kGradRanks;
-            for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + kGradCols<false> - 1) / kGradCols<false>;
+            for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + 1023) / 1024;
             hipLaunchKernelGGL(adapter_grad_rows_kernel, dim3((unsigned)(g.n * g.rank_tiles * (g.col_tiles[0] + g.col_tiles[1]))), dim3(256), 0, st, p, g);
         }
         const int cols = grad_cols(p.r);
