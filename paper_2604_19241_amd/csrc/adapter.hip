@@ -26,7 +26,7 @@ constexpr int kGradRows = 64;         // rows up to which an adapter's gradients
 constexpr int kUnit = 64;             // rows of which the plan knows the first and the last segment
 
 // ------------------------------------------------------------------ the plan
-// int32 words: [0] blocks, [1] adapters with many rows, then the arrays.
+// int32 words: [0] blocks, [1] adapters with many rows, [2] adapters with rows, then the arrays.
 struct PlanView {
     int32_t* head;
     int32_t* order;      // [T] row -> token: those without an adapter, then by adapter, each in the order of the tokens
@@ -166,6 +166,7 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
         v.start[n] = T;
         v.head[0] = base_blocks;
         v.head[1] = base_segs >> 16;
+        v.head[2] = base_segs & 0xffff;
     }
     __syncthreads();
     // rows
@@ -245,7 +246,7 @@ struct GradParams {
     size_t ldx[2];
     const float* h[2];      // [T][r]; NULL: hpart (few tokens)
     float* out[2];          // [n][r][W]
-    int parts;              // more tokens: into how many parts an adapter's rows are cut, and the parts' sums, [parts][n][r][W] each
+    int parts;              // more tokens: into how many parts an adapter's rows are cut at most (GradCut), and the parts' sums, [grad_pieces][r][W] each
     float* part[2];
     int col_tiles[2], rank_tiles;
 };
@@ -1116,6 +1117,16 @@ __device__ __forceinline__ void read_tr(u32x4_t (&f)[N], const uint32_t (&at)[N]
     for (int i = 0; i < N; ++i) f[i] = u32x4_t{lo[i][0], lo[i][1], hi[i][0], hi[i][1]};
 }
 
+// How the adapters' rows are cut, where g.parts allows it: those with rows (g.few: with more than kGradRows) are known only here, and a batch may be on few of many.  As many parts as give
+// every CU a tile, of 512 rows at least; active * eff * tiles <= 256 where eff > 1.
+struct GradCut {
+    int active, eff;
+    __device__ __forceinline__ GradCut(const GradParams& g, const int32_t* head)
+        : active(g.few ? head[1] : head[2]), eff(g.parts > 1 ? max(1, min(g.parts, 256 / ((g.col_tiles[0] + g.col_tiles[1]) * max(active, 1)))) : 1) {}
+    __device__ __forceinline__ int rows(int count) const { return max(512, ((count + eff - 1) / eff + BK - 1) / BK * BK); }
+    __device__ __forceinline__ int pieces(int count) const { return eff > 1 ? (count + rows(count) - 1) / rows(count) : 1; }
+};
+
 // Waves 0..3 multiply, waves 4..7 only move operands: with one wave a SIMD for both, its requests (ten a stage, each with an address of its own)
 // and its products were done one after the other.
 constexpr int kGradThreads = 2 * kSmallThreads;
@@ -1128,23 +1139,23 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
     const int tid = threadIdx.x;
     // every XCD a run of the column tiles, adapter by adapter: its workgroups share one adapter's h in their L2, however unlike the adapters are
     const int tiles = g.col_tiles[0] + g.col_tiles[1], per = (tiles + 7) >> 3, slot = blockIdx.x >> 3;
-    int a = slot / per;
-    if (g.few) {
-        if (a >= p.plan.head[1]) return;
-        a = p.plan.many[a];
-    }
+    const GradCut cut(g, p.plan.head);
+    const int at = slot / per / cut.eff, piece = slot / per - at * cut.eff;
+    if ((g.few || g.parts > 1) && at >= cut.active) return;   // (without rows: left to adapter_grad_rows_kernel or adapter_grad_sum_kernel)
+    const int a = g.few ? p.plan.many[at] : g.parts > 1 ? p.plan.seg[at] : at;
     int ct = (blockIdx.x & 7) * per + slot % per;
     if (ct >= tiles) return;
     const int which = ct < g.col_tiles[0] ? 0 : 1;
     if (which) ct -= g.col_tiles[0];
     const int W = g.W[which], c0 = ct * 32 * NCF, r = g.r;
     int row0 = p.plan.start[a], count = p.plan.start[a + 1] - row0;
-    float* out = g.out[which];
-    if (g.parts > 1) {
-        const int rows = ((count + g.parts - 1) / g.parts + BK - 1) / BK * BK, first = min(count, (int)blockIdx.y * rows);
-        row0 += first;
-        count = min(rows, count - first);
-        out = g.part[which] + (size_t)blockIdx.y * g.n * r * W;
+    float* out = g.out[which] + (size_t)a * r * W;
+    if (cut.eff > 1) {
+        const int rows = cut.rows(count);
+        if (piece * rows >= count) return;
+        if (rows < count) out = g.part[which] + (size_t)(at * cut.eff + piece) * r * W;
+        row0 += piece * rows;
+        count = min(rows, count - piece * rows);
     }
     const Lane ln;
     const int wave = ln.wave_uniform() & 3;
@@ -1251,29 +1262,37 @@ __global__ void __launch_bounds__(kGradThreads) adapter_grad_kernel(ProjParams p
             row += 32 * tf;
             col += c0;
             if (row >= r || col >= W) return;
-            f32x4_t* to = (f32x4_t*)(out + ((size_t)a * r + row) * W + col);
+            f32x4_t* to = (f32x4_t*)(out + (size_t)row * W + col);
             to[0] = f32x4_t{v[0], v[1], v[2], v[3]};
             to[1] = f32x4_t{v[4], v[5], v[6], v[7]};
         });
     }
 }
-// The parts' sums, first part first.
-__global__ void __launch_bounds__(256) adapter_grad_sum_kernel(GradParams g) {
-    const size_t n0 = (size_t)g.n * g.r * g.W[0] / 4, n1 = (size_t)g.n * g.r * g.W[1] / 4;
-    size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+// The parts' sums, first part first, and zeros for adapters without rows (g.few: adapter_grad_rows_kernel's).
+__global__ void __launch_bounds__(256) adapter_grad_sum_kernel(PlanView plan, GradParams g) {
+    const GradCut cut(g, plan.head);
+    if (g.few && (int)blockIdx.y >= cut.active) return;
+    const int a = g.few ? plan.many[blockIdx.y] : blockIdx.y, at = g.few ? blockIdx.y : plan.ordinal[a];
+    const int count = plan.start[a + 1] - plan.start[a], pieces = cut.pieces(count);
+    if (pieces == 1 && count > 0) return;
+    const int n0 = g.r * g.W[0] / 4, n1 = g.r * g.W[1] / 4;
+    int i = blockIdx.x * 256 + threadIdx.x;
     const int which = i < n0 ? 0 : 1;
     if (which) i -= n0;
-    const size_t n = which ? n1 : n0;
+    const int n = which ? n1 : n0;
     if (i >= n) return;
-    const f32x4_t* const q = (const f32x4_t*)g.part[which];
-    f32x4_t v = q[i];
+    f32x4_t v = {0.f, 0.f, 0.f, 0.f};
+    if (count > 0) {
+        const f32x4_t* const q = (const f32x4_t*)g.part[which] + (size_t)at * cut.eff * n + i;
+        v = q[0];
 #pragma unroll 8
-    for (int k = 1; k < g.parts; ++k) {
-        const f32x4_t u = q[(size_t)k * n + i];
+        for (int k = 1; k < pieces; ++k) {
+            const f32x4_t u = q[(size_t)k * n];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] += u[e];
+            for (int e = 0; e < 4; ++e) v[e] += u[e];
+        }
     }
-    ((f32x4_t*)g.out[which])[i] = v;
+    ((f32x4_t*)g.out[which])[(size_t)a * n + i] = v;
 }
 
 // The same for adapters with up to kGradRows rows, on the vector unit: a workgroup of the tiles above takes 6 us whatever its rows and has a CU for itself (a training step of 512 tokens on
@@ -1346,13 +1365,15 @@ static TileShape tile_shape(int T, int C) {
 }
 static size_t hx_most(const moe_adapter_shape_t& s) { return std::max(hx_bytes(s, tile_shape(s.T, s.N).rows), hx_bytes(s, tile_shape(s.T, s.K).rows)); }
 // The factors' gradients: columns of a tile; whether adapters with few rows have a kernel of their own (where they have few on average); and into how many parts
-// an adapter's rows are cut where the tiles would leave more than half of the CUs idle (3594 tokens on one adapter, 2528 x 264: 30.5 us in one part, 13.5 in
-// 7 with the sum of the parts).
+// an adapter's rows are cut at most, if it had all of them (3594 tokens on one adapter, 2528 x 264: 30.5 us in one part, 13.5 in 7 with the sum of the parts; 12337 on 2 of 193, 72 x
+// 24: 94 in one part, 16).  With less than 8 adapters that fill half of the CUs it would be an empty launch for most batches.
 static int grad_cols(int r) { return r > 64 ? 64 : 128; }
+static int grad_tiles(const moe_adapter_shape_t& s) { return (s.K + grad_cols(s.rank) - 1) / grad_cols(s.rank) + (s.N + grad_cols(s.rank) - 1) / grad_cols(s.rank); }
 static bool grad_rows(const moe_adapter_shape_t& s) { return (long long)s.adapters * kGradRows >= s.T; }
+static int grad_pieces(const moe_adapter_shape_t& s) { return 256 / grad_tiles(s); }   // of all adapters together
 static int grad_parts(const moe_adapter_shape_t& s) {
-    const int cols = grad_cols(s.rank), tiles = s.adapters * ((s.K + cols - 1) / cols + (s.N + cols - 1) / cols);
-    return grad_rows(s) ? 1 : std::max(1, std::min(256 / tiles, s.T / (s.adapters * 512)));
+    if (s.adapters < 8 && s.adapters * grad_tiles(s) > 128) return 1;
+    return std::max(1, std::min(grad_pieces(s), s.T / 512));
 }
 // Whether a product of sorted tokens is cut along its reduction into fp32 parts, with h beside it, as that of few tokens: long reductions of small results, which
 // tiles in one piece leave to a few CUs, behind an equally long h.  Measured, us of the forward call in one piece / in parts (tokens, K,
@@ -1365,7 +1386,7 @@ static size_t parts_bytes(const moe_adapter_shape_t& s, int R, int C) {
 static size_t grad_part_at(const moe_adapter_shape_t& s);
 static size_t parts_at(const moe_adapter_shape_t& s) {
     const int parts = grad_parts(s);
-    return grad_part_at(s) + (parts > 1 ? align_up((size_t)parts * s.adapters * s.rank * ((size_t)s.K + s.N) * 4, 256) : 0);
+    return grad_part_at(s) + (parts > 1 ? align_up((size_t)grad_pieces(s) * s.rank * ((size_t)s.K + s.N) * 4, 256) : 0);
 }
 static size_t many_bytes(const moe_adapter_shape_t& s) { return parts_at(s) + std::max(parts_bytes(s, s.K, s.N), parts_bytes(s, s.N, s.K)); }
 static size_t grad_part_at(const moe_adapter_shape_t& s) {
@@ -1513,12 +1534,14 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         for (int i = 0; i < 2; ++i) g.col_tiles[i] = (g.W[i] + cols - 1) / cols;
         g.parts = grad_parts(s);
         g.part[0] = (float*)(ws + grad_part_at(s));
-        g.part[1] = g.part[0] + (size_t)g.parts * g.n * g.r * g.W[0];
-        const dim3 grid((unsigned)(8 * (rows ? std::min(g.n, g.T / (kGradRows + 1)) : g.n) * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)), (unsigned)g.parts);
+        g.part[1] = g.part[0] + (size_t)grad_pieces(s) * g.r * g.W[0];
+        const int most = rows ? std::min(g.n, g.T / (kGradRows + 1)) : g.n;   // adapters that may have to be done
+        const dim3 grid((unsigned)(8 * (g.parts > 1 ? std::max(most, grad_pieces(s)) : most) * ((g.col_tiles[0] + g.col_tiles[1] + 7) / 8)));
         if (p.r <= 32) hipLaunchKernelGGL((adapter_grad_kernel<1, 4>), grid, dim3(kGradThreads), 0, st, p, g);
         else if (p.r <= 64) hipLaunchKernelGGL((adapter_grad_kernel<2, 4>), grid, dim3(kGradThreads), 0, st, p, g);
         else hipLaunchKernelGGL((adapter_grad_kernel<4, 2>), grid, dim3(kGradThreads), 0, st, p, g);
-        if (g.parts > 1) hipLaunchKernelGGL(adapter_grad_sum_kernel, dim3((unsigned)(((size_t)g.n * g.r * (g.W[0] + g.W[1]) / 4 + 255) / 256)), dim3(256), 0, st, g);
+        if (g.parts > 1)   // (more adapters than grad_pieces are not cut)
+            hipLaunchKernelGGL(adapter_grad_sum_kernel, dim3((unsigned)((g.r * (g.W[0] + g.W[1]) / 4 + 255) / 256), (unsigned)(rows ? std::min(most, grad_pieces(s)) : g.n)), dim3(256), 0, st, p.plan, g);
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }

@@ -45,6 +45,10 @@ CASES = [  # T, K, N, rank, adapters, ids, pad, out
     (600, 1544, 1600, 16, 7, "scattered", 0, "bf16"), (2600, 3000, 24, 8, 12, "packed", 8, "bf16"), (1100, 24, 2056, 128, 3, "scattered", 0, "f32"),
     (900, 1552, 1608, 24, 300, "each", 0, "f32"), (3000, 1600, 520, 40, 2, "one", 0, "bf16"),
     (40, 7000, 4104, 16, 3, "scattered", 0, "bf16"), (400, 5000, 264, 24, 2, "packed", 8, "f32"),
+    # a batch on few of many adapters: rows in parts, by adapter or by those with many rows
+    (12337, 72, 24, 16, 193, "packed", 0, "bf16"), (2206, 616, 2320, 64, 189, "packed", 0, "bf16"), (5000, 136, 72, 8, 300, "one", 8, "f32"), (6000, 264, 136, 24, 20, "one", 0, "bf16"),
+    (8200, 72, 136, 16, 12, "packed", 0, "bf16"), (3000, 72, 200, 72, 40, "none", 0, "bf16"), (3000, 72, 200, 72, 9, "none", 0, "bf16"), (9000, 24, 8, 128, 130, "outside", 0, "bf16"),
+    (4000, 136, 264, 16, 8, "scattered", 0, "bf16"), (1100, 2056, 3000, 8, 16, "packed", 0, "bf16"),
 ]
 
 
