@@ -228,6 +228,7 @@ struct ProjParams {
     float* hpart;           // [hsplits][T][r]
     int splits, per_split, hsplits, hper_split;
     int col_tiles, row_tiles, rank_tiles, hgroups;
+    int dot_cut;            // workgroups that share 64 ranks of dots
     // more
     PlanView plan;
     char* hx;               // the low-rank rows of every tile (hx_base)
@@ -350,7 +351,7 @@ __device__ __forceinline__ void few_dots(const ProjParams& p, int a, int j0, int
     }
 }
 
-// Parts of x W and of h.  Tasks: (column tile, split, row tile), then of h (token, rank tile, split), where a workgroup whose token is not every
+// Parts of x W and of h.  Tasks: (column tile, split, row tile), then of h (token, part of a rank tile's dots, rank tile, split), where a workgroup whose token is not every
 // 32nd of its adapter's has nothing to do, or (adapter, 32 of its tokens, rank tile, split) where that is fewer.
 template <int NRF, int FORM>
 __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjParams p) {
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
         return;
     }
     id -= gemm;
-    const int t = id % p.hgroups, rest = id / p.hgroups, rt = rest % p.rank_tiles, sp = rest / p.rank_tiles;
+    const int t = id % p.hgroups, rest = id / p.hgroups, quarter = rest % p.dot_cut, rt = rest / p.dot_cut % p.rank_tiles, sp = rest / p.dot_cut / p.rank_tiles;
     int a, rows, rank = 0;
     if (p.blocks > 0) {   // sorted: a block of the plan
         if (t >= p.plan.head[0]) return;
@@ -418,10 +419,12 @@ __global__ void __launch_bounds__(kSmallThreads) adapter_few_first_kernel(ProjPa
     const int s0 = sp * p.hper_split, s1 = min(nst, s0 + p.hper_split);
     if (rank == 0 && rows <= kDotTokens) {
         float* const out = p.hpart + (size_t)sp * p.T * p.r;
-        few_dots(p, a, 64 * rt, min(p.r, 64 * rt + 64), rows, s0 * BK, min(p.R, s1 * BK), [&](int m) { return s_list[m]; },
+        const int ranks = 64 / p.dot_cut, j0 = 64 * rt + quarter * ranks;
+        few_dots(p, a, j0, min(p.r, j0 + ranks), rows, s0 * BK, min(p.R, s1 * BK), [&](int m) { return s_list[m]; },
                  [&](int m, int j, float v) { out[(size_t)s_list[m] * p.r + j] = v; });
         return;
     }
+    if (quarter > 0) return;
     const Stages st = part_of(s0, s1);
     f32x16_t acc[1][2];
     {
@@ -1312,7 +1315,7 @@ __global__ void __launch_bounds__(256) adapter_grad_rows_kernel(ProjParams p, Gr
 constexpr int kMostSplits = 16;
 static int stages_in(int R) { return (R + BK - 1) / BK; }
 struct FewPlan {
-    int row_frags, col_tiles, row_tiles, rank_tiles, hgroups, splits, per_split, hsplits, hper_split;
+    int row_frags, col_tiles, row_tiles, rank_tiles, hgroups, dot_cut, splits, per_split, hsplits, hper_split;
 };
 // Parts of at least 4 stages, as many as give every CU a workgroup but no more than the second launch fetches in two goes; h is cut alike, or into fewer parts where every token may be a group of its own.
 static FewPlan few_plan(int T, int R, int C, int r, int n, int blocks = 0) {
@@ -1328,6 +1331,10 @@ static FewPlan few_plan(int T, int R, int C, int r, int n, int blocks = 0) {
     f.hgroups = blocks > 0 ? blocks : (int)std::min((long long)T, (long long)n * ((T + 31) / 32));
     f.hper_split = std::max(std::min(f.per_split, 16), (int)(((long long)nst * f.hgroups * f.rank_tiles + 511) / 512));
     f.hsplits = (nst + f.hper_split - 1) / f.hper_split;
+    // dots of many ranks: 16 a workgroup (one turn of its waves) while there are up to 512 workgroups.  First launch, us, 64 ranks a workgroup / cut while there are 256, 512, 1024 (tokens, K, N, ranks,
+    // adapters): 9, 912, 448, 128, 4 14.1 / 7.4 with 256; 100, 1024, 1024, 64, 200 18.0 / 18.0, 14.0, 14.9; 60, 2048, 2048, 64, 60 19.8 / 19.4, 16.6, 18.6.
+    f.dot_cut = 1;
+    while (T <= kDotTokens * n && 64 / f.dot_cut > 16 && r > 64 / f.dot_cut / 2 && (long long)f.hgroups * f.rank_tiles * f.hsplits * f.dot_cut <= 512) f.dot_cut *= 2;
     return f;
 }
 static size_t few_bytes(int T, int R, int C, int r, int n, int blocks = 0) {
@@ -1405,11 +1412,11 @@ static void few_params(ProjParams& p, char* ws, FewPlan& f) {
     p.part = (float*)ws;
     p.hpart = (float*)(ws + align_up((size_t)f.splits * p.T * p.C * 4, 256));
     p.splits = f.splits, p.per_split = f.per_split, p.hsplits = f.hsplits, p.hper_split = f.hper_split;
-    p.col_tiles = f.col_tiles, p.row_tiles = f.row_tiles, p.rank_tiles = f.rank_tiles, p.hgroups = f.hgroups;
+    p.col_tiles = f.col_tiles, p.row_tiles = f.row_tiles, p.rank_tiles = f.rank_tiles, p.hgroups = f.hgroups, p.dot_cut = f.dot_cut;
 }
 template <int FORM>
 static void few_first(const ProjParams& p, const FewPlan& f, hipStream_t st) {
-    const dim3 grid((unsigned)(f.col_tiles * f.splits * f.row_tiles + f.hgroups * f.rank_tiles * f.hsplits));
+    const dim3 grid((unsigned)(f.col_tiles * f.splits * f.row_tiles + f.hgroups * f.rank_tiles * f.hsplits * f.dot_cut));
     if (f.row_frags == 1) hipLaunchKernelGGL((adapter_few_first_kernel<1, FORM>), grid, dim3(kSmallThreads), 0, st, p);
     else hipLaunchKernelGGL((adapter_few_first_kernel<2, FORM>), grid, dim3(kSmallThreads), 0, st, p);
 }
