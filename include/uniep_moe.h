@@ -287,13 +287,16 @@ typedef struct {
     int32_t adapters;
 } moe_adapter_shape_t;
 
-/* Workspace of the forward and of the backward call, and bytes of the plan (host outputs; either may be NULL).  Where few tokens are best not
- * sorted the plan has 0 bytes: moe_adapter_plan then enqueues nothing.  Up to 512 tokens `plan` may be NULL whatever its size. */
+/* Workspace of the forward and of the backward call, and bytes of the plan that this shape's calls read (host outputs; either may be NULL): 0 up to 256 tokens, and
+ * up to 512 where they are best not sorted, which goes by the widths too.  Up to 512 tokens `plan` may be NULL in every call: one that sorts then does so by itself, with the
+ * same results. */
 int moe_adapter_workspace_bytes(const moe_adapter_shape_t* shape, size_t* ws_bytes, size_t* plan_bytes);
 
 /* Sorts the tokens by adapter (stable), for any number of forward and backward calls with the same ids, T and adapters, whatever their
- * widths and rank.  The ids have to stay as they are while the plan is in use.  ids: [T] int32.  The backward call
- * has to be given the plan that the forward call had (or NULL as that). */
+ * widths and rank, those of this shape included.  The ids have to stay as they are while the plan is in use.  ids: [T] int32.
+ * A plan that is not NULL is filled, with more than 256 tokens, also where this shape's calls would not read it (layers of other widths may): plan_bytes has to be
+ * what moe_adapter_workspace_bytes gives for a shape that reads one (for the widest of the layers), which goes by T and adapters alone, else
+ * MOE_ERR_WORKSPACE.  Nothing is enqueued for up to 256 tokens, and where plan is NULL and this shape reads none. */
 int moe_adapter_plan(const moe_adapter_shape_t* shape, const int32_t* ids, void* plan, size_t plan_bytes, void* stream);
 
 /* Forward.

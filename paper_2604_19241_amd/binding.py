@@ -408,12 +408,13 @@ def moe_adapter_workspace_bytes(shape: MoEAdapterShape) -> int:
 class AdapterPlan:
     """The tokens of one batch by adapter.  `ids` has to stay as it is while the plan is in use."""
     ids: torch.Tensor                 # [T] i32, outside [0, adapters): no adapter
-    table: Optional[torch.Tensor]     # None for few tokens: nothing is sorted
+    table: Optional[torch.Tensor]     # None where the shape that it was made with does not sort: up to 256 tokens, up to 512 with small products
     adapters: int = 0                 # that the table was made for
 
 
 def moe_adapter_plan(shape: MoEAdapterShape, ids: torch.Tensor) -> AdapterPlan:
-    """Sorts the tokens by adapter, once for all projections of the batch with as many adapters."""
+    """Sorts the tokens by adapter, once for all projections of the batch with as many adapters.  (With 257 to 512 tokens make it with the widest of
+    them: one that sorts, given a plan of one that does not, sorts by itself in each call.)"""
     call = _call or _load_call()
     out = call.adapter_plan(_addressof(shape), ids, _raw_stream(ids))
     if type(out) is int:

@@ -60,8 +60,10 @@ static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
 // 20.3 and 48.5 / 27.0 and 76.1; 512 2048 x 7168, 8, 256 45.3 and 130 / 62.3 and 306.
 static bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= kFewTokens / 2 || (s.T <= kFewTokens && (long long)s.T * s.K * s.N <= 8ll << 30); }
 bool adapter_needs_plan(const moe_adapter_shape_t& s) { return s.T > kFewTokens; }
-size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) ? 0 : plan_words(s) * 4; }
-static bool goes_few(const moe_adapter_shape_t& s, const void* plan) { return adapter_few(s) || !plan; }
+// What a plan holds goes by the tokens and the adapters alone, whatever the widths of the shape that it is made with: a plan serves layers of all widths, and up to 512 tokens some
+// of them may sort and others not.  (Up to 256 none does.)  Where a shape that sorts is given no plan it makes its own in the workspace, so that the shape alone says which way is taken.
+size_t adapter_table_bytes(const moe_adapter_shape_t& s) { return s.T <= kFewTokens / 2 ? 0 : plan_words(s) * 4; }
+size_t adapter_plan_bytes(const moe_adapter_shape_t& s) { return adapter_few(s) ? 0 : adapter_table_bytes(s); }
 
 // One workgroup: a counting sort.  Every wave counts a contiguous part of the tokens and later gives its tokens their rows, 64 at a
 // time: lanes with the same adapter find each other with a ballot for each bit of the id.
@@ -205,7 +207,6 @@ __global__ void __launch_bounds__(64 * kSortWaves) adapter_plan_kernel(int T, in
 }
 
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st) {
-    if (adapter_few(s)) return MOE_OK;
     hipLaunchKernelGGL(adapter_plan_kernel, dim3(1), dim3(64 * kSortWaves), 0, st, s.T, s.adapters, block_rows(s.T) == 64 ? 6 : 5, ids, plan_view(s, plan));
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -1402,9 +1403,8 @@ static size_t grad_part_at(const moe_adapter_shape_t& s) {
 }
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s) {
     if (s.T == 0) return 256;
-    size_t most = adapter_few(s) ? 0 : many_bytes(s);
-    if (!adapter_needs_plan(s)) most = std::max({most, few_bytes(s.T, s.K, s.N, s.rank, s.adapters), few_bytes(s.T, s.N, s.K, s.rank, s.adapters)});
-    return most;
+    if (adapter_few(s)) return std::max(few_bytes(s.T, s.K, s.N, s.rank, s.adapters), few_bytes(s.T, s.N, s.K, s.rank, s.adapters));
+    return many_bytes(s) + (adapter_needs_plan(s) ? 0 : align_up(adapter_table_bytes(s), 256));
 }
 
 static void few_params(ProjParams& p, char* ws, FewPlan& f) {
@@ -1426,7 +1426,12 @@ static int few_joins(const ProjParams& p) { return p.T * ((p.C + kJoinCols - 1) 
 static bool join_groups(const ProjParams& p) { return (long long)p.T * p.r * p.C > 1 << 27; }
 
 template <int FORM>
-static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
+static int many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan, char* ws, hipStream_t st) {
+    if (!plan) {   // (up to kFewTokens)
+        plan = ws + many_bytes(s);
+        const int rc = adapter_plan_launch(s, p.ids, plan, st);
+        if (rc != MOE_OK) return rc;
+    }
     p.plan = plan_view(s, plan);
     const TileShape tile = tile_shape(p.T, p.C);
     p.tile_rows = tile.rows;
@@ -1448,7 +1453,7 @@ static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan,
         p.join_rows = std::max(1, std::min(kPartsRows, 256 / wide));
         const unsigned groups = (unsigned)((p.T + p.join_rows - 1) / p.join_rows * ((wide + 255) / 256));
         hipLaunchKernelGGL(adapter_parts_join_kernel, dim3(groups), dim3(256), 0, st, p);
-        return;
+        return MOE_OK;
     }
     const dim3 low((unsigned)(p.blocks + (FORM == kKc ? p.n * ((p.C + 63) / 64) : 0)));
     auto low_launch = [&](auto nrf) {
@@ -1464,6 +1469,7 @@ static void many_launch(ProjParams& p, const moe_adapter_shape_t& s, void* plan,
     if (tile.cols == 64) hipLaunchKernelGGL((adapter_tile_kernel<FORM, false>), grid, dim3(kSmallThreads), 0, st, p);
     else if (tile.cols == 128) hipLaunchKernelGGL((adapter_tile_kernel<FORM, true>), grid, dim3(kMidThreads), 0, st, p);
     else hipLaunchKernelGGL((adapter_big_kernel<FORM>), grid, dim3(kMmaThreads), 0, st, p);
+    return MOE_OK;
 }
 
 int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t ldx, const void* w, const void* a, const void* b, const float* scale,
@@ -1473,14 +1479,15 @@ int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t l
     p.T = s.T, p.R = s.K, p.C = s.N, p.r = s.rank, p.n = s.adapters;
     p.x = (const char*)x, p.ldx = ldx * 2, p.w = (const char*)w, p.first = (const char*)a, p.second = (const char*)b;
     p.scale = scale, p.ids = ids, p.y = (char*)y, p.out_f32 = out_f32, p.h = h;
-    if (goes_few(s, plan)) {
+    if (adapter_few(s)) {
         FewPlan f;
         few_params(p, ws, f);
         few_first<kKs>(p, f, st);
         if (join_groups(p)) hipLaunchKernelGGL((adapter_few_second_kernel<4>), dim3((unsigned)few_joins(p)), dim3(256), 0, st, p);
         else hipLaunchKernelGGL((adapter_few_second_kernel<1>), dim3((unsigned)few_joins(p)), dim3(256), 0, st, p);
     } else {
-        many_launch<kKs>(p, s, plan, ws, st);
+        const int rc = many_launch<kKs>(p, s, plan, ws, st);
+        if (rc != MOE_OK) return rc;
     }
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
@@ -1507,7 +1514,7 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
     g.ldx[0] = lddy * 2, g.ldx[1] = ldx * 2;
     g.h[0] = h;
     g.out[0] = db, g.out[1] = da;
-    if (goes_few(s, plan)) {
+    if (adapter_few(s)) {
         FewPlan f;
         if (s.T > 0) {
             few_params(p, ws, f);
@@ -1527,7 +1534,8 @@ int adapter_backward_launch(const moe_adapter_shape_t& s, const void* dy, size_t
         else launch(std::integral_constant<int, 64>{});
     } else {
         p.h_given = h;
-        many_launch<kKc>(p, s, plan, ws, st);
+        const int rc = many_launch<kKc>(p, s, plan, ws, st);
+        if (rc != MOE_OK) return rc;
         // With so many adapters that they have few rows on average, those that do have are done by a kernel for that
         const bool rows = grad_rows(s);
         g.few = rows;

@@ -27,6 +27,7 @@ int bwd_launch(const moe_shape_t& s, const void* dy, const void* x, const void* 
                float* dtopk_w, char* ws, const moe_opts_t& opts, hipStream_t st);
 bool adapter_needs_plan(const moe_adapter_shape_t& s);
 size_t adapter_plan_bytes(const moe_adapter_shape_t& s);
+size_t adapter_table_bytes(const moe_adapter_shape_t& s);
 size_t adapter_workspace_bytes(const moe_adapter_shape_t& s);
 int adapter_plan_launch(const moe_adapter_shape_t& s, const int32_t* ids, void* plan, hipStream_t st);
 int adapter_forward_launch(const moe_adapter_shape_t& s, const void* x, size_t ldx, const void* w, const void* a,
@@ -379,8 +380,9 @@ int moe_adapter_workspace_bytes(const moe_adapter_shape_t* shape, size_t* ws_byt
 int moe_adapter_plan(const moe_adapter_shape_t* shape, const int32_t* ids, void* plan, size_t plan_bytes, void* stream) {
     const int rc = check_adapter_shape(shape);
     if (rc != MOE_OK) return rc;
-    const size_t need = adapter_plan_bytes(*shape);
-    if (need == 0) return MOE_OK;
+    // a plan that is given is filled or refused, also where this shape's own calls do without: those of a wider one may read it
+    const size_t need = adapter_table_bytes(*shape);
+    if (need == 0 || (!plan && adapter_plan_bytes(*shape) == 0)) return MOE_OK;
     if (!ids || !plan || !aligned(ids, 4) || !aligned(plan, 16)) return MOE_ERR_ARG;
     if (plan_bytes < need) return MOE_ERR_WORKSPACE;
     return adapter_plan_launch(*shape, ids, plan, (hipStream_t)stream);

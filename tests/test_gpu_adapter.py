@@ -296,3 +296,37 @@ def test_offsets_beyond_32_bits():
         e = ac.bounds(part, v, m, False)
         ac.check(got["db"][:, :, cols], v["db"], e["db"], (T, apart, "db"))
         del got, s, wide, dy
+
+
+@pytest.mark.parametrize("T", [257, 400, 512])
+def test_a_plan_of_257_to_512_tokens_serves_all_widths(T):
+    """Narrow shapes do not sort so few tokens and wide ones do: the results of either are the same bits whichever the plan was made with, or without one."""
+    import ctypes
+    r, n = 16, 5
+    sizes = {"narrow": (512, 136), "wide": (5800, 5800)}
+    s = {k: ac.make(T, K, N, r, n, "scattered") for k, (K, N) in sizes.items()}
+    s["wide"]["ids"] = s["narrow"]["ids"]
+    ids = s["narrow"]["ids"]
+    shape = {k: moe.make_adapter_shape(T, K, N, r, n) for k, (K, N) in sizes.items()}
+    plans = {k: moe.moe_adapter_plan(shape[k], ids) for k in sizes}
+    assert plans["narrow"].table is None and plans["wide"].table is not None
+    # a caller of the C interface with one buffer for its widest layer, filled by its first
+    table = torch.full_like(plans["wide"].table, -1)
+    lib = moe.load_library()
+    assert lib.moe_adapter_plan(ctypes.byref(shape["narrow"]), ids.data_ptr(), table.data_ptr(), 4 * table.numel(), torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    blocks = int(plans["wide"].table[0])
+    assert int(table[0]) == blocks and torch.equal(table[16:16 + 2 * blocks], plans["wide"].table[16:16 + 2 * blocks])
+    plans |= {"filled": moe.AdapterPlan(ids, table, n), "none": moe.AdapterPlan(ids, None)}
+    for k in sizes:
+        v, m = ac.plain(s[k])
+        e = ac.bounds(s[k], v, m, False)
+        want = None
+        for name, plan in plans.items():
+            h = torch.empty((T, r), device="cuda")
+            got = {"y": moe.moe_adapter_forward(shape[k], s[k]["x"], s[k]["w"], s[k]["a"], s[k]["b"], plan, scale=s[k]["scale"], h=h), "h": h}
+            got |= moe.moe_adapter_backward(shape[k], s[k]["dy"], s[k]["x"], s[k]["w"], s[k]["a"], s[k]["b"], plan, h, scale=s[k]["scale"])
+            for key in got:
+                ac.check(got[key], v[key], e[key], (T, k, name, key))
+            want = want or got
+            assert all(torch.equal(got[key], want[key]) for key in got), (T, k, name)

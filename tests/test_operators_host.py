@@ -139,3 +139,23 @@ def test_the_extension_module_refuses_what_is_no_argument():
         call.adapter_plan(b.ctypes.addressof(s), None, 0)
     with pytest.raises(TypeError):
         call.adapter_plan("shape", torch.zeros(600, dtype=torch.int32), 0)
+
+
+def test_a_plan_that_is_given_is_filled_or_refused(lib):
+    """With 257 to 512 tokens some widths read a plan and others do not: none that a wide shape may read stays unwritten without an error."""
+    for T in (257, 400, 512):
+        narrow, wide = moe.make_adapter_shape(T, 64, 128, 16, 4), moe.make_adapter_shape(T, 1 << 16, 1 << 16, 128, 4)
+        assert b._adapter_bytes(narrow)[1] == 0
+        need = b._adapter_bytes(wide)[1]
+        assert need > 0 and need == b._adapter_bytes(moe.make_adapter_shape(T, 1 << 16, 32768, 8, 4))[1]   # by tokens and adapters alone
+        for nbytes in (0, need - 1):
+            assert adapter_calls(lib, narrow, pbytes=nbytes)["plan"]() == b.MOE_ERR_WORKSPACE
+        assert adapter_calls(lib, narrow, plan=0x1004)["plan"]() == b.MOE_ERR_ARG
+        assert adapter_calls(lib, narrow, ids=None)["plan"]() == b.MOE_ERR_ARG
+        assert adapter_calls(lib, narrow, plan=None)["plan"]() == b.MOE_OK
+        assert adapter_calls(lib, wide, plan=None)["plan"]() == b.MOE_ERR_ARG
+        # a call without a plan has room for its own
+        ws = b._adapter_bytes(wide)[0]
+        assert adapter_calls(lib, wide, plan=None, nbytes=ws - 1)["forward"]() == b.MOE_ERR_WORKSPACE
+    most = moe.make_adapter_shape(256, 1 << 16, 1 << 16, 128, 4)   # no width sorts
+    assert b._adapter_bytes(most)[1] == 0 and adapter_calls(lib, most, plan=FAKE, pbytes=0)["plan"]() == b.MOE_OK
