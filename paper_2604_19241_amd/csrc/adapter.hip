@@ -39,8 +39,9 @@ struct PlanView {
 };
 static size_t plan_blocks(const moe_adapter_shape_t& s) { return (size_t)s.T / block_rows(s.T) + s.adapters + 2; }
 static size_t plan_units(const moe_adapter_shape_t& s) { return ((size_t)s.T + kUnit - 1) / kUnit; }
+// (room for blocks of 32 whatever their rows are: with as many adapters no two numbers of tokens have plans of one size, by which the binding knows a plan's own)
 static size_t plan_words(const moe_adapter_shape_t& s) {
-    return 16 + (size_t)s.T + 4 * (size_t)s.adapters + 1 + 2 * plan_units(s) + 2 * plan_blocks(s);
+    return 16 + (size_t)s.T + 4 * (size_t)s.adapters + 1 + 2 * plan_units(s) + 2 * ((size_t)s.T / 32 + s.adapters + 2);
 }
 static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
     PlanView v;

@@ -150,7 +150,13 @@ struct Operands {
         if (v[5] != Py_None) {
             const at::Tensor& t = tensor(v[5], "plan");
             if (PyLong_AsLong(v[6]) != s.adapters) refuse("plan", "made for another number of adapters");
-            if (!t.is_cuda()) refuse("plan", "expected a table on the GPU");
+            // (the kernels take token numbers from it: one of another batch would have them read elsewhere)
+            if (!t.is_cuda() || t.scalar_type() != at::kInt || !t.is_contiguous()) refuse("plan", "expected a contiguous table of int32 on the GPU");
+            moe_adapter_shape_t widest = s;   // up to 512 tokens some widths read no plan, and a plan serves them all
+            if (s.T <= 512) widest.K = widest.N = 1 << 16;
+            size_t need = 0;
+            if (p_adapter_bytes(&widest, nullptr, &need) == MOE_OK && t.numel() != (int64_t)(need / 4))   // (else the call refuses the shape)
+                refuse("plan", "made for another number of tokens");
             table = t.data_ptr();
         }
     }

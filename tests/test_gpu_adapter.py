@@ -330,3 +330,31 @@ def test_a_plan_of_257_to_512_tokens_serves_all_widths(T):
                 ac.check(got[key], v[key], e[key], (T, k, name, key))
             want = want or got
             assert all(torch.equal(got[key], want[key]) for key in got), (T, k, name)
+
+
+@pytest.mark.parametrize("T,N", [(40, 72), (300, 72), (700, 72), (420, 4616)])
+def test_a_table_that_is_not_the_batch_s_own_is_refused(T, N):
+    K, r, n = (64 if N == 72 else 4616), 8, 3
+    s = ac.make(T, K, N, r, n, "scattered")
+    shape = moe.make_adapter_shape(T, K, N, r, n)
+    plan = moe.moe_adapter_plan(shape, s["ids"])
+    h = torch.zeros((T, r), device="cuda")
+    table = plan.table
+    if table is None and T > 256:   # that of a wider layer
+        table = moe.moe_adapter_plan(moe.make_adapter_shape(T, 1 << 16, 1 << 16, r, n), s["ids"]).table
+
+    def both(t):
+        p = moe.AdapterPlan(s["ids"], t, n)
+        return (lambda: moe.moe_adapter_forward(shape, s["x"], s["w"], s["a"], s["b"], p, h=h),
+                lambda: moe.moe_adapter_backward(shape, s["dy"], s["x"], s["w"], s["a"], s["b"], p, h))
+
+    wrong = [moe.moe_adapter_plan(moe.make_adapter_shape(t, K, N, r, n), ac.ids_of("scattered", t, n)).table for t in (600, T + 513)]   # ids were replaced since
+    if table is not None:
+        for call in both(table):
+            call()
+        wrong += [table[:-1], torch.cat([table, table]), torch.cat([table, table[:1]]), torch.stack([table, table], 1)[:, 0], table.long(), table.float(), table.cpu(), table[:0]]
+    for t in wrong:
+        for call in both(t):
+            with pytest.raises(AssertionError):
+                call()
+    torch.cuda.synchronize()

@@ -159,3 +159,13 @@ def test_a_plan_that_is_given_is_filled_or_refused(lib):
         assert adapter_calls(lib, wide, plan=None, nbytes=ws - 1)["forward"]() == b.MOE_ERR_WORKSPACE
     most = moe.make_adapter_shape(256, 1 << 16, 1 << 16, 128, 4)   # no width sorts
     assert b._adapter_bytes(most)[1] == 0 and adapter_calls(lib, most, plan=FAKE, pbytes=0)["plan"]() == b.MOE_OK
+
+
+def test_plans_of_other_numbers_of_tokens_have_other_sizes():
+    """By which the binding knows that a table is the batch's own: blocks of the plan get longer from 16384 tokens on, its bytes do not get fewer."""
+    for n in (1, 7, 1024):
+        last = 0
+        for T in [257, 258, 300, 511, 512] + list(range(513, 700)) + list(range(16000, 17000)) + [1 << 20, 1 << 22]:
+            need = b._adapter_bytes(moe.make_adapter_shape(T, 1 << 16, 1 << 16, 8, n))[1]
+            assert need > last, (T, n)
+            last = need
