@@ -169,3 +169,44 @@ def test_plans_of_other_numbers_of_tokens_have_other_sizes():
             need = b._adapter_bytes(moe.make_adapter_shape(T, 1 << 16, 1 << 16, 8, n))[1]
             assert need > last, (T, n)
             last = need
+
+
+class NoMemory(torch.Tensor):
+    """A tensor of a GPU that is not there: sizes, type and device, and a null pointer that the library refuses."""
+
+    @staticmethod
+    def __new__(cls, dtype, sizes, device):
+        return torch.Tensor._make_wrapper_subclass(cls, sizes, dtype=dtype, device=device)
+
+    @classmethod
+    def __torch_dispatch__(cls, func, types, args=(), kwargs=None):
+        raise NotImplementedError(func)
+
+
+def test_tensors_on_several_gpus_are_refused():
+    call, bf, f32, i32, u8 = b._load_call(), torch.bfloat16, torch.float32, torch.int32, torch.uint8
+    T, K, N, r, n = 40, 64, 72, 8, 3
+    s = moe.make_adapter_shape(T, K, N, r, n)
+    E, k, S = 16, 2, 2
+    bal = moe.make_balance_shape(T, E, k, S)
+    stats = {"counts": (i32, (S, E)), "tokens": (i32, (S + 1,)), "lse": (f32, (T,))}
+    operands = {"w": (bf, (K, N)), "a": (bf, (n, r, K)), "b": (bf, (n, r, N)), "scale": (f32, (n,)), "ids": (i32, (T,))}
+    inputs = {"logits": (f32, (T, E)), "topk_idx": (i32, (T, k)), "seq_offsets": (i32, (S + 1,))}
+    calls = (   # shape, the tensors in their order and what stands between them
+        (call.adapter_forward, s, {"x": (bf, (T, K))} | operands | {"table": None, "adapters": n, "fp32": False, "h": (f32, (T, r)), "y": (bf, (T, N)), "ws": (u8, (1 << 30,)), "stream": 0}),
+        (call.adapter_backward, s, {"dy": (bf, (T, N)), "x": (bf, (T, K))} | operands | {"table": None, "adapters": n, "h": (f32, (T, r)), "dx": (bf, (T, K)), "da": (f32, (n, r, K)),
+                                                                                        "db": (f32, (n, r, N)), "ws": (u8, (1 << 30,)), "stream": 0}),
+        (call.balance_backward, bal, inputs | stats | {"topk_w": (f32, (T, k)), "dtopk_w": (f32, (T, k)), "dloss": (f32, (1,)), "bf16": False, "out": (f32, (T, E)), "stream": 0}))
+    for function, shape, kw in calls:
+        def made(other=None):
+            return [NoMemory(*v, "cuda:1" if name == other else "cuda:0") if type(v) is tuple else v for name, v in kw.items()]
+        assert function(b._addressof(shape), *made()) == b.MOE_ERR_ARG   # as the library says of a null pointer
+        for name, v in kw.items():
+            if type(v) is tuple:
+                with pytest.raises(AssertionError, match="GPU"):
+                    function(b._addressof(shape), *made(name))
+    # (the balance loss allocates its results before it calls the library)
+    for other in ("topk_idx", "seq_offsets", "mask"):
+        args = [NoMemory(*v, "cuda:1" if name == other else "cuda:0") for name, v in (inputs | {"mask": (torch.bool, (T,))}).items()]
+        with pytest.raises(AssertionError, match="GPU"):
+            call.balance_forward(b._addressof(bal), *args, None, 0)
