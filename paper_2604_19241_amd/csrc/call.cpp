@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include "../../include/uniep_moe.h"
@@ -125,8 +126,8 @@ PyObject* guarded(Py_ssize_t n, Py_ssize_t want, F f) {
         return f();
     } catch (const Refused&) {
         return nullptr;
-    } catch (const std::exception& e) {   // (an allocation that failed among them)
-        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {   // as torch's own functions raise it: torch.OutOfMemoryError for an allocation that failed
+        torch::translate_exception_to_python(std::current_exception());
         return nullptr;
     }
 }

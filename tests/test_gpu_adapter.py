@@ -358,3 +358,20 @@ def test_a_table_that_is_not_the_batch_s_own_is_refused(T, N):
             with pytest.raises(AssertionError):
                 call()
     torch.cuda.synchronize()
+
+
+def test_memory_that_is_not_there_raises_as_torch_does():
+    T, K, N, r, n = 1 << 20, 8, 16384, 8, 2   # a result of 32 GiB
+    s = ac.make(4, K, N, r, n, "one")
+    x, ids = torch.zeros((T, K), dtype=torch.bfloat16, device="cuda"), torch.zeros(T, dtype=torch.int32, device="cuda")
+    shape = moe.make_adapter_shape(T, K, N, r, n)
+    plan = moe.moe_adapter_plan(shape, ids)
+    torch.cuda.empty_cache()
+    torch.cuda.set_per_process_memory_fraction(0.05)   # torch's allocator refuses more by itself
+    try:
+        with pytest.raises(torch.OutOfMemoryError):
+            torch.empty((T, N), dtype=torch.bfloat16, device="cuda")
+        with pytest.raises(torch.OutOfMemoryError):
+            moe.moe_adapter_forward(shape, x, s["w"], s["a"], s["b"], plan)
+    finally:
+        torch.cuda.set_per_process_memory_fraction(1.0)
