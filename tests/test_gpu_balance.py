@@ -257,3 +257,13 @@ def test_logits_far_from_zero(E, k):
     assert ((st.lse.double() - v["lse"]).abs() <= 8 * 2.0 ** -23 * (v["lse"].abs() + 2)).all()
     assert ((st.prob_sums.double() - v["prob_sums"]).abs() <= rel * v["prob_sums"] + 1e-30).all()
     assert ((d.double() - v["dlogits"]).abs() <= err + 1e-30).all()
+
+
+@pytest.mark.parametrize("E,k,S", [(8, 2, 1), (8, 2, 3), (32, 4, 1)])
+def test_many_tokens_that_are_alike(E, k, S):
+    """Sums over 2^22 tokens keep the bound of one probability: equal terms are rounded equally, so that errors of a long sum add up instead of cancelling."""
+    T = (1 << 22) + 5
+    say(f"[balance] {T} {E} {k} {S}, all tokens alike")
+    s = make(T, E, k, S, masked=0.1 if S > 1 else 0.0, gates=False)
+    s["logits"][:], s["idx"][:] = s["logits"][:1].clone(), s["idx"][:1].clone()
+    check(s)
