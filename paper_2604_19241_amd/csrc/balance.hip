@@ -35,7 +35,7 @@ struct BalParams {
     // parts: of the tokens of chunk c that sequence s has, at slot c + s (from one part to the next c or s grows, so no two share a slot)
     float* part_p;            // [slots][E]
     int32_t* part_c;          // [slots][E]
-    float* part_z;            // [slots]
+    double* part_z;           // [slots]
     int32_t* part_n;          // [slots]
     double* sum_b;            // [S][blocks of experts]
     double* sum_z;            // [S]
@@ -124,7 +124,7 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
     constexpr int kMost = 4 * G * NV, kGroups = 64 / G, kU = NV == 1 ? (G == 64 ? 8 : 4) : 1, kSlots = (kMaxTopK + G - 1) / G;
     __shared__ float s_p[kBalWaves][kMost];
     __shared__ int32_t s_c[kMost];
-    __shared__ float s_z[kBalWaves];
+    __shared__ double s_z[kBalWaves];
     __shared__ int32_t s_n[kBalWaves];
     const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, E = p.E;
     const L ln(lane);
@@ -137,7 +137,8 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
         if (a >= b) continue;
         for (int e = tid; e < E; e += kBalThreads) s_c[e] = 0;
         __syncthreads();
-        float sums[L::kValues] = {}, z = 0.f;
+        float sums[L::kValues] = {};
+        double z = 0.0;   // (squares: in fp32 those of logits beyond 1.8e19, such as a mask's lowest value, would be infinite, and 0 times them NaN)
         int n = 0;
         // U tokens a turn: their loads are on their way together
         for (int t0 = a + w * kGroups + lane / G; t0 < b; t0 += kU * kBalWaves * kGroups) {
@@ -181,7 +182,7 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
                     for (int v = 0; v < L::kValues; ++v) sums[v] += x[u][v] * inv;
                     lse = m + logf(total);
                     if (ln.g == 0) {
-                        z += lse * lse;
+                        z += (double)lse * lse;
                         ++n;
                     }
                 }
@@ -221,7 +222,7 @@ __global__ void __launch_bounds__(kBalThreads) balance_forward_kernel(BalParams 
             __syncthreads();
             if (tid == 0) {
                 p.tokens[0] = n;
-                write_losses(p, n > 0 ? (((s_b[0] + s_b[1]) + s_b[2]) + s_b[3]) / ((double)p.k * n) : 0.0, ((double)s_z[0] + s_z[1]) + s_z[2] + s_z[3], n);
+                write_losses(p, n > 0 ? (((s_b[0] + s_b[1]) + s_b[2]) + s_b[3]) / ((double)p.k * n) : 0.0, ((s_z[0] + s_z[1]) + s_z[2]) + s_z[3], n);
             }
             return;
         }
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p, i
     for (int i = tid; i < count; i += kSumThreads) {
         const size_t slot = (size_t)first + i + s;
         n += p.part_n[slot];
-        z += (double)p.part_z[slot];
+        z += p.part_z[slot];
     }
     // (in 64 bits: there are as many parts as the tokens make, and parts that are alike are rounded alike; of 65536 alike, 2048 a thread, sums in fp32 were off by 2.7e-5)
     double sum = 0.0;
@@ -490,7 +491,7 @@ static BalLayout bal_layout(const moe_balance_shape_t& s) {
     size_t at = 0;
     L.p = at, at = align_up(at + slots * s.E * 4, 256);
     L.c = at, at = align_up(at + slots * s.E * 4, 256);
-    L.z = at, at = align_up(at + slots * 4, 256);
+    L.z = at, at = align_up(at + slots * 8, 256);
     L.n = at, at = align_up(at + slots * 4, 256);
     L.b = at, at = align_up(at + (size_t)s.seqs * sum_blocks(s) * 8, 256);
     L.sz = at, at = align_up(at + (size_t)s.seqs * 8, 256);
@@ -533,7 +534,7 @@ int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, co
     const BalLayout L = bal_layout(s);
     p.logits = logits, p.idx = idx, p.offsets = offsets, p.mask = mask;
     p.loss = out.loss, p.counts = out.counts, p.tokens = out.tokens, p.prob_sums = out.prob_sums, p.lse = out.lse;
-    p.part_p = (float*)(ws + L.p), p.part_c = (int32_t*)(ws + L.c), p.part_z = (float*)(ws + L.z), p.part_n = (int32_t*)(ws + L.n);
+    p.part_p = (float*)(ws + L.p), p.part_c = (int32_t*)(ws + L.c), p.part_z = (double*)(ws + L.z), p.part_n = (int32_t*)(ws + L.n);
     p.sum_b = (double*)(ws + L.b), p.sum_z = (double*)(ws + L.sz), p.ticket = (int32_t*)(ws + L.ticket);
     if (p.chunks > 0)
         by_experts(s.E, rows_aligned(logits, nullptr, s.E), [&](auto g, auto nv, auto vec) {

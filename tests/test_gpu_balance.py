@@ -267,3 +267,27 @@ def test_many_tokens_that_are_alike(E, k, S):
     s = make(T, E, k, S, masked=0.1 if S > 1 else 0.0, gates=False)
     s["logits"][:], s["idx"][:] = s["logits"][:1].clone(), s["idx"][:1].clone()
     check(s)
+
+
+@pytest.mark.parametrize("T,E,k,S", [(200, 40, 3, 1), (200, 8, 2, 1), (3000, 64, 4, 5), (700, 300, 8, 2)])
+def test_tokens_with_every_expert_at_the_lowest_value(T, E, k, S, monkeypatch):
+    """Their lse is beyond what has a square in fp32.  Without a z loss that square is nothing; with it the loss is what 64 bits give, rounded.
+    (Equal logits have equal probabilities whatever they are: the formulas are taken at 0, as 3e38 + log E is 3e38 in 64 bits too.)"""
+    s = make(T, E, k, S, gates=False)
+    at = T // 3
+    s["logits"][at] = 0.0
+    rel = 64 * 2.0 ** -23   # as in check()
+    monkeypatch.setitem(globals(), "ZC", 0.0)
+    v = plain(s)
+    s["logits"][at] = torch.finfo(torch.float32).min
+    st, d = run(s)
+    assert abs(float(st.loss[0]) - v["loss"][0]) <= rel * v["loss"][1] and abs(float(st.loss[1]) - v["loss"][1]) <= rel * v["loss"][1]
+    assert float(st.loss[2]) == float("inf")   # (1e77 / T)
+    err = rel * v["p"] * 0.75 * BC * E * 2 / T + 16 * 2.0 ** -23 * v["dlogits"].abs()
+    assert ((d.double() - v["dlogits"]).abs() <= err + 1e-30).all()
+    monkeypatch.setitem(globals(), "ZC", 0.003)
+    s["logits"][at] = 1e20   # a square of 1e40, of which 1 / T is less than 3e38 (the other tokens' are nothing beside it)
+    z = float(s["logits"][at, 0]) ** 2 / T
+    st, d = run(s)
+    for got, want in zip(st.loss.tolist(), (0.003 * z, v["loss"][1], z)):
+        assert abs(got - want) <= rel * want
