@@ -269,16 +269,30 @@ __global__ void __launch_bounds__(kSumThreads) balance_sum_kernel(BalParams p, i
         n += p.part_n[slot];
         z += p.part_z[slot];
     }
-    // (in 64 bits: there are as many parts as the tokens make, and parts that are alike are rounded alike; of 65536 alike, 2048 a thread, sums in fp32 were off by 2.7e-5)
+    // (in 64 bits: there are as many parts as the tokens make, and parts that are alike are rounded alike; of 65536 alike, 2048 a thread, sums in fp32 were off by 2.7e-5.
+    // The eight parts that a turn fetches are added among themselves first: 131072 tokens, 129 experts 15.9 us, with a 64-bit addition for each 19.8)
     double sum = 0.0;
     int c = 0;
-    if (e < p.E)
-#pragma unroll 8
-        for (int i = grp; i < count; i += groups) {
+    if (e < p.E) {
+        int i = grp;
+        for (; i + 7 * groups < count; i += 8 * groups) {
+            float v[8];
+            int u[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const size_t at = ((size_t)first + i + k * groups + s) * p.E + e;
+                v[k] = p.part_p[at];
+                u[k] = p.part_c[at];
+            }
+            sum += (double)(((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7])));
+            c += ((u[0] + u[1]) + (u[2] + u[3])) + ((u[4] + u[5]) + (u[6] + u[7]));
+        }
+        for (; i < count; i += groups) {
             const size_t at = ((size_t)first + i + s) * p.E + e;
             sum += (double)p.part_p[at];
             c += p.part_c[at];
         }
+    }
     s_p[tid] = sum;
     s_c[tid] = c;
     sum_i(n, 0);
