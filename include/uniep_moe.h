@@ -343,7 +343,8 @@ int moe_balance_workspace_bytes(const moe_balance_shape_t* shape, size_t* ws_byt
  *   logits       [T,E] fp32
  *   topk_idx     [T,k] int32, as moe_route writes it (values outside [0,E) are no slot)
  *   seq_offsets  [seqs + 1] int32, ascending from 0 to T; NULL: one sequence (seqs must be 1)
- *   mask         [T] bytes, 0 = not kept (padding: its logits are not looked at), or NULL (all kept) */
+ *   mask         [T] bytes, 0 = not kept (padding: whatever its logits and slots hold, they enter no result), or NULL (all kept)
+ * A kept token needs a logit above -inf: one without has no softmax, and the loss is NaN. */
 int moe_balance_forward(const moe_balance_shape_t* shape, const float* logits, const int32_t* topk_idx, const int32_t* seq_offsets,
                         const uint8_t* mask, const moe_balance_stats_t* out, void* ws, size_t ws_bytes, void* stream);
 

@@ -55,10 +55,16 @@ static PlanView plan_view(const moe_adapter_shape_t& s, void* plan) {
     v.many = v.seg + s.adapters;
     return v;
 }
-// Whether the path for few tokens is taken where there is a choice: up to 512 tokens, unless a large product in tiles of 64 x 64 would cost more than the sorting does.  Measured, us
-// of the forward call and of the training step, few tokens / sorted (K, N, ranks, adapters): 200 tokens 7168 x 7168, 16, 16 55.9 and 118 / 71.0 and 154, 300 79.0 and 161 / 81.6
-// and 183, 400 98.8 and 204 / 82.6 and 184; 300 4096 x 4096, 128, 2 66.5 and 136 / 52.8 and 122; 512 2048 x 2816, 16, 16 21.0 and 48.4 / 31.0 and 66.4; 512 680 x 480, 128, 4
-// 20.3 and 48.5 / 27.0 and 76.1; 512 2048 x 7168, 8, 256 45.3 and 130 / 62.3 and 306.
+// Whether the path for few tokens is taken: up to 256 tokens always, up to 512 unless the product, in tiles of 64 x 64, is large. Measured, us of the forward call and of the training step in a
+// graph of ten, few tokens / sorted with the plan (tokens, K x N, ranks, adapters):
+//   512, 2048 x 2816,  16,  16     24.4,  58.1 /  33.6,  80.2        400, 7168 x 7168,  16,   2    106.3, 216.7 /  83.5, 164.9
+//   512, 2048 x 2816, 128,   2     43.2,  95.0 /  40.8,  87.7        400, 7168 x 7168,  16,  16    104.7, 225.3 /  89.5, 197.5
+//   512, 2048 x 2816, 128, 256     57.7, 361.7 /  93.5, 352.2        400, 7168 x 7168, 128,   2    134.4, 298.6 / 102.3, 240.4
+//   300, 4096 x 4096, 128,   2     50.4, 109.7 /  54.4, 115.1        300, 7168 x 7168,  16,   2     85.1, 170.2 /  81.6, 159.0
+//   512, 4096 x 4096,  16,  16     44.2,  98.9 /  52.8, 118.8        300, 7168 x 7168,  16,  16     83.8, 177.4 /  91.5, 202.5
+//   512, 4096 x 4096, 128,   2     61.9, 143.9 /  60.1, 126.5        400, 7168 x 7168, 128,  16    143.8, 361.4 / 232.6, 510.6
+// The left column's are not sorted, the right one's are.  The rule knows neither ranks nor adapters and is on the slower side for 300 tokens of 16 adapters (9 to 14 %), by 40 to 60 % where tiles of
+// sorted tokens have long low-rank parts (the last line on the right), and by up to 14 % for 512 tokens on few adapters of many ranks (128, 2 on the left).
 static bool adapter_few(const moe_adapter_shape_t& s) { return s.T <= kFewTokens / 2 || (s.T <= kFewTokens && (long long)s.T * s.K * s.N <= 8ll << 30); }
 bool adapter_needs_plan(const moe_adapter_shape_t& s) { return s.T > kFewTokens; }
 // What a plan holds goes by the tokens and the adapters alone, whatever the widths of the shape that it is made with: a plan serves layers of all widths, and up to 512 tokens some
@@ -703,8 +709,6 @@ static size_t hx_bytes(const moe_adapter_shape_t& s, int tile_rows) {
     return 2 * (size_t)tile_rows * (tiles * (3 * (size_t)s.rank + BK) + segs * 3 * (size_t)s.rank);   // (three terms, for an fp32 result)
 }
 
-// h of one block of the plan, as fp32 and as the rows of its tile's low-rank part; behind the blocks, where the factors are wanted
-// transposed, 64 columns of one adapter's a workgroup.
 // v as three bf16 terms: the whole 24 bits of an fp32 value
 __device__ __forceinline__ void store_terms(uint16_t* to, int r, float (&v)[8]) {
 #pragma unroll
@@ -717,6 +721,8 @@ __device__ __forceinline__ void store_terms(uint16_t* to, int r, float (&v)[8]) 
         for (int q = 0; q < 8; ++q) v[q] = fabsf(e[q]) < INFINITY ? v[q] - e[q] : 0.f;   // (an infinite value stays one)
     }
 }
+// h of one block of the plan, as fp32 and as the rows of its tile's low-rank part; behind the blocks, where the factors are wanted
+// transposed, 64 columns of one adapter's a workgroup.
 template <int NRF, int NCF>
 __global__ void __launch_bounds__(kSmallThreads) adapter_low_kernel(ProjParams p) {
     using S = SmallTile<NRF, NCF>;
@@ -898,7 +904,7 @@ __global__ void __launch_bounds__(256) adapter_parts_join_kernel(ProjParams p) {
     else *(u32x2_t*)(p.y + at * 2) = u32x2_t{pack_bf16x2(acc[0], acc[1]), pack_bf16x2(acc[2], acc[3])};
 }
 
-// sum_j h[j] second[a][j][col ..]: the low-rank part of 8 columns of one row, for tiles in which something is not finite
+// sum_j h[j] second[a][j][col ..]: the low-rank part of 8 columns of one row, for tiles with many adapters (tile_low's `apart`) and those in which something is not finite
 __device__ __forceinline__ void add_low(const ProjParams& p, int row, int col, float (&v)[8]) {
     const int t = p.plan.order[row], a = adapter_of(p.ids, t, p.n);
     if (a < 0) return;
@@ -1385,8 +1391,13 @@ static int grad_parts(const moe_adapter_shape_t& s) {
     return std::max(1, std::min(grad_pieces(s), s.T / 512));
 }
 // Whether a product of sorted tokens is cut along its reduction into fp32 parts, with h beside it, as that of few tokens: long reductions of small results, which
-// tiles in one piece leave to a few CUs, behind an equally long h.  Measured, us of the forward call in one piece / in parts (tokens, K,
-// N): 2608, 6952, 24 58.8 / 30.2; 4099, 2048, 128 27.6 / 24.8; 6793, 5800, 64 50.1 / 45.3; 1214, 5720, 1640 79.4 / 93.6.
+// tiles in one piece leave to a few CUs, behind an equally long h.  Measured, us of the forward call with its plan in a graph of ten, in one piece / in parts (tokens, K, N):
+//   2608, 6952,  24   49.7 / 30.6      8192, 2048,  64   31.6 / 31.6  (T C = 512 << 10)      12000, 2048, 128   42.5 / 47.2
+//   6793, 5800,  64   52.7 / 44.4      1214, 5720, 840   80.3 / 70.9  (996 << 10)             8192, 2048, 256   39.8 / 53.5
+//   4099, 2048, 128   28.2 / 24.0      4099, 2048, 256   33.3 / 34.9  (1025 << 10)            8192, 7168, 256   88.8 / 113.2
+//                                      4099, 7168, 256   72.9 / 70.1                          1214, 5720, 1640  83.8 / 93.5
+//                                      8192, 2048, 128   32.6 / 38.7  (1024 << 10)
+// (the middle column is what lies about the limit: either way within 4 %, but for one line that gains 12 % in parts and one that loses 19)
 static bool parts_pay(int T, int R, int C) { return T < 16384 && stages_in(R) >= 24 && (long long)T * C <= 640 << 10; }
 static int parts_blocks(const moe_adapter_shape_t& s) { return ((int)plan_blocks(s) + 7) & ~7; }
 static size_t parts_bytes(const moe_adapter_shape_t& s, int R, int C) {
