@@ -356,6 +356,57 @@ int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, 
                          const moe_balance_stats_t* stats, const float* topk_w, const float* dtopk_w,
                          const float* dloss, void* dlogits, int32_t out_bf16, void* stream);
 
+/* ---- Tokens to the rows of their experts and back -----------------------------------
+ * For experts that are not the fused layer's own (the products in 4 bits below, experts of other ranks behind moe_global_map): with row(t,j) = row_of[t,j],
+ *   dispatch  xs[row(t,j)] = x[t]                    its gradient  dx[t] = sum_j dxs[row(t,j)]
+ *   combine   y[t] = sum_j w[t,j] o[row(t,j)]        its gradient  do[row(t,j)] = w[t,j] dy[t],  dw[t,j] = <dy[t], o[row(t,j)]>
+ * Slots whose row is outside [0, rows) have none: they are not read, not written and add nothing (dw = 0).  Every row may stand in the table once at most: two slots
+ * that name one row leave either token's values there.  Rows that no slot names are left as they were.  Sums are fp32 in the order of the slots, rounded once; the results are
+ * the same bits on every run.  All activations of a call have one type, bf16 or (f32 = 1) fp32.
+ * Limits (MOE_ERR_SHAPE otherwise): 0 <= T, 1 <= k <= 16, T * k < 2^30, d a multiple of 8 from 8 to 2^20, T * d <= 2^38, 0 <= rows. */
+typedef struct {
+    int32_t T;      /* tokens */
+    int32_t k;      /* slots of a token */
+    int32_t d;      /* columns */
+    int32_t rows;   /* of the sorted buffers */
+} moe_dispatch_shape_t;
+
+/*   x       [T,d], rows ldx elements apart (a multiple of 8, at least d)
+ *   row_of  [T,k] int32: moe_route's inv_perm, or moe_global_map's dst_row for a send buffer
+ *   xs      [rows,d] */
+int moe_dispatch_forward(const moe_dispatch_shape_t* shape, const void* x, int64_t ldx, int32_t f32, const int32_t* row_of, void* xs, void* stream);
+int moe_dispatch_backward(const moe_dispatch_shape_t* shape, const void* dxs, int32_t f32, const int32_t* row_of, void* dx, void* stream);
+/*   w       [T,k] fp32: the gates, or NULL (1) */
+int moe_combine_forward(const moe_dispatch_shape_t* shape, const void* o, int32_t f32, const int32_t* row_of, const float* w, void* y, void* stream);
+/*   dy      [T,d], rows lddy apart;   d_o [rows,d];   dw [T,k] fp32, or NULL (o is not read then and may be NULL) */
+int moe_combine_backward(const moe_dispatch_shape_t* shape, const void* dy, int64_t lddy, const void* o, int32_t f32, const int32_t* row_of, const float* w,
+                         void* d_o, float* dw, void* stream);
+
+/* ---- The stash in 8 bits ------------------------------------------------------------------
+ * What the backward pass reads of `saved` is G, U and h.  Packed, G and U of every row are 8-bit integers with an exponent for 32 of them, 2.06 I bytes a row instead of the
+ * stash's 6 I + 2 d: a layer keeps that, and the layers of a model share one stash.
+ *   block of 32 values, e = floor(log2 max|v|), at least -126:  v ~ 2^(e - 6) q, q whole in [-127, 127], nearest, ties to even (exact in bf16)
+ * A block that holds an infinity or NaN comes back as NaN.  Rows at and beyond A (routing->offsets[e_count]) are neither read nor written.
+ *   codes   [T*k, 2 I] int8;  scales [T*k, 2 I / 32] bytes: e + 127, 255 for NaN */
+int moe_saved_pack(const moe_shape_t* shape, const moe_routing_t* routing, const void* saved, void* codes, void* scales, void* stream);
+/* Writes the stash that moe_fused_backward reads: G and U as packed, h = silu(G) U of these; its part o is left as it was. */
+int moe_saved_unpack(const moe_shape_t* shape, const moe_routing_t* routing, const void* codes, const void* scales, void* saved, void* stream);
+
+/* ---- Microscaled 4-bit floating point -------------------------------------------------------
+ * Rows of K values in blocks of 32 along K: with e = floor(log2 max|v|), at least -125, a block's scale is 2^(e - 2) and its values are multiples of it by
+ * {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign (e2m1: nearest, ties to even, beyond 6 becomes 6).  Codes lie two to a byte, the first in the lower half; a scale is a byte,
+ * e - 2 + 127, 255 for a block that holds an infinity or NaN (all of it is NaN then).
+ * Rows are filled up with zeros to K' = K rounded up to a multiple of 128: codes [rows, K' / 2], scales [rows, K' / 32] bytes, both 16-byte aligned.  (Codes and scales
+ * of the same layout from elsewhere are as good; their padding has to be zeros with a scale other than 255.)
+ * Limits (MOE_ERR_SHAPE otherwise): 0 <= rows < 2^31, K a multiple of 8 from 8 to 2^16, rows * K <= 2^36. */
+
+/*   x       [rows,K] bf16 or (f32 = 1) fp32, rows ldx elements apart (a multiple of 8, at least K) */
+int moe_mx_quantize(const void* x, int64_t ldx, int32_t f32, int64_t rows, int32_t K, void* codes, void* scales, void* stream);
+/* Weights w [experts,K,N] bf16, as moe_fused_forward takes them, to codes and scales of [experts,N,K]: blocks along K.  N a multiple of 8 from 8 to 2^16, experts from 1 to 1024. */
+int moe_mx_quantize_weights(const void* w, int32_t experts, int32_t K, int32_t N, void* codes, void* scales, void* stream);
+/* The values that codes and scales stand for, [rows,K] bf16 (exact but for scales beyond 2^125) or fp32. */
+int moe_mx_values(const void* codes, const void* scales, int64_t rows, int32_t K, void* out, int32_t out_f32, void* stream);
+
 /* Synchronises `stream`, reads the status word a forward/backward call left in
  * its workspace and returns MOE_OK or MOE_ERR_DEVICE (test and debug aid; the
  * hot path never calls it). */

@@ -4,7 +4,7 @@ Argument marshalling only: torch supplies device memory and the current HIP
 stream; every step of the hot path runs in the library's kernels.  There is
 no CPU fallback: a missing library or a failed call raises.
 
-The calls that take longer on the host than on the GPU in Python (the projection with adapters and the balance loss) check their tensors and
+The calls that take longer on the host than on the GPU in Python (all but the routed experts' own) check their tensors and
 allocate their outputs in an extension module (csrc/call.cpp), which calls the same library.
 """
 from __future__ import annotations
@@ -27,7 +27,9 @@ EXPORTS = ("moe_workspace_bytes", "moe_backward_workspace_bytes", "moe_saved_lay
            "moe_fused_backward", "moe_route_backward", "moe_global_map", "moe_device_status",
            "moe_status_string", "moe_calibration_copy", "moe_perf_model_eval",
            "moe_perf_model_search", "moe_route_static", "moe_calibration_mfma", "moe_adapter_workspace_bytes", "moe_adapter_plan",
-           "moe_adapter_forward", "moe_adapter_backward", "moe_balance_workspace_bytes", "moe_balance_forward", "moe_balance_backward")
+           "moe_adapter_forward", "moe_adapter_backward", "moe_balance_workspace_bytes", "moe_balance_forward", "moe_balance_backward",
+           "moe_dispatch_forward", "moe_dispatch_backward", "moe_combine_forward", "moe_combine_backward", "moe_saved_pack", "moe_saved_unpack",
+           "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values")
 
 ROUTE_STATIC_SCRATCH_BYTES = 4 << 20   # MOE_ROUTE_STATIC_SCRATCH_BYTES
 
@@ -73,6 +75,15 @@ _ARGTYPES = {
     "moe_adapter_backward": [_P, _P, _L, _P, _L] + [_P] * 10 + [_P, _N, _P],
     "moe_balance_forward": [_P] * 7 + [_N, _P],
     "moe_balance_backward": [_P] * 9 + [_I, _P],
+    "moe_dispatch_forward": [_P, _P, _L, _I, _P, _P, _P],
+    "moe_dispatch_backward": [_P, _P, _I, _P, _P, _P],
+    "moe_combine_forward": [_P, _P, _I, _P, _P, _P, _P],
+    "moe_combine_backward": [_P, _P, _L, _P, _I] + [_P] * 5,
+    "moe_saved_pack": [_P] * 6,
+    "moe_saved_unpack": [_P] * 6,
+    "moe_mx_quantize": [_P, _L, _I, _L, _I, _P, _P, _P],
+    "moe_mx_quantize_weights": [_P, _I, _I, _I, _P, _P, _P],
+    "moe_mx_values": [_P, _P, _L, _I, _P, _I, _P],
 }
 _lib = None
 
@@ -145,7 +156,8 @@ def _load_call():
             raise FileNotFoundError(f"{CALL_PATH} is missing: build it with `python -m paper_2604_19241_amd.build`.")
         from . import _call as module
         names = ("moe_adapter_plan", "moe_adapter_forward", "moe_adapter_backward", "moe_balance_forward", "moe_balance_backward",
-                 "moe_adapter_workspace_bytes", "moe_balance_workspace_bytes")
+                 "moe_adapter_workspace_bytes", "moe_balance_workspace_bytes", "moe_dispatch_forward", "moe_dispatch_backward", "moe_combine_forward",
+                 "moe_combine_backward", "moe_saved_pack", "moe_saved_unpack", "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values")
         module.bind(*[ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names])
         _call = module
     return _call
@@ -497,6 +509,124 @@ def moe_balance_backward(shape: MoEBalanceShape, logits, topk_idx, stats: Balanc
                                 out_dtype is _BF16, out, _raw_stream(logits))
     if type(got) is int:
         _check(got, "moe_balance_backward")
+    return got
+
+
+# ---- tokens to the rows of their experts and back ----------------------------
+
+class MoEDispatchShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("T", "k", "d", "rows")]
+
+
+def make_dispatch_shape(T, k, d, rows=None) -> MoEDispatchShape:
+    """T tokens of k slots and d columns; rows of the sorted buffers: T k without a number."""
+    return MoEDispatchShape(T, k, d, T * k if rows is None else rows)
+
+
+def moe_dispatch_forward(shape: MoEDispatchShape, x, row_of, out: torch.Tensor | None = None) -> torch.Tensor:
+    """xs[row_of[t,j]] = x[t]: x [T,d] bf16 or fp32 (rows may be parts of wider ones), row_of [T,k] int32 (moe_route's inv_perm, moe_global_map's dst_row),
+    every row at most once.  Slots with a row outside [0, rows) have none; rows that no slot names keep what `out` held (unspecified in a new one)."""
+    call = _call or _load_call()
+    got = call.dispatch_forward(_addressof(shape), x, row_of, out, _raw_stream(x))
+    if type(got) is int:
+        _check(got, "moe_dispatch_forward")
+    return got
+
+
+def moe_dispatch_backward(shape: MoEDispatchShape, dxs, row_of, out: torch.Tensor | None = None) -> torch.Tensor:
+    """Gradient of x: dx[t] = sum_j dxs[row_of[t,j]]."""
+    call = _call or _load_call()
+    got = call.combine_forward(_addressof(shape), dxs, row_of, None, out, _raw_stream(dxs))
+    if type(got) is int:
+        _check(got, "moe_dispatch_backward")
+    return got
+
+
+def moe_combine_forward(shape: MoEDispatchShape, o, row_of, weights=None, out: torch.Tensor | None = None) -> torch.Tensor:
+    """y[t] = sum_j weights[t,j] o[row_of[t,j]]: o [rows,d] bf16 or fp32, weights [T,k] fp32 (ones without)."""
+    call = _call or _load_call()
+    got = call.combine_forward(_addressof(shape), o, row_of, weights, out, _raw_stream(o))
+    if type(got) is int:
+        _check(got, "moe_combine_forward")
+    return got
+
+
+def moe_combine_backward(shape: MoEDispatchShape, dy, o, row_of, weights=None, want_dw: bool = True, out: dict | None = None) -> dict:
+    """Gradients of o, do[row_of[t,j]] = weights[t,j] dy[t] (rows that no slot names as in moe_dispatch_forward), and of the weights, fp32.  Without
+    want_dw o is not read."""
+    call = _call or _load_call()
+    d_o, dw = (None, None) if out is None else (out["do"], out.get("dw"))
+    got = call.combine_backward(_addressof(shape), dy, o, row_of, weights, d_o, dw, bool(want_dw), _raw_stream(dy))
+    if type(got) is int:
+        _check(got, "moe_combine_backward")
+    return {"do": got[0], "dw": got[1]}
+
+
+# ---- the stash in 8 bits -----------------------------------------------------
+
+@dataclass
+class PackedSaved:
+    """What the backward pass needs of one layer's stash, in 8 bits."""
+    codes: torch.Tensor    # [T k, 2 I] int8
+    scales: torch.Tensor   # [T k, 2 I / 32] uint8
+
+
+def moe_saved_pack(shape: MoEShape, routing: Routing, saved: torch.Tensor, out: PackedSaved | None = None) -> PackedSaved:
+    """G and U of the stash that moe_fused_forward filled, in 8 bits with an exponent for 32 of them.  The stash is free for another layer then."""
+    call = _call or _load_call()
+    codes, scales = (None, None) if out is None else (out.codes, out.scales)
+    got = call.saved_pack(_addressof(shape), routing.offsets, saved, codes, scales, _raw_stream(saved))
+    if type(got) is int:
+        _check(got, "moe_saved_pack")
+    return PackedSaved(*got)
+
+
+def moe_saved_unpack(shape: MoEShape, routing: Routing, packed: PackedSaved, saved: torch.Tensor) -> torch.Tensor:
+    """Fills the stash for moe_fused_backward: G and U as they were packed, and h = silu(G) U."""
+    call = _call or _load_call()
+    got = call.saved_unpack(_addressof(shape), routing.offsets, saved, packed.codes, packed.scales, _raw_stream(saved))
+    if type(got) is int:
+        _check(got, "moe_saved_unpack")
+    return saved
+
+
+# ---- microscaled 4-bit floating point ----------------------------------------
+
+@dataclass
+class MXTensor:
+    """Values [..., K] in 4 bits, with a scale for every 32 of them along K; K' is K rounded up to a multiple of 128, filled up with zeros."""
+    codes: torch.Tensor    # [..., K' / 2] uint8: two values a byte, the first in the lower half
+    scales: torch.Tensor   # [..., K' / 32] uint8: powers of two with a bias of 127, 255 for NaN
+    K: int
+
+
+def moe_mx_quantize(x, out: MXTensor | None = None) -> MXTensor:
+    """Rows x [rows,K] bf16 or fp32 (they may be parts of wider ones), K a multiple of 8."""
+    call = _call or _load_call()
+    codes, scales = (None, None) if out is None else (out.codes, out.scales)
+    got = call.mx_quantize(x, codes, scales, _raw_stream(x))
+    if type(got) is int:
+        _check(got, "moe_mx_quantize")
+    return MXTensor(got[0], got[1], x.shape[1])
+
+
+def moe_mx_quantize_weights(w, out: MXTensor | None = None) -> MXTensor:
+    """Weights w [experts,K,N] bf16, as moe_fused_forward takes them, to values [experts,N,K]: their blocks run along K."""
+    call = _call or _load_call()
+    codes, scales = (None, None) if out is None else (out.codes, out.scales)
+    got = call.mx_quantize_weights(w, codes, scales, _raw_stream(w))
+    if type(got) is int:
+        _check(got, "moe_mx_quantize_weights")
+    return MXTensor(got[0], got[1], w.shape[1])
+
+
+def moe_mx_values(mx: MXTensor, out_dtype=torch.bfloat16, out: torch.Tensor | None = None) -> torch.Tensor:
+    """The values [..., K] that codes and scales stand for."""
+    assert out_dtype is _F32 or out_dtype is _BF16
+    call = _call or _load_call()
+    got = call.mx_values(mx.codes, mx.scales, mx.K, out_dtype is _F32, out, _raw_stream(mx.codes))
+    if type(got) is int:
+        _check(got, "moe_mx_values")
     return got
 
 

@@ -43,6 +43,15 @@ int balance_forward_launch(const moe_balance_shape_t& s, const float* logits, co
 int balance_backward_launch(const moe_balance_shape_t& s, const float* logits, const int32_t* idx,
                             const int32_t* offsets, const moe_balance_stats_t& stats, const float* w, const float* dw, const float* dloss, void* dlogits, int out_bf16,
                             hipStream_t st);
+int dispatch_forward_launch(const moe_dispatch_shape_t& s, const void* x, size_t ldx, int f32, const int32_t* row_of, void* xs, hipStream_t st);
+int combine_forward_launch(const moe_dispatch_shape_t& s, const void* o, int f32, const int32_t* row_of, const float* w, void* y, hipStream_t st);
+int combine_backward_launch(const moe_dispatch_shape_t& s, const void* dy, size_t lddy, const void* o, int f32, const int32_t* row_of, const float* w,
+                            void* d_o, float* dw, hipStream_t st);
+int saved_pack_launch(const moe_shape_t& s, const int32_t* offsets, const char* gu, uint8_t* codes, uint8_t* scales, hipStream_t st);
+int saved_unpack_launch(const moe_shape_t& s, const int32_t* offsets, const uint8_t* codes, const uint8_t* scales, char* gu, char* h, hipStream_t st);
+int mx_quantize_launch(const void* x, size_t ldx, int f32, int64_t rows, int K, uint8_t* codes, uint8_t* scales, hipStream_t st);
+int mx_values_launch(const uint8_t* codes, const uint8_t* scales, int64_t rows, int K, void* out, int f32, hipStream_t st);
+int mx_quantize_weights_launch(const void* w, int experts, int K, int N, uint8_t* codes, uint8_t* scales, hipStream_t st);
 }  // namespace uniep
 
 using namespace uniep;
@@ -130,6 +139,32 @@ int check_balance(const moe_balance_shape_t& s, const float* logits, const int32
         if (!aligned(p, 4)) return MOE_ERR_ARG;
     return MOE_OK;
 }
+
+int check_dispatch_shape(const moe_dispatch_shape_t* s) {
+    if (!s) return MOE_ERR_ARG;
+    if (s->T < 0 || s->k < 1 || s->k > kMaxTopK || (int64_t)s->T * s->k >= (1ll << 30) || s->rows < 0) return MOE_ERR_SHAPE;
+    if (s->d < 8 || s->d > 1 << 20 || s->d % 8 != 0 || (int64_t)s->T * s->d > (1ll << 38)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+// What every call that moves tokens has to be given: the token's side (rows ld apart), the rows' side and the table.
+int check_move(const moe_dispatch_shape_t& s, const void* tokens, int64_t ld, const void* rows, int f32, const int32_t* row_of) {
+    if (f32 != 0 && f32 != 1) return MOE_ERR_ARG;
+    if (s.T > 0 && (!tokens || !row_of || ld < s.d || ld % 8 != 0 || ld > (1ll << 40) / s.T)) return MOE_ERR_ARG;
+    if (s.T > 0 && s.rows > 0 && !rows) return MOE_ERR_ARG;
+    return aligned(tokens, 16) && aligned(rows, 16) && aligned(row_of, 4) ? MOE_OK : MOE_ERR_ARG;
+}
+int check_packed(const moe_shape_t* s, const moe_routing_t* r, const void* saved, const void* codes, const void* scales) {
+    const int rc = check_shape(s);
+    if (rc != MOE_OK) return rc;
+    if (!r || !r->offsets || !aligned(r->offsets, 4)) return MOE_ERR_ARG;
+    if (s->T > 0 && (!saved || !codes || !scales)) return MOE_ERR_ARG;
+    return aligned(saved, 256) && aligned(codes, 16) && aligned(scales, 4) ? MOE_OK : MOE_ERR_ARG;
+}
+int check_mx(int64_t rows, int K) {
+    if (rows < 0 || rows >= (1ll << 31) || K < 8 || K > 1 << 16 || K % 8 != 0 || rows * K > (1ll << 36)) return MOE_ERR_SHAPE;
+    return MOE_OK;
+}
+bool bad_mx(const void* codes, const void* scales, bool any) { return (any && (!codes || !scales)) || !aligned(codes, 16) || !aligned(scales, 16); }
 
 struct SavedLayout {
     size_t gu, h, o, total;
@@ -443,6 +478,73 @@ int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, 
     if ((shape->T > 0 && !dlogits) || !aligned(dlogits, out_bf16 ? 2 : 4)) return MOE_ERR_ARG;
     return balance_backward_launch(*shape, logits, topk_idx, seq_offsets, *stats, topk_w, dtopk_w, dloss, dlogits, out_bf16,
                                    (hipStream_t)stream);
+}
+
+int moe_dispatch_forward(const moe_dispatch_shape_t* shape, const void* x, int64_t ldx, int32_t f32, const int32_t* row_of, void* xs, void* stream) {
+    int rc = check_dispatch_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_move(*shape, x, ldx, xs, f32, row_of);
+    if (rc != MOE_OK) return rc;
+    return dispatch_forward_launch(*shape, x, (size_t)ldx, f32, row_of, xs, (hipStream_t)stream);
+}
+
+int moe_dispatch_backward(const moe_dispatch_shape_t* shape, const void* dxs, int32_t f32, const int32_t* row_of, void* dx, void* stream) {
+    return moe_combine_forward(shape, dxs, f32, row_of, nullptr, dx, stream);
+}
+
+int moe_combine_forward(const moe_dispatch_shape_t* shape, const void* o, int32_t f32, const int32_t* row_of, const float* w, void* y, void* stream) {
+    int rc = check_dispatch_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_move(*shape, y, shape->d, o, f32, row_of);
+    if (rc != MOE_OK) return rc;
+    if (!aligned(w, 4)) return MOE_ERR_ARG;
+    return combine_forward_launch(*shape, o, f32, row_of, w, y, (hipStream_t)stream);
+}
+
+int moe_combine_backward(const moe_dispatch_shape_t* shape, const void* dy, int64_t lddy, const void* o, int32_t f32, const int32_t* row_of, const float* w,
+                         void* d_o, float* dw, void* stream) {
+    int rc = check_dispatch_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_move(*shape, dy, lddy, d_o, f32, row_of);
+    if (rc != MOE_OK) return rc;
+    if ((dw && shape->T > 0 && shape->rows > 0 && !o) || !aligned(o, 16) || !aligned(w, 4) || !aligned(dw, 4)) return MOE_ERR_ARG;
+    return combine_backward_launch(*shape, dy, (size_t)lddy, o, f32, row_of, w, d_o, dw, (hipStream_t)stream);
+}
+
+int moe_saved_pack(const moe_shape_t* shape, const moe_routing_t* routing, const void* saved, void* codes, void* scales, void* stream) {
+    const int rc = check_packed(shape, routing, saved, codes, scales);
+    if (rc != MOE_OK) return rc;
+    return saved_pack_launch(*shape, routing->offsets, (const char*)saved + saved_layout(*shape).gu, (uint8_t*)codes, (uint8_t*)scales, (hipStream_t)stream);
+}
+
+int moe_saved_unpack(const moe_shape_t* shape, const moe_routing_t* routing, const void* codes, const void* scales, void* saved, void* stream) {
+    const int rc = check_packed(shape, routing, saved, codes, scales);
+    if (rc != MOE_OK) return rc;
+    const SavedLayout L = saved_layout(*shape);
+    return saved_unpack_launch(*shape, routing->offsets, (const uint8_t*)codes, (const uint8_t*)scales, (char*)saved + L.gu, (char*)saved + L.h, (hipStream_t)stream);
+}
+
+int moe_mx_quantize(const void* x, int64_t ldx, int32_t f32, int64_t rows, int32_t K, void* codes, void* scales, void* stream) {
+    const int rc = check_mx(rows, K);
+    if (rc != MOE_OK) return rc;
+    if ((f32 != 0 && f32 != 1) || bad_mx(codes, scales, rows > 0)) return MOE_ERR_ARG;
+    if ((rows > 0 && (!x || ldx < K || ldx % 8 != 0 || ldx > (1ll << 40) / rows)) || !aligned(x, 16)) return MOE_ERR_ARG;
+    return mx_quantize_launch(x, (size_t)ldx, f32, rows, K, (uint8_t*)codes, (uint8_t*)scales, (hipStream_t)stream);
+}
+
+int moe_mx_quantize_weights(const void* w, int32_t experts, int32_t K, int32_t N, void* codes, void* scales, void* stream) {
+    if (experts < 1 || experts > kMaxExperts || N < 8 || N > 1 << 16 || N % 8 != 0) return MOE_ERR_SHAPE;
+    const int rc = check_mx((int64_t)experts * N, K);
+    if (rc != MOE_OK) return rc;
+    if (!w || !aligned(w, 16) || bad_mx(codes, scales, true)) return MOE_ERR_ARG;
+    return mx_quantize_weights_launch(w, experts, K, N, (uint8_t*)codes, (uint8_t*)scales, (hipStream_t)stream);
+}
+
+int moe_mx_values(const void* codes, const void* scales, int64_t rows, int32_t K, void* out, int32_t out_f32, void* stream) {
+    const int rc = check_mx(rows, K);
+    if (rc != MOE_OK) return rc;
+    if ((out_f32 != 0 && out_f32 != 1) || bad_mx(codes, scales, rows > 0) || (rows > 0 && !out) || !aligned(out, 16)) return MOE_ERR_ARG;
+    return mx_values_launch((const uint8_t*)codes, (const uint8_t*)scales, rows, K, out, out_f32, (hipStream_t)stream);
 }
 
 int moe_device_status(const void* ws, void* stream) {

@@ -8,6 +8,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <vector>
+
 #include "../../include/uniep_moe.h"
 
 namespace {
@@ -19,6 +21,15 @@ decltype(&moe_balance_forward) p_balance_forward;
 decltype(&moe_balance_backward) p_balance_backward;
 decltype(&moe_adapter_workspace_bytes) p_adapter_bytes;
 decltype(&moe_balance_workspace_bytes) p_balance_bytes;
+decltype(&moe_dispatch_forward) p_dispatch_forward;
+decltype(&moe_dispatch_backward) p_dispatch_backward;
+decltype(&moe_combine_forward) p_combine_forward;
+decltype(&moe_combine_backward) p_combine_backward;
+decltype(&moe_saved_pack) p_saved_pack;
+decltype(&moe_saved_unpack) p_saved_unpack;
+decltype(&moe_mx_quantize) p_mx_quantize;
+decltype(&moe_mx_quantize_weights) p_mx_quantize_weights;
+decltype(&moe_mx_values) p_mx_values;
 
 struct Refused {};   // a Python exception is set
 
@@ -57,9 +68,9 @@ struct On {
         return o == Py_None ? nullptr : dense(o, name, type, sizes);
     }
     // Rows of `width` that may be parts of wider ones; ld = elements from one to the next.
-    void* rows(PyObject* o, const char* name, int64_t n, int64_t width, int64_t* ld) const {
+    void* rows(PyObject* o, const char* name, int64_t n, int64_t width, int64_t* ld, at::ScalarType type = at::kBFloat16) const {
         const at::Tensor& t = tensor(o, name);
-        check(t, name, at::kBFloat16, {n, width});
+        check(t, name, type, {n, width});
         if (t.stride(1) != 1 && width > 1) refuse(name, "expected rows without gaps");
         *ld = n > 1 ? t.stride(0) : width;
         return t.data_ptr();
@@ -282,24 +293,217 @@ PyObject* balance_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+// bf16 or fp32, as the call's first tensor says
+bool is_f32(const On& on, const char* name) {
+    const auto type = on.first.scalar_type();
+    if (type != at::kFloat && type != at::kBFloat16) refuse(name, "expected bf16 or fp32");
+    return type == at::kFloat;
+}
+
+// shape, x, row_of, out, stream -> xs
+PyObject* dispatch_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 5, [&]() -> PyObject* {
+        const auto s = shape_at<moe_dispatch_shape_t>(v[0]);
+        const On on(v[1], "x");
+        const bool f32 = is_f32(on, "x");
+        const auto type = on.first.scalar_type();
+        int64_t ldx;
+        const void* x = on.rows(v[1], "x", s.T, s.d, &ldx, type);
+        const void* row_of = on.dense(v[2], "row_of", at::kInt, {s.T, s.k});
+        const at::Tensor out = on.output(v[3], "out", type, {s.rows, s.d});
+        void* const stream = stream_of(v[4]);
+        const int rc = call([&] { return p_dispatch_forward(&s, x, ldx, f32, (const int32_t*)row_of, out.data_ptr(), stream); });
+        return rc != MOE_OK ? code_of(rc) : wrapped(out);
+    });
+}
+
+// shape, rows, row_of, weights, out, stream -> tokens (weights None: ones, dispatch's gradient)
+PyObject* combine_forward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 6, [&]() -> PyObject* {
+        const auto s = shape_at<moe_dispatch_shape_t>(v[0]);
+        const On on(v[1], "rows");
+        const bool f32 = is_f32(on, "rows");
+        const auto type = on.first.scalar_type();
+        const void* rows = on.dense(v[1], "rows", type, {s.rows, s.d});
+        const void* row_of = on.dense(v[2], "row_of", at::kInt, {s.T, s.k});
+        const void* w = on.optional(v[3], "weights", at::kFloat, {s.T, s.k});
+        const at::Tensor out = on.output(v[4], "out", type, {s.T, s.d});
+        void* const stream = stream_of(v[5]);
+        const int rc = call([&] {
+            return w ? p_combine_forward(&s, rows, f32, (const int32_t*)row_of, (const float*)w, out.data_ptr(), stream)
+                     : p_dispatch_backward(&s, rows, f32, (const int32_t*)row_of, out.data_ptr(), stream);
+        });
+        return rc != MOE_OK ? code_of(rc) : wrapped(out);
+    });
+}
+
+// shape, dy, o, row_of, weights, do, dw, want dw, stream -> (do, dw or None)
+PyObject* combine_backward(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 9, [&]() -> PyObject* {
+        const auto s = shape_at<moe_dispatch_shape_t>(v[0]);
+        const On on(v[1], "dy");
+        const bool f32 = is_f32(on, "dy"), want = v[7] == Py_True;
+        const auto type = on.first.scalar_type();
+        int64_t lddy;
+        const void* dy = on.rows(v[1], "dy", s.T, s.d, &lddy, type);
+        const void* o = want ? on.dense(v[2], "o", type, {s.rows, s.d}) : nullptr;
+        const void* row_of = on.dense(v[3], "row_of", at::kInt, {s.T, s.k});
+        const void* w = on.optional(v[4], "weights", at::kFloat, {s.T, s.k});
+        const at::Tensor d_o = on.output(v[5], "do", type, {s.rows, s.d});
+        at::Tensor dw;
+        if (want) dw = on.output(v[6], "dw", at::kFloat, {s.T, s.k});
+        void* const stream = stream_of(v[8]);
+        const int rc = call([&] {
+            return p_combine_backward(&s, dy, lddy, o, f32, (const int32_t*)row_of, (const float*)w, d_o.data_ptr(), want ? (float*)dw.data_ptr() : nullptr, stream);
+        });
+        if (rc != MOE_OK) return code_of(rc);
+        if (want) return wrapped({d_o, dw});
+        PyObject* out = wrapped(d_o);
+        PyObject* pair = out ? PyTuple_Pack(2, out, Py_None) : nullptr;
+        Py_XDECREF(out);
+        return pair;
+    });
+}
+
+struct Stash {
+    moe_routing_t routing = {};
+    void* saved;
+    int64_t rows;
+    // offsets, saved
+    Stash(const On& on, const moe_shape_t& s, PyObject* const* v) {
+        rows = (int64_t)s.T * s.k;
+        routing.offsets = (const int32_t*)on.dense(v[0], "routing.offsets", at::kInt, {(int64_t)s.e_count + 1});
+        const at::Tensor& t = tensor(v[1], "saved");
+        on.here(t, "saved");
+        const int64_t need = (rows * 4 * s.I + 255) / 256 * 256 + rows * 2 * s.I;   // up to h's end
+        if (t.scalar_type() != at::kByte || !t.is_contiguous() || t.numel() < need) refuse("saved", "expected a stash of this shape");
+        saved = t.data_ptr();
+    }
+};
+
+// shape, offsets, saved, codes, scales, stream -> (codes, scales)
+PyObject* saved_pack(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 6, [&]() -> PyObject* {
+        const auto s = shape_at<moe_shape_t>(v[0]);
+        const On on(v[2], "saved");
+        const Stash in(on, s, v + 1);
+        const at::Tensor codes = on.output(v[3], "codes", at::kChar, {in.rows, 2 * (int64_t)s.I});
+        const at::Tensor scales = on.output(v[4], "scales", at::kByte, {in.rows, (int64_t)s.I / 16});
+        void* const stream = stream_of(v[5]);
+        const int rc = call([&] { return p_saved_pack(&s, &in.routing, in.saved, codes.data_ptr(), scales.data_ptr(), stream); });
+        return rc != MOE_OK ? code_of(rc) : wrapped({codes, scales});
+    });
+}
+
+// shape, offsets, saved, codes, scales, stream -> None
+PyObject* saved_unpack(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 6, [&]() -> PyObject* {
+        const auto s = shape_at<moe_shape_t>(v[0]);
+        const On on(v[2], "saved");
+        const Stash out(on, s, v + 1);
+        const void* codes = on.dense(v[3], "codes", at::kChar, {out.rows, 2 * (int64_t)s.I});
+        const void* scales = on.dense(v[4], "scales", at::kByte, {out.rows, (int64_t)s.I / 16});
+        void* const stream = stream_of(v[5]);
+        const int rc = call([&] { return p_saved_unpack(&s, &out.routing, codes, scales, out.saved, stream); });
+        if (rc != MOE_OK) return code_of(rc);
+        Py_RETURN_NONE;
+    });
+}
+
+int64_t padded(int64_t K) { return (K + 127) / 128 * 128; }
+
+// x, codes, scales, stream -> (codes, scales)
+PyObject* mx_quantize(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 4, [&]() -> PyObject* {
+        const On on(v[0], "x");
+        const bool f32 = is_f32(on, "x");
+        if (on.first.dim() != 2) refuse("x", "expected rows");
+        const int64_t rows = on.first.size(0), K = on.first.size(1);
+        int64_t ldx;
+        const void* x = on.rows(v[0], "x", rows, K, &ldx, on.first.scalar_type());
+        if (K < 1 || K > 1 << 16) return code_of(MOE_ERR_SHAPE);
+        const at::Tensor codes = on.output(v[1], "codes", at::kByte, {rows, padded(K) / 2}), scales = on.output(v[2], "scales", at::kByte, {rows, padded(K) / 32});
+        void* const stream = stream_of(v[3]);
+        const int rc = call([&] { return p_mx_quantize(x, ldx, f32, rows, (int32_t)K, codes.data_ptr(), scales.data_ptr(), stream); });
+        return rc != MOE_OK ? code_of(rc) : wrapped({codes, scales});
+    });
+}
+
+// w, codes, scales, stream -> (codes, scales)
+PyObject* mx_quantize_weights(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 4, [&]() -> PyObject* {
+        const On on(v[0], "w");
+        if (on.first.dim() != 3) refuse("w", "expected [experts, K, N]");
+        const int64_t E = on.first.size(0), K = on.first.size(1), N = on.first.size(2);
+        const void* w = on.dense(v[0], "w", at::kBFloat16, {E, K, N});
+        if (E < 1 || E > 1 << 16 || K < 1 || K > 1 << 16 || N < 1 || N > 1 << 16) return code_of(MOE_ERR_SHAPE);
+        const at::Tensor codes = on.output(v[1], "codes", at::kByte, {E, N, padded(K) / 2}), scales = on.output(v[2], "scales", at::kByte, {E, N, padded(K) / 32});
+        void* const stream = stream_of(v[3]);
+        const int rc = call([&] { return p_mx_quantize_weights(w, (int32_t)E, (int32_t)K, (int32_t)N, codes.data_ptr(), scales.data_ptr(), stream); });
+        return rc != MOE_OK ? code_of(rc) : wrapped({codes, scales});
+    });
+}
+
+// Sizes of codes and scales [..., K] but for the last
+std::vector<int64_t> leading(const On& on, PyObject* scales, int64_t K) {
+    const at::Tensor &c = on.first, &s = tensor(scales, "scales");
+    on.here(s, "scales");
+    if (c.scalar_type() != at::kByte || s.scalar_type() != at::kByte) refuse("codes", "expected bytes");
+    if (!c.is_contiguous() || !s.is_contiguous()) refuse("codes", "expected contiguous tensors");
+    if (K < 1 || c.dim() < 2 || c.dim() != s.dim() || c.size(-1) != padded(K) / 2 || s.size(-1) != padded(K) / 32) refuse("codes", "sizes");
+    std::vector<int64_t> sizes(c.sizes().begin(), c.sizes().end() - 1);
+    for (size_t i = 0; i < sizes.size(); ++i)
+        if (s.size((int64_t)i) != sizes[i]) refuse("scales", "sizes");
+    return sizes;
+}
+
+// codes, scales, K, fp32, out, stream -> values
+PyObject* mx_values(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 6, [&]() -> PyObject* {
+        const On on(v[0], "codes");
+        const int64_t K = PyLong_AsLongLong(v[2]);
+        if (PyErr_Occurred()) return nullptr;
+        if (K < 1 || K > 1 << 16) return code_of(MOE_ERR_SHAPE);
+        std::vector<int64_t> sizes = leading(on, v[1], K);
+        int64_t rows = 1;
+        for (int64_t m : sizes) rows *= m;
+        sizes.push_back(K);
+        const bool f32 = v[3] == Py_True;
+        const auto type = f32 ? at::kFloat : at::kBFloat16;
+        at::Tensor out;
+        if (v[4] == Py_None) {
+            out = made(on.first, type, sizes);
+        } else {
+            out = tensor(v[4], "out");
+            on.here(out, "out");
+            if (out.scalar_type() != type) refuse("out", "type");
+            if (out.sizes() != at::IntArrayRef(sizes) || !out.is_contiguous()) refuse("out", "sizes");
+        }
+        void* const stream = stream_of(v[5]);
+        const void *codes = on.first.data_ptr(), *scales = tensor(v[1], "scales").data_ptr();
+        const int rc = call([&] { return p_mx_values(codes, scales, rows, (int32_t)K, out.data_ptr(), f32, stream); });
+        return rc != MOE_OK ? code_of(rc) : wrapped(out);
+    });
+}
+
 // addresses of the library's functions, in the order of the pointers above
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
-    return guarded(n, 7, [&]() -> PyObject* {
-        void* f[7];
-        for (int i = 0; i < 7; ++i) f[i] = stream_of(v[i]);
-        p_adapter_plan = (decltype(p_adapter_plan))f[0];
-        p_adapter_forward = (decltype(p_adapter_forward))f[1];
-        p_adapter_backward = (decltype(p_adapter_backward))f[2];
-        p_balance_forward = (decltype(p_balance_forward))f[3];
-        p_balance_backward = (decltype(p_balance_backward))f[4];
-        p_adapter_bytes = (decltype(p_adapter_bytes))f[5];
-        p_balance_bytes = (decltype(p_balance_bytes))f[6];
+    return guarded(n, 16, [&]() -> PyObject* {
+        void* f[16];
+        for (int i = 0; i < 16; ++i) f[i] = stream_of(v[i]);
+        int i = 0;
+        auto take = [&](auto& p) { p = (std::decay_t<decltype(p)>)f[i++]; };
+        take(p_adapter_plan), take(p_adapter_forward), take(p_adapter_backward), take(p_balance_forward), take(p_balance_backward), take(p_adapter_bytes);
+        take(p_balance_bytes), take(p_dispatch_forward), take(p_dispatch_backward), take(p_combine_forward), take(p_combine_backward), take(p_saved_pack);
+        take(p_saved_unpack), take(p_mx_quantize), take(p_mx_quantize_weights), take(p_mx_values);
         Py_RETURN_NONE;
     });
 }
 
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {FAST(adapter_plan), FAST(adapter_forward), FAST(adapter_backward), FAST(balance_forward), FAST(balance_backward), FAST(bind),
+PyMethodDef methods[] = {FAST(adapter_plan), FAST(adapter_forward), FAST(adapter_backward), FAST(balance_forward), FAST(balance_backward), FAST(dispatch_forward),
+                         FAST(combine_forward), FAST(combine_backward), FAST(saved_pack), FAST(saved_unpack), FAST(mx_quantize), FAST(mx_quantize_weights),
+                         FAST(mx_values), FAST(bind),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
