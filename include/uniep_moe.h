@@ -407,6 +407,29 @@ int moe_mx_quantize_weights(const void* w, int32_t experts, int32_t K, int32_t N
 /* The values that codes and scales stand for, [rows,K] bf16 (exact but for scales beyond 2^125) or fp32. */
 int moe_mx_values(const void* codes, const void* scales, int64_t rows, int32_t K, void* out, int32_t out_f32, void* stream);
 
+/* Products of rows sorted by expert with their experts' weights, everything in 4 bits, fp32 accumulate; for serving: the weights have no gradient.
+ * Limits (MOE_ERR_SHAPE otherwise): 0 <= rows < 2^30, K and N multiples of 8 from 8 to 2^16, rows * max(K, N) <= 2^36, 1 <= experts <= 1024, experts * N * K <= 2^40. */
+typedef struct {
+    int32_t rows;      /* of the sorted buffers (A_cap) */
+    int32_t K, N;      /* inner and outer width */
+    int32_t experts;
+} moe_mx_shape_t;
+
+/* y[r] = a[src(r)] W_e^T for offsets[e] <= r < offsets[e+1]; rows at and beyond offsets[experts] are left as they were.
+ *   a_*      codes and scales of a_rows rows of K;  a_rows * K <= 2^36
+ *   perm     [rows] int32, as moe_route writes it: src(r) = perm[r] / k, below a_rows (values for rows of experts only; one that is out of range gives a row of
+ *            unspecified values); or NULL: src(r) = r, a_rows at least `rows`
+ *   w_*      codes and scales of [experts,N,K], as moe_mx_quantize_weights writes them
+ *   offsets  [experts+1] int32, ascending, as moe_route writes them
+ *   y        [rows,N] bf16, or fp32 with out_f32 = 1 */
+int moe_mx_product(const moe_mx_shape_t* shape, const void* a_codes, const void* a_scales, int64_t a_rows, const int32_t* perm, int32_t k, const void* w_codes,
+                   const void* w_scales, const int32_t* offsets, void* y, int32_t out_f32, void* stream);
+/* h[r] = silu(a[src(r)] Wg_e^T) * (a[src(r)] Wu_e^T), N = the experts' inner width.  Either
+ *   h                  [rows,N] bf16, or
+ *   h_codes, h_scales  the bf16 result in 4 bits, as moe_mx_quantize gives it (what the down projection takes), padding included */
+int moe_mx_gate_up(const moe_mx_shape_t* shape, const void* a_codes, const void* a_scales, int64_t a_rows, const int32_t* perm, int32_t k, const void* gate_codes,
+                   const void* gate_scales, const void* up_codes, const void* up_scales, const int32_t* offsets, void* h, void* h_codes, void* h_scales, void* stream);
+
 /* Synchronises `stream`, reads the status word a forward/backward call left in
  * its workspace and returns MOE_OK or MOE_ERR_DEVICE (test and debug aid; the
  * hot path never calls it). */

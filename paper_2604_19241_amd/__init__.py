@@ -14,7 +14,7 @@ from .binding import (  # noqa: F401
     AdapterPlan, BalanceStats, MoEAdapterShape, MoEBalanceShape, make_adapter_shape, make_balance_shape,
     moe_adapter_backward, moe_adapter_forward, moe_adapter_plan, moe_adapter_workspace_bytes,
     moe_balance_backward, moe_balance_forward, moe_balance_workspace_bytes,
-    MoEDispatchShape, MXTensor, PackedSaved, make_dispatch_shape,
+    MoEDispatchShape, MoEMXShape, MXTensor, PackedSaved, make_dispatch_shape, make_mx_shape,
     moe_combine_backward, moe_combine_forward, moe_dispatch_backward, moe_dispatch_forward,
-    moe_mx_quantize, moe_mx_quantize_weights, moe_mx_values, moe_saved_pack, moe_saved_unpack,
+    moe_mx_gate_up, moe_mx_product, moe_mx_quantize, moe_mx_quantize_weights, moe_mx_values, moe_saved_pack, moe_saved_unpack,
 )

@@ -29,7 +29,7 @@ EXPORTS = ("moe_workspace_bytes", "moe_backward_workspace_bytes", "moe_saved_lay
            "moe_perf_model_search", "moe_route_static", "moe_calibration_mfma", "moe_adapter_workspace_bytes", "moe_adapter_plan",
            "moe_adapter_forward", "moe_adapter_backward", "moe_balance_workspace_bytes", "moe_balance_forward", "moe_balance_backward",
            "moe_dispatch_forward", "moe_dispatch_backward", "moe_combine_forward", "moe_combine_backward", "moe_saved_pack", "moe_saved_unpack",
-           "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values")
+           "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values", "moe_mx_product", "moe_mx_gate_up")
 
 ROUTE_STATIC_SCRATCH_BYTES = 4 << 20   # MOE_ROUTE_STATIC_SCRATCH_BYTES
 
@@ -84,6 +84,8 @@ _ARGTYPES = {
     "moe_mx_quantize": [_P, _L, _I, _L, _I, _P, _P, _P],
     "moe_mx_quantize_weights": [_P, _I, _I, _I, _P, _P, _P],
     "moe_mx_values": [_P, _P, _L, _I, _P, _I, _P],
+    "moe_mx_product": [_P, _P, _P, _L, _P, _I, _P, _P, _P, _P, _I, _P],
+    "moe_mx_gate_up": [_P, _P, _P, _L, _P, _I] + [_P] * 9,
 }
 _lib = None
 
@@ -157,7 +159,8 @@ def _load_call():
         from . import _call as module
         names = ("moe_adapter_plan", "moe_adapter_forward", "moe_adapter_backward", "moe_balance_forward", "moe_balance_backward",
                  "moe_adapter_workspace_bytes", "moe_balance_workspace_bytes", "moe_dispatch_forward", "moe_dispatch_backward", "moe_combine_forward",
-                 "moe_combine_backward", "moe_saved_pack", "moe_saved_unpack", "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values")
+                 "moe_combine_backward", "moe_saved_pack", "moe_saved_unpack", "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values",
+                 "moe_mx_product", "moe_mx_gate_up")
         module.bind(*[ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names])
         _call = module
     return _call
@@ -628,6 +631,41 @@ def moe_mx_values(mx: MXTensor, out_dtype=torch.bfloat16, out: torch.Tensor | No
     if type(got) is int:
         _check(got, "moe_mx_values")
     return got
+
+
+class MoEMXShape(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "K", "N", "experts")]
+
+
+def make_mx_shape(rows, K, N, experts) -> MoEMXShape:
+    """Rows of the sorted buffers (T k), inner and outer width, experts."""
+    return MoEMXShape(rows, K, N, experts)
+
+
+def moe_mx_product(shape: MoEMXShape, a: MXTensor, w: MXTensor, offsets, perm=None, k: int = 1, out_dtype=torch.bfloat16,
+                   y: torch.Tensor | None = None) -> torch.Tensor:
+    """y[r] = a[src] w[e]^T for the rows offsets[e] <= r < offsets[e+1] of every expert: a [.., K], w [experts,N,K] as moe_mx_quantize_weights makes it; src = r, or
+    perm[r] // k with a routing's perm.  Rows behind the last expert's keep what y held (unspecified in a new one).  For serving: without a gradient."""
+    assert out_dtype is _F32 or out_dtype is _BF16
+    assert a.K == shape.K == w.K
+    call = _call or _load_call()
+    got = call.mx_product(_addressof(shape), a.codes, a.scales, w.codes, w.scales, offsets, perm, k, out_dtype is _F32, y, _raw_stream(a.codes))
+    if type(got) is int:
+        _check(got, "moe_mx_product")
+    return got
+
+
+def moe_mx_gate_up(shape: MoEMXShape, a: MXTensor, w_gate: MXTensor, w_up: MXTensor, offsets, perm=None, k: int = 1, quantize: bool = False,
+                   h: torch.Tensor | MXTensor | None = None) -> torch.Tensor | MXTensor:
+    """h[r] = silu(a[src] w_gate[e]^T) * (a[src] w_up[e]^T), rows as in moe_mx_product: bf16, or with quantize what moe_mx_quantize makes of that."""
+    assert a.K == shape.K == w_gate.K == w_up.K
+    call = _call or _load_call()
+    out, scales = (h.codes, h.scales) if quantize and h is not None else (h, None)
+    got = call.mx_gate_up(_addressof(shape), a.codes, a.scales, w_gate.codes, w_gate.scales, w_up.codes, w_up.scales, offsets, perm, k, bool(quantize), out, scales,
+                          _raw_stream(a.codes))
+    if type(got) is int:
+        _check(got, "moe_mx_gate_up")
+    return MXTensor(got[0], got[1], shape.N) if quantize else got
 
 
 # ---- analytical performance model and configuration search (host only) -------

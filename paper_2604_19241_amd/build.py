@@ -16,7 +16,7 @@ CSRC = PKG / "csrc"
 LIB = PKG / "libuniep_moe.so"
 CALL = PKG / "_call.so"                  # host side of the short calls (csrc/call.cpp)
 BUILD = PKG.parent / "_build"
-SOURCES = ["route.hip", "forward.hip", "backward.hip", "adapter.hip", "balance.hip", "move.hip", "saved.hip", "mx.hip", "api.hip", "perf_model.hip"]
+SOURCES = ["route.hip", "forward.hip", "backward.hip", "adapter.hip", "balance.hip", "move.hip", "saved.hip", "mx.hip", "mx_product.hip", "api.hip", "perf_model.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

@@ -52,6 +52,9 @@ int saved_unpack_launch(const moe_shape_t& s, const int32_t* offsets, const uint
 int mx_quantize_launch(const void* x, size_t ldx, int f32, int64_t rows, int K, uint8_t* codes, uint8_t* scales, hipStream_t st);
 int mx_values_launch(const uint8_t* codes, const uint8_t* scales, int64_t rows, int K, void* out, int f32, hipStream_t st);
 int mx_quantize_weights_launch(const void* w, int experts, int K, int N, uint8_t* codes, uint8_t* scales, hipStream_t st);
+int mx_product_launch(const moe_mx_shape_t& s, bool gate, const uint8_t* a_codes, const uint8_t* a_scales, int64_t a_rows, const int32_t* perm, int k,
+                      const uint8_t* w_codes, const uint8_t* w_scales, const uint8_t* u_codes, const uint8_t* u_scales, const int32_t* offsets, void* y, int f32,
+                      uint8_t* h_codes, uint8_t* h_scales, hipStream_t st);
 }  // namespace uniep
 
 using namespace uniep;
@@ -164,7 +167,23 @@ int check_mx(int64_t rows, int K) {
     if (rows < 0 || rows >= (1ll << 31) || K < 8 || K > 1 << 16 || K % 8 != 0 || rows * K > (1ll << 36)) return MOE_ERR_SHAPE;
     return MOE_OK;
 }
+int check_mx_shape(const moe_mx_shape_t* s) {
+    if (!s) return MOE_ERR_ARG;
+    if (s->rows < 0 || s->rows >= 1 << 30 || s->experts < 1 || s->experts > kMaxExperts) return MOE_ERR_SHAPE;
+    for (int width : {s->K, s->N})
+        if (width < 8 || width > 1 << 16 || width % 8 != 0 || (int64_t)s->rows * width > (1ll << 36)) return MOE_ERR_SHAPE;
+    return (int64_t)s->experts * s->N * s->K > (1ll << 40) ? MOE_ERR_SHAPE : MOE_OK;
+}
 bool bad_mx(const void* codes, const void* scales, bool any) { return (any && (!codes || !scales)) || !aligned(codes, 16) || !aligned(scales, 16); }
+
+// What both products have to be given; any: there are rows.
+int check_mx_operands(const moe_mx_shape_t& s, const void* a_codes, const void* a_scales, int64_t a_rows, const int32_t* perm, int k, const void* w_codes,
+                      const void* w_scales, const int32_t* offsets) {
+    if (a_rows < 0 || a_rows >= (1ll << 31) || a_rows * s.K > (1ll << 36)) return MOE_ERR_SHAPE;
+    if (k < 1 || (perm ? s.rows > 0 && a_rows == 0 : a_rows < s.rows)) return MOE_ERR_ARG;
+    if (bad_mx(a_codes, a_scales, s.rows > 0) || bad_mx(w_codes, w_scales, true) || !offsets) return MOE_ERR_ARG;
+    return aligned(perm, 4) && aligned(offsets, 4) ? MOE_OK : MOE_ERR_ARG;
+}
 
 struct SavedLayout {
     size_t gu, h, o, total;
@@ -545,6 +564,29 @@ int moe_mx_values(const void* codes, const void* scales, int64_t rows, int32_t K
     if (rc != MOE_OK) return rc;
     if ((out_f32 != 0 && out_f32 != 1) || bad_mx(codes, scales, rows > 0) || (rows > 0 && !out) || !aligned(out, 16)) return MOE_ERR_ARG;
     return mx_values_launch((const uint8_t*)codes, (const uint8_t*)scales, rows, K, out, out_f32, (hipStream_t)stream);
+}
+
+int moe_mx_product(const moe_mx_shape_t* shape, const void* a_codes, const void* a_scales, int64_t a_rows, const int32_t* perm, int32_t k, const void* w_codes,
+                   const void* w_scales, const int32_t* offsets, void* y, int32_t out_f32, void* stream) {
+    int rc = check_mx_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_mx_operands(*shape, a_codes, a_scales, a_rows, perm, k, w_codes, w_scales, offsets);
+    if (rc != MOE_OK) return rc;
+    if ((out_f32 != 0 && out_f32 != 1) || (shape->rows > 0 && !y) || !aligned(y, 16)) return MOE_ERR_ARG;
+    return mx_product_launch(*shape, false, (const uint8_t*)a_codes, (const uint8_t*)a_scales, a_rows, perm, k, (const uint8_t*)w_codes, (const uint8_t*)w_scales,
+                             nullptr, nullptr, offsets, y, out_f32, nullptr, nullptr, (hipStream_t)stream);
+}
+
+int moe_mx_gate_up(const moe_mx_shape_t* shape, const void* a_codes, const void* a_scales, int64_t a_rows, const int32_t* perm, int32_t k, const void* gate_codes,
+                   const void* gate_scales, const void* up_codes, const void* up_scales, const int32_t* offsets, void* h, void* h_codes, void* h_scales, void* stream) {
+    int rc = check_mx_shape(shape);
+    if (rc != MOE_OK) return rc;
+    rc = check_mx_operands(*shape, a_codes, a_scales, a_rows, perm, k, gate_codes, gate_scales, offsets);
+    if (rc != MOE_OK) return rc;
+    if (bad_mx(up_codes, up_scales, true) || !aligned(h, 16) || bad_mx(h_codes, h_scales, false)) return MOE_ERR_ARG;
+    if ((h && (h_codes || h_scales)) || (!h_codes != !h_scales) || (shape->rows > 0 && !h && !h_codes)) return MOE_ERR_ARG;
+    return mx_product_launch(*shape, true, (const uint8_t*)a_codes, (const uint8_t*)a_scales, a_rows, perm, k, (const uint8_t*)gate_codes, (const uint8_t*)gate_scales,
+                             (const uint8_t*)up_codes, (const uint8_t*)up_scales, offsets, h, 0, (uint8_t*)h_codes, (uint8_t*)h_scales, (hipStream_t)stream);
 }
 
 int moe_device_status(const void* ws, void* stream) {

@@ -5,6 +5,7 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/DeviceGuard.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -30,6 +31,8 @@ decltype(&moe_saved_unpack) p_saved_unpack;
 decltype(&moe_mx_quantize) p_mx_quantize;
 decltype(&moe_mx_quantize_weights) p_mx_quantize_weights;
 decltype(&moe_mx_values) p_mx_values;
+decltype(&moe_mx_product) p_mx_product;
+decltype(&moe_mx_gate_up) p_mx_gate_up;
 
 struct Refused {};   // a Python exception is set
 
@@ -48,7 +51,12 @@ at::Tensor made(const at::Tensor& like, at::ScalarType type, at::IntArrayRef siz
 // sizes that are asked for.
 struct On {
     const at::Tensor& first;
-    On(PyObject* o, const char* name) : first(tensor(o, name)) { here(first, name); }
+    c10::OptionalDeviceGuard current;   // its GPU is the current one during the call, where there are several
+    On(PyObject* o, const char* name) : first(tensor(o, name)) {
+        here(first, name);
+        static const bool several = c10::impl::getDeviceGuardImpl(c10::DeviceType::CUDA)->deviceCount() > 1;
+        if (several) current.reset_device(first.device());
+    }
     void here(const at::Tensor& t, const char* name) const {
         if (!t.is_cuda()) refuse(name, "expected a tensor on the GPU");
         if (t.get_device() != first.get_device()) refuse(name, "on another GPU than the call's other tensors");
@@ -486,16 +494,89 @@ PyObject* mx_values(PyObject*, PyObject* const* v, Py_ssize_t n) {
     });
 }
 
+struct MxOperand {
+    void *codes, *scales;
+    // codes and scales of `sizes` rows, of K values each
+    MxOperand(const On& on, PyObject* const* v, std::initializer_list<int64_t> sizes, int64_t K) {
+        std::vector<int64_t> c(sizes), s(sizes);
+        c.push_back(padded(K) / 2), s.push_back(padded(K) / 32);
+        codes = checked(on, v[0], "codes", c);
+        scales = checked(on, v[1], "scales", s);
+    }
+    static void* checked(const On& on, PyObject* o, const char* name, const std::vector<int64_t>& sizes) {
+        const at::Tensor& t = tensor(o, name);
+        on.here(t, name);
+        if (t.scalar_type() != at::kByte) refuse(name, "type");
+        if (t.sizes() != at::IntArrayRef(sizes)) refuse(name, "sizes");
+        if (!t.is_contiguous()) refuse(name, "expected a contiguous tensor");
+        return t.data_ptr();
+    }
+};
+int32_t whole(PyObject* o) {
+    const long v = PyLong_AsLong(o);
+    if (PyErr_Occurred()) throw Refused{};
+    return v < INT32_MIN || v > INT32_MAX ? 0 : (int32_t)v;
+}
+
+// shape, a's codes and scales, w's, offsets, perm, k, fp32, y, stream -> y
+PyObject* mx_product(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 11, [&]() -> PyObject* {
+        const auto s = shape_at<moe_mx_shape_t>(v[0]);
+        const On on(v[1], "codes");
+        const int64_t a_rows = on.first.dim() > 0 ? on.first.size(0) : 0;
+        const MxOperand a(on, v + 1, {a_rows}, s.K), w(on, v + 3, {s.experts, s.N}, s.K);
+        const int32_t* offsets = (const int32_t*)on.dense(v[5], "offsets", at::kInt, {(int64_t)s.experts + 1});
+        const int32_t* perm = (const int32_t*)on.optional(v[6], "perm", at::kInt, {s.rows});
+        const int32_t k = whole(v[7]);
+        const bool f32 = v[8] == Py_True;
+        const at::Tensor y = on.output(v[9], "y", f32 ? at::kFloat : at::kBFloat16, {s.rows, s.N});
+        void* const stream = stream_of(v[10]);
+        void* const out = y.data_ptr();
+        const int rc = call([&] { return p_mx_product(&s, a.codes, a.scales, a_rows, perm, k, w.codes, w.scales, offsets, out, f32, stream); });
+        return rc != MOE_OK ? code_of(rc) : wrapped(y);
+    });
+}
+
+// shape, a's codes and scales, the gate's, up's, offsets, perm, k, quantize, h or codes, scales, stream -> h or (codes, scales)
+PyObject* mx_gate_up(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 14, [&]() -> PyObject* {
+        const auto s = shape_at<moe_mx_shape_t>(v[0]);
+        const On on(v[1], "codes");
+        const int64_t a_rows = on.first.dim() > 0 ? on.first.size(0) : 0;
+        const MxOperand a(on, v + 1, {a_rows}, s.K), g(on, v + 3, {s.experts, s.N}, s.K), u(on, v + 5, {s.experts, s.N}, s.K);
+        const int32_t* offsets = (const int32_t*)on.dense(v[7], "offsets", at::kInt, {(int64_t)s.experts + 1});
+        const int32_t* perm = (const int32_t*)on.optional(v[8], "perm", at::kInt, {s.rows});
+        const int32_t k = whole(v[9]);
+        const bool quantize = v[10] == Py_True;
+        at::Tensor h, scales;
+        if (quantize) {
+            h = on.output(v[11], "h codes", at::kByte, {s.rows, padded(s.N) / 2});
+            scales = on.output(v[12], "h scales", at::kByte, {s.rows, padded(s.N) / 32});
+        } else {
+            h = on.output(v[11], "h", at::kBFloat16, {s.rows, s.N});
+        }
+        void* const stream = stream_of(v[13]);
+        void *const out = h.data_ptr(), *const out_scales = quantize ? scales.data_ptr() : nullptr;
+        const int rc = call([&] {
+            return p_mx_gate_up(&s, a.codes, a.scales, a_rows, perm, k, g.codes, g.scales, u.codes, u.scales, offsets, quantize ? nullptr : out, quantize ? out : nullptr,
+                                out_scales, stream);
+        });
+        if (rc != MOE_OK) return code_of(rc);
+        return quantize ? wrapped({h, scales}) : wrapped(h);
+    });
+}
+
 // addresses of the library's functions, in the order of the pointers above
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
-    return guarded(n, 16, [&]() -> PyObject* {
-        void* f[16];
-        for (int i = 0; i < 16; ++i) f[i] = stream_of(v[i]);
+    return guarded(n, 18, [&]() -> PyObject* {
+        void* f[18];
+        for (int i = 0; i < 18; ++i) f[i] = stream_of(v[i]);
         int i = 0;
         auto take = [&](auto& p) { p = (std::decay_t<decltype(p)>)f[i++]; };
         take(p_adapter_plan), take(p_adapter_forward), take(p_adapter_backward), take(p_balance_forward), take(p_balance_backward), take(p_adapter_bytes);
         take(p_balance_bytes), take(p_dispatch_forward), take(p_dispatch_backward), take(p_combine_forward), take(p_combine_backward), take(p_saved_pack);
         take(p_saved_unpack), take(p_mx_quantize), take(p_mx_quantize_weights), take(p_mx_values);
+        take(p_mx_product), take(p_mx_gate_up);
         Py_RETURN_NONE;
     });
 }
@@ -503,7 +584,7 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(adapter_plan), FAST(adapter_forward), FAST(adapter_backward), FAST(balance_forward), FAST(balance_backward), FAST(dispatch_forward),
                          FAST(combine_forward), FAST(combine_backward), FAST(saved_pack), FAST(saved_unpack), FAST(mx_quantize), FAST(mx_quantize_weights),
-                         FAST(mx_values), FAST(bind),
+                         FAST(mx_values), FAST(mx_product), FAST(mx_gate_up), FAST(bind),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -96,6 +96,45 @@ def test_arguments_of_4_bits(lib):
     assert lib.moe_mx_quantize(None, 64, 0, 0, 64, None, None, None) == b.MOE_OK and lib.moe_mx_values(None, None, 0, 64, None, 0, None) == b.MOE_OK
 
 
+GOOD = dict(rows=100, K=64, N=72, experts=4)
+
+
+def product_calls(lib, s, **kw):
+    a = dict(a=FAKE, sc=FAKE, a_rows=100, perm=None, k=1, w=FAKE, ws=FAKE, u=FAKE, us=FAKE, offsets=FAKE, y=FAKE, f32=0, hc=None, hs=None)
+    a.update(kw)
+    r = ctypes.byref(s) if s else None
+    head = (r, a["a"], a["sc"], a["a_rows"], a["perm"], a["k"], a["w"], a["ws"])
+    return {"product": lambda: lib.moe_mx_product(*head, a["offsets"], a["y"], a["f32"], None),
+            "gate_up": lambda: lib.moe_mx_gate_up(*head, a["u"], a["us"], a["offsets"], a["y"], a["hc"], a["hs"], None)}
+
+
+@pytest.mark.parametrize("kw", [dict(rows=-1), dict(rows=1 << 30), dict(K=0), dict(K=60), dict(K=(1 << 16) + 8), dict(N=4), dict(N=73), dict(N=(1 << 16) + 8), dict(experts=0), dict(experts=1025),
+                                dict(rows=1 << 21, K=1 << 16), dict(rows=1 << 21, N=1 << 16), dict(experts=1024, K=1 << 16, N=1 << 16)])
+def test_shapes_outside_the_limits_of_the_products(lib, kw):
+    s = moe.make_mx_shape(**(GOOD | kw))
+    assert all(call() == SHAPE for call in product_calls(lib, s, a_rows=1 << 22).values())
+
+
+def test_arguments_of_the_products(lib):
+    assert ctypes.sizeof(b.MoEMXShape) == 16
+    s = moe.make_mx_shape(**GOOD)
+    assert all(call() == ARG for call in product_calls(lib, None).values())
+    for kw in (dict(a=None), dict(a=ODD), dict(sc=None), dict(sc=ODD), dict(w=None), dict(w=ODD), dict(ws=None), dict(ws=ODD), dict(offsets=None), dict(offsets=0x1002), dict(y=None), dict(y=ODD),
+               dict(k=0), dict(k=-1), dict(a_rows=99), dict(perm=FAKE, a_rows=0), dict(perm=0x1002)):
+        for name, call in product_calls(lib, s, **kw).items():
+            assert call() == ARG, (name, kw)
+    for kw in (dict(a_rows=-1), dict(a_rows=1 << 31)):
+        assert all(call() == SHAPE for call in product_calls(lib, s, **kw).values()), kw
+    assert product_calls(lib, s, f32=2)["product"]() == ARG
+    for kw in (dict(u=None), dict(u=ODD), dict(us=None), dict(us=ODD), dict(hc=FAKE, hs=FAKE), dict(y=None, hc=FAKE), dict(y=None, hs=FAKE), dict(y=None, hc=ODD, hs=FAKE), dict(y=None, hc=FAKE, hs=ODD)):
+        assert product_calls(lib, s, **kw)["gate_up"]() == ARG, kw
+    none = moe.make_mx_shape(**(GOOD | dict(rows=0)))
+    assert all(call() == b.MOE_OK for call in product_calls(lib, none, a=None, s=None, a_rows=0, y=None).values())   # nothing to do
+    q = moe.MXTensor(torch.zeros((4, 64), dtype=U8), torch.zeros((4, 4), dtype=U8), 64)
+    with pytest.raises(AssertionError):
+        moe.moe_mx_product(moe.make_mx_shape(4, 128, 8, 1), q, q, torch.zeros(2, dtype=I32))   # another K
+
+
 def gpu(dtype, *sizes, device="cuda:0"):
     return NoMemory(dtype, sizes, device)
 
@@ -108,6 +147,11 @@ def calls():
     layer = moe.make_shape(T, 64, 8, k, 64)
     n = moe.alloc_saved(layer, "cpu").numel()
     packed = {"codes": (I8, (T * k, 128)), "scales": (U8, (T * k, 4))}
+    mxs = moe.make_mx_shape(**GOOD)
+
+    def operand(name, *sizes):
+        return {name: (U8, (*sizes, 64)), name + "_scales": (U8, (*sizes, 4))}
+
     mxt = {"codes": (U8, (10, 64)), "scales": (U8, (10, 4))}
     return [
         (call.dispatch_forward, [move], {"x": (BF, (T, d)), "row_of": (I32, (T, k)), "out": (BF, (rows, d)), "stream": 0}),
@@ -119,6 +163,11 @@ def calls():
         (call.saved_unpack, [layer], {"offsets": (I32, (9,)), "saved": (U8, (n,))} | packed | {"stream": 0}),
         (call.mx_quantize, [], {"x": (BF, (10, 72))} | mxt | {"stream": 0}),
         (call.mx_quantize_weights, [], {"w": (BF, (2, 72, 5 * 8)), "codes": (U8, (2, 40, 64)), "scales": (U8, (2, 40, 4)), "stream": 0}),
+        (call.mx_product, [mxs], operand("a", 100) | operand("w", 4, 72) | {"offsets": (I32, (5,)), "perm": (I32, (100,)), "k": 2, "f32": False, "y": (BF, (100, 72)), "stream": 0}),
+        (call.mx_gate_up, [mxs], operand("a", 30) | operand("g", 4, 72) | operand("u", 4, 72) | {"offsets": (I32, (5,)), "perm": (I32, (100,)), "k": 2, "q": True,
+                                                                                               "h": (U8, (100, 64)), "hs": (U8, (100, 4)), "stream": 0}),
+        (call.mx_gate_up, [mxs], operand("a", 100) | operand("g", 4, 72) | operand("u", 4, 72) | {"offsets": (I32, (5,)), "perm": None, "k": 1, "q": False, "h": (BF, (100, 72)),
+                                                                                                "none": None, "stream": 0}),
         (call.mx_values, [], mxt | {"K": 72, "f32": False, "out": (BF, (10, 72)), "stream": 0}),
     ]
 
