@@ -129,7 +129,7 @@ def test_arguments_of_the_products(lib):
     for kw in (dict(u=None), dict(u=ODD), dict(us=None), dict(us=ODD), dict(hc=FAKE, hs=FAKE), dict(y=None, hc=FAKE), dict(y=None, hs=FAKE), dict(y=None, hc=ODD, hs=FAKE), dict(y=None, hc=FAKE, hs=ODD)):
         assert product_calls(lib, s, **kw)["gate_up"]() == ARG, kw
     none = moe.make_mx_shape(**(GOOD | dict(rows=0)))
-    assert all(call() == b.MOE_OK for call in product_calls(lib, none, a=None, s=None, a_rows=0, y=None).values())   # nothing to do
+    assert all(call() == b.MOE_OK for call in product_calls(lib, none, a=None, sc=None, a_rows=0, y=None).values())   # nothing to do
     q = moe.MXTensor(torch.zeros((4, 64), dtype=U8), torch.zeros((4, 4), dtype=U8), 64)
     with pytest.raises(AssertionError):
         moe.moe_mx_product(moe.make_mx_shape(4, 128, 8, 1), q, q, torch.zeros(2, dtype=I32))   # another K
