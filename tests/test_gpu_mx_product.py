@@ -119,6 +119,24 @@ def test_experts_of_any_number_and_size(counts):
     check_gate_up(make(counts, 384, N, tokens=30, k=4, pair=True))
 
 
+@pytest.mark.parametrize("K,N", [(1280, 256), (1288, 264), (1408, 520), (2048, 136), (1544, 40), (4096, 128)])
+@pytest.mark.parametrize("counts", [[300, 5, 0, 257, 256, 64, 33, 1], [1000], [0, 97, 0, 230, 1], [191, 193, 512, 31, 224], [100] * 70])
+def test_many_rows_and_long_reductions(counts, K, N):
+    """Large tiles: from 96 rows an expert and 1280 values on; an odd and an even number of 128 values."""
+    say(f"[mx product] {len(counts)} experts, {sum(counts)} rows, {K} {N}")
+    check_product(make(counts, K, N, spare=3))
+    check_gate_up(make(counts, K, N, tokens=77, k=2, pair=True))
+
+
+@pytest.mark.parametrize("counts", [[16] * 12, [16] * 11 + [17], [3, 9, 0, 16], [20, 4, 0, 31], [32, 33]])
+@pytest.mark.parametrize("K,N", [(4096, 264), (4224, 1000), (512, 72)])
+def test_few_rows(counts, K, N):
+    """Narrow tiles, for all experts or for some: by the rows of the largest, the reduction and how many wide ones there would be."""
+    say(f"[mx product] {counts} {K} {N}")
+    check_product(make(counts, K, N, tokens=11, k=3))
+    check_gate_up(make(counts, K, N, spare=1, pair=True))
+
+
 @pytest.mark.parametrize("T,K,N,E,k,e_start,e_count", [(1, 768, 2048, 128, 8, 0, 128), (37, 7168, 256, 256, 8, 32, 32), (300, 512, 1024, 8, 2, 0, 8), (2000, 1024, 384, 128, 6, 0, 128)])
 def test_with_a_routing(T, K, N, E, k, e_start, e_count):
     say(f"[mx product] {T} {K} {N} {E} {k}")
