@@ -160,7 +160,7 @@ def _load_call():
         names = ("moe_adapter_plan", "moe_adapter_forward", "moe_adapter_backward", "moe_balance_forward", "moe_balance_backward",
                  "moe_adapter_workspace_bytes", "moe_balance_workspace_bytes", "moe_dispatch_forward", "moe_dispatch_backward", "moe_combine_forward",
                  "moe_combine_backward", "moe_saved_pack", "moe_saved_unpack", "moe_mx_quantize", "moe_mx_quantize_weights", "moe_mx_values",
-                 "moe_mx_product", "moe_mx_gate_up")
+                 "moe_mx_product", "moe_mx_gate_up", "moe_saved_layout")
         module.bind(*[ctypes.cast(getattr(lib, n), ctypes.c_void_p).value for n in names])
         _call = module
     return _call
@@ -389,7 +389,13 @@ def alloc_saved(shape: MoEShape, device) -> torch.Tensor:
 
 def saved_views(shape: MoEShape, saved: torch.Tensor) -> dict:
     """bf16 views of the stash: gu [A_cap,2I], h [A_cap,I], o [A_cap,d]."""
-    L = moe_saved_layout(shape)
+    call = _call or _load_call()
+    got = call.saved_views(_addressof(shape), saved)
+    if type(got) is int:
+        _check(got, "moe_saved_layout")
+    if got is not None:
+        return dict(zip(("gu", "h", "o"), got))
+    L = moe_saved_layout(shape)   # a buffer of another kind: torch says what is wrong with it
     A = shape.T * shape.k
 
     def view(off, cols):

@@ -26,6 +26,7 @@ decltype(&moe_dispatch_forward) p_dispatch_forward;
 decltype(&moe_dispatch_backward) p_dispatch_backward;
 decltype(&moe_combine_forward) p_combine_forward;
 decltype(&moe_combine_backward) p_combine_backward;
+decltype(&moe_saved_layout) p_saved_layout;
 decltype(&moe_saved_pack) p_saved_pack;
 decltype(&moe_saved_unpack) p_saved_unpack;
 decltype(&moe_mx_quantize) p_mx_quantize;
@@ -389,6 +390,24 @@ struct Stash {
     }
 };
 
+// shape, saved -> bf16 views of gu [A,2I], h [A,I], o [A,d] in the stash's bytes, A = T k; None where they do not fit
+PyObject* saved_views(PyObject*, PyObject* const* v, Py_ssize_t n) {
+    return guarded(n, 2, [&]() -> PyObject* {
+        const auto s = shape_at<moe_shape_t>(v[0]);
+        const at::Tensor& t = tensor(v[1], "saved");
+        size_t at[3];
+        const int rc = p_saved_layout(&s, at, at + 1, at + 2);
+        if (rc != MOE_OK) return code_of(rc);
+        const int64_t rows = (int64_t)s.T * s.k, cols[3] = {2 * (int64_t)s.I, s.I, s.d};
+        if (t.scalar_type() != at::kByte || t.dim() != 1 || !t.is_contiguous() || t.numel() % 2 != 0 || t.storage_offset() % 2 != 0 ||
+            t.numel() < (int64_t)at[2] + rows * cols[2] * 2)
+            Py_RETURN_NONE;
+        const at::Tensor flat = t.view(at::kBFloat16);
+        auto view = [&](int i) { return flat.as_strided({rows, cols[i]}, {cols[i], 1}, flat.storage_offset() + (int64_t)at[i] / 2); };
+        return wrapped({view(0), view(1), view(2)});
+    });
+}
+
 // shape, offsets, saved, codes, scales, stream -> (codes, scales)
 PyObject* saved_pack(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return guarded(n, 6, [&]() -> PyObject* {
@@ -568,15 +587,15 @@ PyObject* mx_gate_up(PyObject*, PyObject* const* v, Py_ssize_t n) {
 
 // addresses of the library's functions, in the order of the pointers above
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
-    return guarded(n, 18, [&]() -> PyObject* {
-        void* f[18];
-        for (int i = 0; i < 18; ++i) f[i] = stream_of(v[i]);
+    return guarded(n, 19, [&]() -> PyObject* {
+        void* f[19];
+        for (int i = 0; i < 19; ++i) f[i] = stream_of(v[i]);
         int i = 0;
         auto take = [&](auto& p) { p = (std::decay_t<decltype(p)>)f[i++]; };
         take(p_adapter_plan), take(p_adapter_forward), take(p_adapter_backward), take(p_balance_forward), take(p_balance_backward), take(p_adapter_bytes);
         take(p_balance_bytes), take(p_dispatch_forward), take(p_dispatch_backward), take(p_combine_forward), take(p_combine_backward), take(p_saved_pack);
         take(p_saved_unpack), take(p_mx_quantize), take(p_mx_quantize_weights), take(p_mx_values);
-        take(p_mx_product), take(p_mx_gate_up);
+        take(p_mx_product), take(p_mx_gate_up), take(p_saved_layout);
         Py_RETURN_NONE;
     });
 }
@@ -584,7 +603,7 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 #define FAST(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(adapter_plan), FAST(adapter_forward), FAST(adapter_backward), FAST(balance_forward), FAST(balance_backward), FAST(dispatch_forward),
                          FAST(combine_forward), FAST(combine_backward), FAST(saved_pack), FAST(saved_unpack), FAST(mx_quantize), FAST(mx_quantize_weights),
-                         FAST(mx_values), FAST(mx_product), FAST(mx_gate_up), FAST(bind),
+                         FAST(mx_values), FAST(mx_product), FAST(mx_gate_up), FAST(saved_views), FAST(bind),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_call", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
