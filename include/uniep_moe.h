@@ -416,7 +416,7 @@ typedef struct {
 } moe_mx_shape_t;
 
 /* y[r] = a[src(r)] W_e^T for offsets[e] <= r < offsets[e+1]; rows at and beyond offsets[experts] are left as they were.
- *   a_*      codes and scales of a_rows rows of K;  a_rows * K <= 2^36
+ *   a_*      codes and scales of a_rows rows of K;  a_rows < 2^31, a_rows * K' <= 2^36 (MOE_ERR_SHAPE otherwise)
  *   perm     [rows] int32, as moe_route writes it: src(r) = perm[r] / k, below a_rows (values for rows of experts only; one that is out of range gives a row of
  *            unspecified values); or NULL: src(r) = r, a_rows at least `rows`
  *   w_*      codes and scales of [experts,N,K], as moe_mx_quantize_weights writes them

@@ -179,7 +179,7 @@ bool bad_mx(const void* codes, const void* scales, bool any) { return (any && (!
 // What both products have to be given; any: there are rows.
 int check_mx_operands(const moe_mx_shape_t& s, const void* a_codes, const void* a_scales, int64_t a_rows, const int32_t* perm, int k, const void* w_codes,
                       const void* w_scales, const int32_t* offsets) {
-    if (a_rows < 0 || a_rows >= (1ll << 31) || a_rows * s.K > (1ll << 36)) return MOE_ERR_SHAPE;
+    if (a_rows < 0 || a_rows >= (1ll << 31) || a_rows * ((s.K + 127) / 128 * 128) > (1ll << 36)) return MOE_ERR_SHAPE;   // (a row's scales begin below 2^32)
     if (k < 1 || (perm ? s.rows > 0 && a_rows == 0 : a_rows < s.rows)) return MOE_ERR_ARG;
     if (bad_mx(a_codes, a_scales, s.rows > 0) || bad_mx(w_codes, w_scales, true) || !offsets) return MOE_ERR_ARG;
     return aligned(perm, 4) && aligned(offsets, 4) ? MOE_OK : MOE_ERR_ARG;

@@ -123,7 +123,7 @@ def test_arguments_of_the_products(lib):
                dict(k=0), dict(k=-1), dict(a_rows=99), dict(perm=FAKE, a_rows=0), dict(perm=0x1002)):
         for name, call in product_calls(lib, s, **kw).items():
             assert call() == ARG, (name, kw)
-    for kw in (dict(a_rows=-1), dict(a_rows=1 << 31)):
+    for kw in (dict(a_rows=-1), dict(a_rows=1 << 31), dict(a_rows=(1 << 29) + 1)):
         assert all(call() == SHAPE for call in product_calls(lib, s, **kw).values()), kw
     assert product_calls(lib, s, f32=2)["product"]() == ARG
     for kw in (dict(u=None), dict(u=ODD), dict(us=None), dict(us=ODD), dict(hc=FAKE, hs=FAKE), dict(y=None, hc=FAKE), dict(y=None, hs=FAKE), dict(y=None, hc=ODD, hs=FAKE), dict(y=None, hc=FAKE, hs=ODD)):
