@@ -22,7 +22,7 @@ struct SavedParams {
     uint8_t* scales;          // [rows][2 I / 32]
 };
 constexpr int kSavedThreads = 256;
-constexpr int kSavedUnits = 4;   // of 8 values, a thread
+constexpr int kSavedUnits = 4;   // of 8 values, a thread (65536 rows of 768 packed and unpacked: 2 118 us, 4 119, 8 124; 1542 of 1408 12.2, 12.1, 12.9)
 
 __device__ __forceinline__ uint32_t saved_rows(const SavedParams& p) { return (uint32_t)min((int64_t)max(p.offsets[p.experts], 0), (int64_t)p.rows); }
 
