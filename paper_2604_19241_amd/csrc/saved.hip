@@ -2,10 +2,10 @@
 // h = silu(G) U is made again.  The stash's third part, the experts' outputs, is not read by the backward pass and not kept.
 //
 // 2.06 I bytes a row instead of the stash's 6 I + 2 d, so that the layers of a model can share one stash.  Both directions are copies that change the type:
-// they are bound by memory, and what a lane computes for its 16 bytes hides behind it.
+// they are bound by memory, and what a lane computes for its 16 bytes hides behind it.  65536 rows of 768: packed in 48 us (6.4 TB/s of 305 MB), unpacked in 70 (5.8 TB/s of 406 MB).
 //
 // Eight bits of an integer, not of a floating-point number with three bits of mantissa: among 32 values of alike size the step of 2^-6 of the largest's
-// power of two is closer for all but the smallest, whose errors weigh little (values from a normal distribution: 0.8 % of their norm, e4m3 2.6 %).
+// power of two is closer for all but the smallest, whose errors weigh little (values from a normal distribution: 0.9 % of their norm, e4m3 with the same exponents 2.9 %).
 #include "mma.hpp"
 #include "mx.hpp"
 
