@@ -362,7 +362,7 @@ int moe_balance_backward(const moe_balance_shape_t* shape, const float* logits, 
  *   combine   y[t] = sum_j w[t,j] o[row(t,j)]        its gradient  do[row(t,j)] = w[t,j] dy[t],  dw[t,j] = <dy[t], o[row(t,j)]>
  * Slots whose row is outside [0, rows) have none: they are not read, not written and add nothing (dw = 0).  Every row may stand in the table once at most: two slots
  * that name one row leave some of its columns from either token.  Rows that no slot names are left as they were.  Sums are fp32 in the order of the slots, rounded once; the results are
- * the same bits on every run.  All activations of a call have one type, bf16 or (f32 = 1) fp32.
+ * the same bits on every run.  All activations of a call have one type, bf16 or (f32 = 1) fp32.  Here and in the calls below, what is written may not overlap what is read.
  * Limits (MOE_ERR_SHAPE otherwise): 0 <= T, 1 <= k <= 16, T * k < 2^30, d a multiple of 8 from 8 to 2^20, T * d <= 2^38, 0 <= rows. */
 typedef struct {
     int32_t T;      /* tokens */
