@@ -406,7 +406,7 @@ constexpr int kBigImage = 256 * 128, kBigStage = 2 * kBigImage;
 constexpr int kBigScales = 2 * kBigStage;
 constexpr int kBigSmem = kBigScales + 512 * 32;
 static_assert(kBigSmem <= 160 * 1024, "");
-constexpr int kBigStages = 10, kBigRows = 96;   // see mx_product_launch
+constexpr int kBigRows = 96;   // see mx_large
 constexpr int kBigRequests = 8;   // of a wave, a stage, without the scales
 
 // A DMA instruction fills 8 rows of an image, of codes and of scales; wave w moves rows 32 w .. + 31 and as many columns (gate_up: of the gate where w is even).
@@ -912,6 +912,25 @@ int mx_launch(K kernel, int threads, int smem, int (&known)[kMaxDevices], int64_
     return hipGetLastError() == hipSuccess ? MOE_OK : MOE_ERR_HIP;
 }
 int g_resident[4][kMaxDevices];
+
+// Large tiles move two thirds of the operands' bytes, but half as many of them run on a CU, one instead of two: they pay in long reductions and in many rounds, and not where they leave CUs idle.
+// `large` and `wide`: how often the 256 CUs are filled, were half of every expert's last tile used; the rest of the rule (a tile's time by its stages, what a first round costs more) is fitted to a
+// thousand sizes in both kinds, 64 to 1000 rows an expert on average, inputs from memory: 1.4 % above the better kind on average and 11 % in the worst twentieth (ten stages and 96 rows as the limits: 2.9 and 20 %).
+// us, 128 x 256 / 256 x 256, by the rows of an expert on average:
+//   gate_up, 32 of 7168 x 2048        100 146 / 132, 230 210 / 177, 512 363 / 301, 1000 646 / 506
+//   gate_up, 8 of 4096 x 14336        100 139 / 130, 230 201 / 177, 512 356 / 308, 1000 642 / 522
+//   gate_up, 256 of 2048 x 768        100 124 / 132, 230 187 / 177, 512 333 / 303, 1000 596 / 519
+//   gate_up, 64 of 512 x 1024         100 15 / 24, 230 22 / 26, 512 41 / 47, 1000 72 / 76
+//   product, 32 of 1408 x 2048        100 18 / 18, 230 25 / 28, 512 40 / 44, 1000 71 / 73
+//   product, 64 of 2048 x 1024        100 23 / 29, 230 34 / 34, 512 62 / 60, 1000 117 / 103
+//   product, 128 of 768 x 2048        100 44 / 48, 230 69 / 69, 512 126 / 118, 1000 216 / 204
+//   product, 8 of 4096 x 2048         100 21 / 21, 230 22 / 26, 512 37 / 29, 700 40 / 32
+// The rows are those that the buffer has room for: where few of them are used (a share of the experts), the choice may be the slower one.
+bool mx_large(int rows, int64_t experts, int col_tiles, int stages) {
+    if (rows / experts < kBigRows) return false;
+    const float large = (rows / 256.f + experts / 2.f) * col_tiles / 256.f, wide = (rows / 128.f + experts / 2.f) * col_tiles / 512.f;
+    return (0.56f + 1.5f / stages) * (large + 1.6f) < wide + 0.8f;
+}
 }  // namespace
 
 int mx_product_launch(const moe_mx_shape_t& s, bool gate, const uint8_t* a_codes, const uint8_t* a_scales, int64_t a_rows, const int32_t* perm, int k,
@@ -929,17 +948,7 @@ int mx_product_launch(const moe_mx_shape_t& s, bool gate, const uint8_t* a_codes
     p.w_codes = w_codes, p.w_scales = w_scales, p.u_codes = u_codes, p.u_scales = u_scales;
     p.offsets = offsets, p.y = y, p.f32 = f32, p.h_codes = h_codes, p.h_scales = h_scales;
     const int64_t experts = s.experts < s.rows ? s.experts : s.rows;
-    // Large tiles pay where the rows fill them and the reduction is long enough for what they do before and after it.  us, 128 x 256 / 256 x 256, by the rows of an expert on average:
-    //   gate_up, 32 of 7168 x 2048        48 107 / 109, 96 144 / 114, 250 205 / 171, 700 476 / 380
-    //   gate_up, 8 of 4096 x 14336        96 124 / 124, 160 166 / 146, 400 322 / 263, 700 544 / 458
-    //   gate_up, 128 of 2048 x 768        48 47 / 53, 96 60 / 57, 160 78 / 66, 400 129 / 129, 700 218 / 192
-    //   gate_up, 64 of 1024 x 512         96 14.4 / 12.7, 250 20.5 / 24.9, 700 45 / 48
-    //   product, 8 of 14336 x 4096        96 83 / 90, 160 85 / 99, 250 135 / 100, 700 232 / 200
-    //   product, 64 of 1408 x 2048        48 24 / 26, 96 35 / 29, 400 79 / 74, 700 117 / 114
-    //   product, 128 of 768 x 2048        96 37 / 37, 250 67 / 70, 400 95 / 95, 700 154 / 147
-    //   product, 64 of 512 x 1024         160 9.9 / 10.1, 400 17.6 / 23.9
-    // The rows are those that the buffer has room for: where few of them are used (a share of the experts), the choice may be the slower one, by 10 to 25 %.
-    if (p.stages >= kBigStages && s.rows / s.experts >= kBigRows) {
+    if (mx_large(s.rows, experts, p.col_tiles, p.stages)) {
         const int64_t most = (s.rows / 256 + experts) * p.col_tiles;
         return gate ? mx_launch(mx_big_kernel<true>, kBigThreads, kBigSmem, g_resident[3], most, p, st)
                     : mx_launch(mx_big_kernel<false>, kBigThreads, kBigSmem, g_resident[2], most, p, st);

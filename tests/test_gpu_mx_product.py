@@ -122,7 +122,7 @@ def test_experts_of_any_number_and_size(counts):
 @pytest.mark.parametrize("K,N", [(1280, 256), (1288, 264), (1408, 520), (2048, 136), (1544, 40), (4096, 128)])
 @pytest.mark.parametrize("counts", [[300, 5, 0, 257, 256, 64, 33, 1], [1000], [0, 97, 0, 230, 1], [191, 193, 512, 31, 224], [100] * 70])
 def test_many_rows_and_long_reductions(counts, K, N):
-    """Large tiles: from 96 rows an expert and 1280 values on; an odd and an even number of 128 values."""
+    """Full tiles and parts of them, in an odd and an even number of 128 values."""
     say(f"[mx product] {len(counts)} experts, {sum(counts)} rows, {K} {N}")
     check_product(make(counts, K, N, spare=3))
     check_gate_up(make(counts, K, N, tokens=77, k=2, pair=True))
@@ -252,3 +252,13 @@ def test_offsets_beyond_32_bits():
     y = moe.moe_mx_product(moe.make_mx_shape(7, K, N, E), a, w, offsets, perm=perm, out_dtype=F32)
     x, v = wide(tail), mx.values(last.codes[0], last.scales[0], K)
     near(y, x @ v.T, (K / 64 + 18) * 2.0 ** -23 * (x.abs() @ v.abs().T), "y")
+
+
+@pytest.mark.parametrize("counts,K,widths", [
+    ([1000], 4096, (15872, 7936)), ([1000], 1288, (40000, 20000)), ([1000], 896, (65536, 40968)), ([300, 5, 0, 513, 256, 64, 33, 1030], 4224, (6152, 3080)),
+    ([191, 193, 512, 31, 224], 4104, (14344, 7176)), ([97] * 24, 7168, (6400, 3208)), ([2500, 0, 1, 0, 31, 33, 255, 257], 1408, (16000, 8008)), ([577, 640], 768, (65536, 51200))])
+def test_large_tiles(counts, K, widths):
+    """Wide enough for tiles of 256 x 256 to fill the chip more than once: products, then gate and up."""
+    say(f"[mx product] {counts if len(counts) < 9 else len(counts)} {K} {widths}")
+    check_product(make(counts, K, widths[0], spare=3))
+    check_gate_up(make(counts, K, widths[1], tokens=77, k=2, pair=True))
