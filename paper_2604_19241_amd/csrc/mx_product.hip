@@ -4,23 +4,24 @@
 // src(r) = perm[r] / k where there is a table (the rows' tokens), else r.
 //
 // v_mfma_scale_f32_32x32x64_f8f6f4 takes 32 values of a row and one scale a lane: exactly a block.  It runs four times as many products a clock as the bf16 instruction on
-// as many bytes, so that a tile needs its operands as fast as a bf16 tile does, for four times the reduction.  At the row counts of a layer's experts (hundreds) the weights, read once
-// from memory, take longer than the matrix work.
+// as many bytes, so that a tile needs its operands as fast as a bf16 tile does, for four times the reduction.  Up to some 300 rows an expert the weights, read once from memory, take longer
+// than the matrix work.
 //
 // Tile: 128 rows by 256 columns (gate_up: 128 columns of each weight) by four waves, each with all rows of 64 columns: 4 x 2 accumulators of 32 x 32.  K advances 128 values a stage, 64 bytes
 // a row, by DMA into one of three images (24 KB); chunk c of row r lies at c ^ (r / 4 % 4), so that fragments are read without bank conflicts.  Two workgroups share a
 // CU (78 KB of LDS and 256 registers a lane each): one's first stages and stores run behind the other's matrix work, as a tile has only K / 128 stages.
 // Scales: four stages' bytes of a row are 16 of memory; they are moved a dword a lane into an image of their own, and one LDS read a fragment and four stages hands a lane its row's.
-// A lane takes values 32 (2 s + half) .. + 31 of sub-step s, so its scale is byte 2 s + half of the stage's dword: the dword is shifted by the half once, and the
-// instruction selects byte 0 or 2.
+// A lane takes values 32 (2 s + half) .. + 31 of sub-step s, so its scale is byte 2 s + half of the stage's dword: the bytes of its half in two stages' dwords are put into one, of which the
+// instruction selects one.
 //
 // Tiles are listed expert by expert, columns by columns, rows fastest, and dealt to the XCDs in eight runs: the tiles that share weights and rows meet in one L2.
 //
-// What bounds it.  The instruction alone runs at 6.5 PFLOP/s on normally distributed values, where the chip lowers its clock to 1.65 GHz, and at 9.8 on zeros.  4001 tokens on two of 8 experts each, gate and
-// up 4096 x 14336 (1.88 TFLOP): 516 us, with codes of zero 422; the matrix work alone 392 and the operands' way into LDS alone 352 to 375.  So what the
-// values cost in power is a fifth of it, and the rest is a tile's beginning and end (3.1 + 2.1 of 34 us).  8192 tokens on 8 of 128, down 768 x 2048: 94 to 118 us of which 76 are bytes.  37 tokens, 32 experts of 256
-// here, 7168 x 2048: 53 to 60 us for the weights of some 22 experts that have rows, 0.34 GB (a large copy: 65; some come from the cache of 256 MB).
-// Slower or nothing: the next tile's first stages requested before the stores (126 us for 120 in the second case), waves that only move operands (152 for 120), tiles of 256 x 256 with 64 bytes a row
+// What bounds it.  The instruction alone runs at 6.5 PFLOP/s on normally distributed values, where the chip lowers its clock to 1.65 GHz, and at 9.8 on zeros.  4001 tokens on two of 8 experts each,
+// gate and up 4096 x 14336 (1.88 TFLOP): 510 us, with codes of zero 422; the matrix work alone 392 and the operands' way into LDS alone 352 to 375.  So what the values cost in power is a sixth of it,
+// and the rest is a tile's beginning and end (3.1 + 2.1 of 34 us).  8192 tokens on 8 of 128 experts, down 768 x 2048: 94 us, with inputs from memory 110 to 120, of which 76 are bytes.  There it is what
+// goes through L2 (in tiles of 128 x 256: 127 us, without the stores 85, without the operands 73, with neither 50).  37 tokens, 32 experts of 256 here, 7168 x 2048: 53 to 71 us for the weights of
+// 22 to 26 experts that have rows, 0.34 to 0.40 GB (a large copy: 65 to 77; some come from the cache of 256 MB).
+// Slower or nothing: the next tile's first stages requested before the stores (127 us for 121 in the second case), waves that only move operands (152 for 120), tiles of 256 x 256 with 64 bytes a row
 // in four images (560 for 516), weights' lines requested into L2 ahead (548 for 530), XCDs' runs of equal cost instead of equal count (518 both), the operands' rows that a tile does not have left out
 // (514 both).
 #include "mma.hpp"

@@ -262,3 +262,27 @@ def test_large_tiles(counts, K, widths):
     say(f"[mx product] {counts if len(counts) < 9 else len(counts)} {K} {widths}")
     check_product(make(counts, K, widths[0], spare=3))
     check_gate_up(make(counts, K, widths[1], tokens=77, k=2, pair=True))
+
+
+def test_large_tiles_with_values_that_are_not_numbers_and_routings_that_do_not_fit():
+    counts, N = [600, 130, 270], 15880
+    say("[mx product] large tiles, not finite")
+    s = make(counts, 4096, N, tokens=700, k=2, spare=3, pair=True, seed=9)
+    s["perm"][:1000] = torch.arange(1000, device="cuda")
+    run = lambda: (moe.moe_mx_product(s["shape"], s["a"], s["w"], s["offsets"], perm=s["perm"], k=2), moe.moe_mx_gate_up(s["shape"], s["a"], s["w"], s["u"], s["offsets"], perm=s["perm"], k=2))  # noqa: E731
+    clean = run()
+    s["a"].scales[200, 77] = 255               # rows 400 and 401
+    s["w"].scales[2, N - 1, 3] = 255
+    bad = torch.zeros((1003, N), dtype=torch.bool, device="cuda")
+    bad[400:402] = True
+    bad[730:1000, N - 1] = True
+    bad[1000:] = True                          # (nobody's)
+    for got, want in zip(run(), clean):
+        assert torch.isnan(got[:1000][bad[:1000]]).all() and torch.equal(got[~bad], want[~bad])
+    s["a"].scales[200, 77], s["w"].scales[2, N - 1, 3] = 127, 127
+    clean = run()
+    s["perm"][5], s["perm"][999], s["perm"][1001] = -9, 2 ** 31 - 1, 2 ** 31 - 1
+    s["offsets"] = torch.tensor([-4, 600, 730, 2 ** 31 - 1], dtype=torch.int32, device="cuda")
+    fine = [r for r in range(1000) if r not in (5, 999)]
+    for got, want in zip(run(), clean):
+        assert torch.equal(got[fine], want[fine])
