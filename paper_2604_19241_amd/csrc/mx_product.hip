@@ -22,8 +22,8 @@
 // goes through L2 (in tiles of 128 x 256: 127 us, without the stores 85, without the operands 73, with neither 50).  37 tokens, 32 experts of 256 here, 7168 x 2048: 53 to 71 us for the weights of
 // 22 to 26 experts that have rows, 0.34 to 0.40 GB (a large copy: 65 to 77; some come from the cache of 256 MB).
 // Slower or nothing: the next tile's first stages requested before the stores (127 us for 121 in the second case), waves that only move operands (152 for 120), tiles of 256 x 256 with 64 bytes a row
-// in four images (560 for 516), by four waves of 128 x 128 (548 for 515), with the requests of a stage between its last products (514 to 518 for 510), weights' lines requested into L2 ahead (548 for 530), XCDs' runs of equal cost instead of equal count (518 both), the operands' rows that a tile does not have left out
-// (514 both).
+// in four images (560 for 516), by four waves of 128 x 128 (548 for 515), with the requests of a stage between its last products (514 to 518 for 510), weights' lines requested into L2 ahead
+// (548 for 530), XCDs' runs of equal cost instead of equal count (518 both), the operands' rows that a tile does not have left out (514 both).
 #include "mma.hpp"
 #include "mx.hpp"
 
