@@ -378,14 +378,13 @@ struct Stash {
     moe_routing_t routing = {};
     void* saved;
     int64_t rows;
-    // offsets, saved
-    Stash(const On& on, const moe_shape_t& s, PyObject* const* v) {
+    // offsets, saved; at_h: where the stash's h begins
+    Stash(const On& on, const moe_shape_t& s, size_t at_h, PyObject* const* v) {
         rows = (int64_t)s.T * s.k;
         routing.offsets = (const int32_t*)on.dense(v[0], "routing.offsets", at::kInt, {(int64_t)s.e_count + 1});
         const at::Tensor& t = tensor(v[1], "saved");
         on.here(t, "saved");
-        const int64_t need = (rows * 4 * s.I + 255) / 256 * 256 + rows * 2 * s.I;   // up to h's end
-        if (t.scalar_type() != at::kByte || !t.is_contiguous() || t.numel() < need) refuse("saved", "expected a stash of this shape");
+        if (t.scalar_type() != at::kByte || !t.is_contiguous() || t.numel() < (int64_t)at_h + rows * 2 * s.I) refuse("saved", "expected a stash of this shape");
         saved = t.data_ptr();
     }
 };
@@ -413,11 +412,14 @@ PyObject* saved_pack(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return guarded(n, 6, [&]() -> PyObject* {
         const auto s = shape_at<moe_shape_t>(v[0]);
         const On on(v[2], "saved");
-        const Stash in(on, s, v + 1);
+        size_t at_h;
+        int rc = p_saved_layout(&s, nullptr, &at_h, nullptr);
+        if (rc != MOE_OK) return code_of(rc);
+        const Stash in(on, s, at_h, v + 1);
         const at::Tensor codes = on.output(v[3], "codes", at::kChar, {in.rows, 2 * (int64_t)s.I});
         const at::Tensor scales = on.output(v[4], "scales", at::kByte, {in.rows, (int64_t)s.I / 16});
         void* const stream = stream_of(v[5]);
-        const int rc = call([&] { return p_saved_pack(&s, &in.routing, in.saved, codes.data_ptr(), scales.data_ptr(), stream); });
+        rc = call([&] { return p_saved_pack(&s, &in.routing, in.saved, codes.data_ptr(), scales.data_ptr(), stream); });
         return rc != MOE_OK ? code_of(rc) : wrapped({codes, scales});
     });
 }
@@ -427,11 +429,14 @@ PyObject* saved_unpack(PyObject*, PyObject* const* v, Py_ssize_t n) {
     return guarded(n, 6, [&]() -> PyObject* {
         const auto s = shape_at<moe_shape_t>(v[0]);
         const On on(v[2], "saved");
-        const Stash out(on, s, v + 1);
+        size_t at_h;
+        int rc = p_saved_layout(&s, nullptr, &at_h, nullptr);
+        if (rc != MOE_OK) return code_of(rc);
+        const Stash out(on, s, at_h, v + 1);
         const void* codes = on.dense(v[3], "codes", at::kChar, {out.rows, 2 * (int64_t)s.I});
         const void* scales = on.dense(v[4], "scales", at::kByte, {out.rows, (int64_t)s.I / 16});
         void* const stream = stream_of(v[5]);
-        const int rc = call([&] { return p_saved_unpack(&s, &out.routing, codes, scales, out.saved, stream); });
+        rc = call([&] { return p_saved_unpack(&s, &out.routing, codes, scales, out.saved, stream); });
         if (rc != MOE_OK) return code_of(rc);
         Py_RETURN_NONE;
     });
