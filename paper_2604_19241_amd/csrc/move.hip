@@ -6,7 +6,7 @@
 // Slots whose row is outside the buffer have none: nothing is read or written for them.  dx is y with weights of one.  Every wave has a token's run of columns, so two slots that name
 // one row leave some of its columns from either token.
 //
-// Nothing is computed that memory could wait for: every token's side is read or written once, by the lanes that have all of its rows, so the k copies of a
+// Nothing is computed that memory could wait for: every token's side is read or written once (by combine's gradients once for eight slots), by the lanes that have all of its rows, so the k copies of a
 // token come from registers and its sum needs no pass over a sorted buffer.  Sums are fp32 in the order of the slots (dw: lanes, then waves), rounded once.
 // bf16, 8192 tokens of 2048 with 8 rows each: dispatch 57 us (5.3 TB/s of 302 MB), its gradient 52 (5.9).  fp32, 4099 tokens of 2304 with two rows here on average: combine 21 us (5.5),
 // its gradients 36 (5.3).  A large copy: 5.3.  One token: 2.5 us, the launch and two loads in a row.
@@ -141,6 +141,8 @@ __global__ void __launch_bounds__(64 * kTailWaves) combine_kernel(MoveParams p, 
 }
 
 // do and dw: a workgroup a token, as dw is a sum over all of its columns.  dy is read once for eight slots and stays in registers between the rows' products and their stores.
+// Narrow rows leave threads, or whole waves, without columns, and a token costs its workgroup and its sums all the same.  us, 65536 tokens in bf16, 2 / 8 / 16 rows each: 64 columns 90 / 119 / 213 (combine
+// itself 18 / 32 / 51), 256 98 / 141 / 249, 512 109 / 214 / 429, 1024 130 / 430 / 855, 2048 220 / 872 / 1727 (5.1 to 6.1 TB/s).
 template <bool F32>
 __global__ void __launch_bounds__(64 * kTailWaves) combine_backward_kernel(MoveParams p, uint32_t first) {
     using P = Piece<F32>;

@@ -4,7 +4,7 @@
 //   4 bits   value = 2^(e - 2) * {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign (e2m1), nearest, ties to even, magnitudes beyond 6 become 6
 //   8 bits   value = 2^(e - 6) * q, q whole from -127 to 127, nearest, ties to even, 128 becomes 127
 // The exponent is kept as a byte with a bias of 127; 255 stands for a block that holds an infinity or NaN, and all of it is NaN then.  Both kinds of
-// values are exact in bf16: two and seven significant bits, and nothing below 2^-133.
+// values are exact in bf16: two and seven significant bits, and nothing below 2^-132.
 #pragma once
 #include "common.hpp"
 
@@ -19,7 +19,7 @@ constexpr uint32_t kMxNan = 255;
 __device__ __forceinline__ uint32_t mag(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 // floor(log2 m) of a magnitude m > 0; subnormal ones count as the smallest normal (their blocks' exponents are at the lower end anyway).
 __device__ __forceinline__ int exponent_of(uint32_t m) { return max((int)(m >> 23), 1) - 127; }
-// The shared byte: of 2^(e - 2), and of 2^(e - 6) + 6.  Blocks whose scale would be below 2^-127 (2^-133) have that.
+// The shared byte: of 2^(e - 2), and of 2^(e - 6) + 6.  Blocks whose scale would be below 2^-127 (in 8 bits 2^-132) have that; in 8 bits a byte of 0 is a block of zeros.
 __device__ __forceinline__ uint32_t mx4_byte(uint32_t m) { return m >= 0x7f800000u ? kMxNan : (uint32_t)max(exponent_of(m) + 125, 0); }
 __device__ __forceinline__ uint32_t mx8_byte(uint32_t m) { return m >= 0x7f800000u ? kMxNan : (uint32_t)(m == 0u ? 0 : exponent_of(m) + 127); }
 // 2^(byte - 127)

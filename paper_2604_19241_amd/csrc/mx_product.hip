@@ -16,11 +16,17 @@
 //
 // Tiles are listed expert by expert, columns by columns, rows fastest, and dealt to the XCDs in eight runs: the tiles that share weights and rows meet in one L2.
 //
-// What bounds it.  The instruction alone runs at 6.5 PFLOP/s on normally distributed values, where the chip lowers its clock to 1.65 GHz, and at 9.8 on zeros.  4001 tokens on two of 8 experts each,
-// gate and up 4096 x 14336 (1.88 TFLOP): 510 us, with codes of zero 422; the matrix work alone 392 and the operands' way into LDS alone 352 to 375.  So what the values cost in power is a sixth of it,
-// and the rest is a tile's beginning and end (3.1 + 2.1 of 34 us).  8192 tokens on 8 of 128 experts, down 768 x 2048: 94 us, with inputs from memory 110 to 120, of which 76 are bytes.  There it is what
-// goes through L2 (in tiles of 128 x 256: 127 us, without the stores 85, without the operands 73, with neither 50).  37 tokens, 32 experts of 256 here, 7168 x 2048: 53 to 71 us for the weights of
-// 22 to 26 experts that have rows, 0.34 to 0.40 GB (a large copy: 65 to 77; some come from the cache of 256 MB).
+// What bounds it.  The instruction alone runs at 6.5 PFLOP/s on normally distributed values, where the chip lowers its clock to 1.65 GHz, and at 9.8 on zeros.  In large tiles the operands' way through
+// L2 into LDS takes longer than the matrix work, and the two do not overlap whole.  us with parts of the loop left out (the stores and a tile's ends are in all of them):
+//                                                           whole   requests alone   matrix work alone   neither, without reads of LDS
+//   gate_up, 8 of 4096 x 14336, 8002 rows (1.88 TFLOP)        529              436                 372                              77
+//   gate_up, 256 of 2048 x 768, 512 rows each                 300              257                 206                              69
+//   gate_up, 32 of 7168 x 2048, 512 rows each                 314              275                 207                              36
+//   product, 128 of 768 x 2048, 512 rows each                 120              102                  84                              58
+// Between the ends the first one's matrix work takes 295 us, the instruction's own rate, and its requests 359: 38 million of up to 128 bytes to L2, a fifth of them for the scales' 32 bytes a row.  The
+// reads of fragments from LDS cost it 8 us (LDS is busy a quarter of the time, without bank conflicts).  With codes of zero, whose matrix work is done in two thirds, it took 422 us where random ones took
+// 510; by the clock that a chip holds it is 510 to 551.  The last one is 111 to 118 with inputs in the cache (93 at best), 110 to 130 from memory, of which 76 are bytes.  37 tokens, 32 experts of 256
+// here, 7168 x 2048: 53 to 71 us for the weights of 22 to 26 experts that have rows, 0.34 to 0.40 GB (a large copy: 65 to 77; some come from the cache of 256 MB).
 // Slower or nothing: the next tile's first stages requested before the stores (127 us for 121 in the second case), waves that only move operands (152 for 120), tiles of 256 x 256 with 64 bytes a row
 // in four images (560 for 516), by four waves of 128 x 128 (548 for 515), with the requests of a stage between its last products (514 to 518 for 510), weights' lines requested into L2 ahead
 // (548 for 530), XCDs' runs of equal cost instead of equal count (518 both), the operands' rows that a tile does not have left out (514 both).
@@ -701,6 +707,8 @@ __device__ __forceinline__ void mx_store_h(const MxParams& p, const MxTile& t, c
     }
     // The wave's 32 columns are a block: 16 values in either half of the wave.  What is quantised is h as the bf16 result would be, so that both ways
     // to the next product give the same bits (a second rounding of 2^-8 before one of 2^-2).
+    // A lane's 8 bytes and a block's byte leave as they are, in pieces of a row; a quarter of the bytes takes as long as the bf16 result.  us, 4 bits / bf16: 8 of 4096 x 14336, 8002 rows 517 / 512; 128 of 2048 x 768, 65536 rows
+    // 154 / 153, 8 rows 7.7 / 7.5; 7168 x 2048 for 37 tokens 63 / 63; where the reductions are short, 64 of 512 x 1024, 8192 rows 16.3 / 15.5, 32768 rows 43 / 41.
     const int pitch = mx_padded(p.N);
     if (col0 >= pitch) return;
 #pragma unroll
@@ -926,7 +934,15 @@ int g_resident[4][kMaxDevices];
 //   product, 64 of 2048 x 1024        100 23 / 29, 230 34 / 34, 512 62 / 60, 1000 117 / 103
 //   product, 128 of 768 x 2048        100 44 / 48, 230 69 / 69, 512 126 / 118, 1000 216 / 204
 //   product, 8 of 4096 x 2048         100 21 / 21, 230 22 / 26, 512 37 / 29, 700 40 / 32
-// The rows are those that the buffer has room for: where few of them are used (a share of the experts), the choice may be the slower one.
+// The rows are those that the buffer has room for, as only the device knows how many there are; a share of the experts fills its part of them, and the choice may be the slower one.  Of 144 shares (1/4, 1/8
+// and 1/16 of 128 and 256 experts, 256 to 8192 tokens of 8, products of 768 x 2048 and 2048 x 7168, gate_up of 2048 x 768 and 7168 x 2048) 90 are done in large tiles and take 6 % more than in
+// the better kind on average, 24 % in the worst twentieth; by the rows that are there it would be 2.5 and 17 %.  us, 128 x 256 / 256 x 256:
+//   gate_up, 16 of 128 of 7168 x 2048   256 tokens 53 / 56, 1024 78 / 62, 2048 91 / 93, 8192 200 / 171
+//   gate_up, 32 of 256 of 2048 x 768    2048 tokens 15 / 17, 4096 22 / 20, 8192 25 / 35
+//   gate_up, 8 of 128 of 7168 x 2048    256 tokens 38 / 48, 2048 46 / 56, 4096 66 / 56
+//   product, 32 of 256 of 768 x 2048    4096 tokens 13 / 17, 8192 17 / 20
+//   product, 16 of 128 of 2048 x 7168   512 tokens 30 / 34, 2048 42 / 41, 8192 106 / 97
+// The 256 CUs are the whole chip's; a part of it as a device of its own would be filled more often than the rule says.
 bool mx_large(int rows, int64_t experts, int col_tiles, int stages) {
     if (rows / experts < kBigRows) return false;
     const float large = (rows / 256.f + experts / 2.f) * col_tiles / 256.f, wide = (rows / 128.f + experts / 2.f) * col_tiles / 512.f;
